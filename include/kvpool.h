@@ -581,6 +581,154 @@ int kv_probe_copy_kernel(void *dst, const void *src, uint64_t bytes, uint32_t gr
  * engines' rate over the same buffers.  Errors: HIP. */
 int kv_probe_memcpy(void *dst, const void *src, uint64_t bytes, void *stream);
 
+/* ---- operators on the engine's paged cache ----
+ *
+ * What an engine computes on the cache that store and retrieve move: rotary
+ * positions on the way into it, attention over it, the attention weight of
+ * its tokens, and eviction by that weight.  They need no pool.  A call works
+ * on one layer, on `stream` of the current device, and only launches kernels
+ * (it allocates nothing, waits for nothing, and may be captured into a
+ * graph).  All pointers except those of the structures themselves are device
+ * memory.  Everything checkable on the host is checked before any launch;
+ * lengths and block tables lie in device memory and are clamped by the
+ * kernels to what the batch says, so a wrong one gives a wrong result and no
+ * access outside the buffers.  Errors of every call: INVALID (an argument),
+ * HIP.
+ */
+#define KVP_BF16 0u
+#define KVP_F16  1u
+
+/* The cache of a layer and the heads over it. */
+typedef struct {
+    uint32_t dtype;           /* KVP_BF16 or KVP_F16: queries, cache and outputs */
+    uint32_t num_q_heads;     /* a multiple of num_kv_heads; head h reads KV head h / (num_q_heads / num_kv_heads) */
+    uint32_t num_kv_heads;
+    uint32_t head_dim;        /* a multiple of 8, at most 256 */
+    uint32_t block_size;      /* tokens per slot */
+    uint32_t num_slots;       /* slots of the K and of the V buffer; num_slots * num_kv_heads * block_size < 2^32 */
+    uint32_t reserved;        /* 0 */
+} kvp_cache_shape;
+
+/*
+ * A batch of sequences over the cache.  Each has n_q = cu_q[s+1] - cu_q[s]
+ * new tokens, packed one sequence after the other, and kv_len[s] cached
+ * tokens, the new ones included: new token i has cache index
+ * kv_len[s] - n_q + i.  Cached token j lies in slot
+ * block_table[s * table_stride + j / block_size]; an entry outside
+ * [0, num_slots) is absent: no query sees its tokens and nothing is written
+ * there.  A sequence may have no new token, or no cached one.
+ */
+typedef struct {
+    uint32_t n_seq;
+    uint32_t total_q;         /* cu_q[n_seq] */
+    uint32_t max_q;           /* at least the new tokens of any sequence */
+    uint32_t max_kv;          /* at least the cached tokens of any sequence, at most table_stride * block_size */
+    uint32_t table_stride;
+    uint32_t reserved;        /* 0 */
+    const int32_t *cu_q;      /* [n_seq + 1], ascending from 0; not used by kv_evict */
+    const int32_t *kv_len;    /* [n_seq] */
+    const int32_t *block_table; /* [n_seq][table_stride] */
+} kvp_batch;
+
+/* How rotary frequencies f_j = base^(-2j / rot_dim) are scaled for contexts longer than the trained one. */
+#define KVP_ROPE_PLAIN          0u  /* not at all */
+#define KVP_ROPE_LINEAR         1u  /* all: f / factor */
+#define KVP_ROPE_BY_PARTS       2u  /* f (g + (1 - g) / factor); with r the turns that f makes over original_length,
+                                       g = (r - alpha) / (beta - alpha), limited to [0, 1] */
+#define KVP_ROPE_BY_PARTS_INDEX 3u  /* the same with g linear in j instead: 1 where f_j makes beta turns, 0 where alpha */
+typedef struct {
+    uint32_t kind;            /* KVP_ROPE_* above */
+    uint32_t reserved;        /* 0 */
+    double base, factor, original_length, alpha, beta;
+    double magnitude;         /* cosines and sines are multiplied by it; 1 for none */
+} kvp_rope_scaling;
+
+/* Fills table[n_positions][rot_dim / 2][2] with the cosine and sine of position * frequency, computed in 64 bits
+ * and rounded to 32.  rot_dim is even, from 2 to 256; table is 8-byte aligned. */
+int kv_rope_table(float *table, uint32_t n_positions, uint32_t rot_dim, const kvp_rope_scaling *scaling, void *stream);
+
+#define KVP_ROPE_INTERLEAVED 1u   /* pairs (2j, 2j + 1); else (j, j + rot_dim / 2) */
+
+/*
+ * Rotates the new tokens' queries and keys and writes them, with the values,
+ * where attention reads them.
+ *   table[n_positions][rot_dim / 2][2]  from kv_rope_table, or any other.
+ *   rot_dim      the first rot_dim elements of a head turn, the others stay; 0: none.
+ *   flags        0 or KVP_ROPE_INTERLEAVED.
+ *   positions[total_q]  a token's position; one outside [0, n_positions) makes its query and key NaN.
+ *   q, k, v      [total_q][heads][head_dim], strides in elements between tokens (multiples of 8; a fused
+ *                projection's output can be passed as it is).  q and q_out may both be NULL.
+ *   q_out        the rotated queries; must not overlap q.
+ *   k_cache, v_cache  receive keys and values at the tokens' cache indexes.
+ *   pos[n_seq][num_kv_heads][pos_stride]  NULL, or receives every new token's position at its cache index:
+ *                the list that kv_evict takes.
+ * Pointers of 16-bit data are 16-byte aligned, here and below.
+ */
+int kv_rope_append(const kvp_cache_shape *shape, const kvp_batch *batch, const float *table, uint32_t n_positions,
+                   uint32_t rot_dim, uint32_t flags, const int32_t *positions, const void *q, uint64_t q_stride,
+                   void *q_out, uint64_t q_out_stride, const void *k, uint64_t k_stride, const void *v,
+                   uint64_t v_stride, void *k_cache, void *v_cache, int32_t *pos, uint32_t pos_stride, void *stream);
+
+/*
+ * Causal attention of the new tokens over the cached ones: single tokens,
+ * chunks and whole prompts, mixed in a batch.  A new token at cache index c
+ * sees the cached tokens j <= c (and, with a window, j > c - window).
+ *   q[total_q][num_q_heads][head_dim], q_stride as above.
+ *   scale        positive; logits are scale * q . k.
+ *   window       0: none.
+ *   sinks[num_q_heads]  NULL, or a logit per head that takes part in the softmax without a value.
+ *   out          as q; a token that sees nothing gets 0.
+ *   lse[num_q_heads][total_q]  NULL, or the logarithm of each row's sum of exponentials, sink included
+ *                (-inf for an empty one): what kv_attention_mass takes.
+ *   workspace    of kv_attention_workspace bytes, 16-byte aligned, in use until the call's kernels are done.
+ */
+int kv_attention(const kvp_cache_shape *shape, const kvp_batch *batch, const void *q, uint64_t q_stride,
+                 const void *k_cache, const void *v_cache, float scale, uint32_t window, const float *sinks,
+                 void *out, uint64_t out_stride, float *lse, void *workspace, uint64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace that kv_attention needs for this shape and batch (only its four sizes count); may be 0. */
+int kv_attention_workspace(const kvp_cache_shape *shape, const kvp_batch *batch, uint64_t *bytes);
+
+/*
+ * The attention weight that each cached token collects from the last `last`
+ * new tokens of its sequence (0: from all), over all query heads of its KV
+ * head:
+ *   score_out[s][h][j] = score_in[s][h][j] + sum over queries of exp(logit - lse)
+ * for j < kv_len[s]; entries from kv_len[s] on are not written.  q, scale and
+ * window as in the kv_attention call that made lse.
+ *   score_in     NULL for 0; may be score_out.
+ *   score_*[n_seq][num_kv_heads][score_stride]
+ * Sums run in a fixed order: the same inputs give the same bits.
+ */
+int kv_attention_mass(const kvp_cache_shape *shape, const kvp_batch *batch, const void *q, uint64_t q_stride,
+                      const void *k_cache, float scale, uint32_t window, const float *lse, uint32_t last,
+                      const float *score_in, float *score_out, uint32_t score_stride, void *stream);
+
+/*
+ * Evicts from every sequence and KV head all but keep[s] tokens and compacts
+ * the cache in place.  The kept ones are the first by this order: protected
+ * tokens (position >= protect[s]), then by score (a NaN below every number),
+ * then by lower index.  Kept tokens at index >= keep[s] move, in ascending
+ * order, into the indexes below keep[s] that fell free; the others stay where
+ * they are.  A sequence with at most keep[s] tokens stays as it is.
+ *   keep[n_seq], protect[n_seq]   protect may be NULL: none is protected.
+ *   score_in, score_out[n_seq][num_kv_heads][score_stride]   scores move with their tokens; those from the new
+ *                length to the old one become 0.  May be the same array.
+ *   pos_in, pos_out[n_seq][num_kv_heads][pos_stride]   positions, moved likewise (the tail is left as it is).
+ *                pos_in NULL: a token's position is its index; pos_out NULL: not written.  May be the same.
+ *   k_cache, v_cache   of slots that no other sequence shares.
+ *   len_out[n_seq]     min(kv_len[s], keep[s]); may be batch->kv_len.
+ *   workspace    of kv_evict_workspace bytes, 16-byte aligned.
+ * The slots past the new length are free afterwards.
+ */
+int kv_evict(const kvp_cache_shape *shape, const kvp_batch *batch, const int32_t *keep, const int32_t *protect,
+             const float *score_in, float *score_out, uint32_t score_stride, const int32_t *pos_in, int32_t *pos_out,
+             uint32_t pos_stride, void *k_cache, void *v_cache, int32_t *len_out, void *workspace,
+             uint64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace that kv_evict needs for this shape and batch. */
+int kv_evict_workspace(const kvp_cache_shape *shape, const kvp_batch *batch, uint64_t *bytes);
+
 #ifdef __cplusplus
 }
 #endif

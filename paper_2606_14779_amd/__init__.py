@@ -6,7 +6,9 @@ loaded on first use so that ``build`` can run before the library exists.
 """
 
 _BINDING = ("KVPool", "KVPoolError", "KVSpec", "Region", "allowed_numa_nodes", "counts",
-            "probe_copy_kernel", "probe_memcpy", "LOC_DTYPE", "ABSENT", "EXPORTED")
+            "probe_copy_kernel", "probe_memcpy", "LOC_DTYPE", "ABSENT", "EXPORTED",
+            "CacheShape", "Batch", "rope_table", "rope_append", "attention", "attention_workspace", "attention_mass",
+            "evict", "evict_workspace")
 
 
 def __getattr__(name):

@@ -77,7 +77,7 @@ def build(verbose: bool = False, extra: list[str] | None = None) -> str:
         os.replace(exe + ".tmp", exe)
         # the same client over a host-sanitized build of the library (its own file: g++ only)
         from . import build_asan
-        build_asan.build(os.path.join(BUILD, "kernels.hip.o"))
+        build_asan.build([o for o in objs if o.endswith(".hip.o")])
     if verbose:
         print("built", LIB)
     return LIB

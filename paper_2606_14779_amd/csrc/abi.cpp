@@ -28,6 +28,18 @@ void pool_last_timing(Pool &, kvp_timing *);
 void pool_timing_summary(Pool &, kvp_timing_summary *);
 void pool_measure(Pool &, uint64_t, uint32_t, uint64_t *);
 void pool_set_bandwidths(Pool &, const uint64_t *);
+void op_rope_table(float *, uint32_t, uint32_t, const kvp_rope_scaling *, void *);
+void op_rope_append(const kvp_cache_shape *, const kvp_batch *, const float *, uint32_t, uint32_t, uint32_t,
+                    const int32_t *, const void *, uint64_t, void *, uint64_t, const void *, uint64_t, const void *,
+                    uint64_t, void *, void *, int32_t *, uint32_t, void *);
+void op_attention(const kvp_cache_shape *, const kvp_batch *, const void *, uint64_t, const void *, const void *, float,
+                  uint32_t, const float *, void *, uint64_t, float *, void *, uint64_t, void *);
+void op_attention_workspace(const kvp_cache_shape *, const kvp_batch *, uint64_t *);
+void op_attention_mass(const kvp_cache_shape *, const kvp_batch *, const void *, uint64_t, const void *, float, uint32_t,
+                       const float *, uint32_t, const float *, float *, uint32_t, void *);
+void op_evict(const kvp_cache_shape *, const kvp_batch *, const int32_t *, const int32_t *, const float *, float *,
+              uint32_t, const int32_t *, int32_t *, uint32_t, void *, void *, int32_t *, void *, uint64_t, void *);
+void op_evict_workspace(const kvp_cache_shape *, const kvp_batch *, uint64_t *);
 }  // namespace kvp
 
 struct kvp_pool {
@@ -291,6 +303,63 @@ int kv_probe_memcpy(void *dst, const void *src, uint64_t bytes, void *stream)
         kvp::check_hip(hipMemcpyAsync(dst, src, bytes, hipMemcpyDefault, static_cast<hipStream_t>(stream)),
                        "hipMemcpyAsync");
     });
+}
+
+int kv_rope_table(float *table, uint32_t n_positions, uint32_t rot_dim, const kvp_rope_scaling *scaling, void *stream)
+{
+    return guarded([&] { kvp::op_rope_table(table, n_positions, rot_dim, scaling, stream); });
+}
+
+int kv_rope_append(const kvp_cache_shape *shape, const kvp_batch *batch, const float *table, uint32_t n_positions,
+                   uint32_t rot_dim, uint32_t flags, const int32_t *positions, const void *q, uint64_t q_stride,
+                   void *q_out, uint64_t q_out_stride, const void *k, uint64_t k_stride, const void *v,
+                   uint64_t v_stride, void *k_cache, void *v_cache, int32_t *pos, uint32_t pos_stride, void *stream)
+{
+    return guarded([&] {
+        kvp::op_rope_append(shape, batch, table, n_positions, rot_dim, flags, positions, q, q_stride, q_out,
+                            q_out_stride, k, k_stride, v, v_stride, k_cache, v_cache, pos, pos_stride, stream);
+    });
+}
+
+int kv_attention(const kvp_cache_shape *shape, const kvp_batch *batch, const void *q, uint64_t q_stride,
+                 const void *k_cache, const void *v_cache, float scale, uint32_t window, const float *sinks, void *out,
+                 uint64_t out_stride, float *lse, void *workspace, uint64_t workspace_bytes, void *stream)
+{
+    return guarded([&] {
+        kvp::op_attention(shape, batch, q, q_stride, k_cache, v_cache, scale, window, sinks, out, out_stride, lse,
+                          workspace, workspace_bytes, stream);
+    });
+}
+
+int kv_attention_workspace(const kvp_cache_shape *shape, const kvp_batch *batch, uint64_t *bytes)
+{
+    return guarded([&] { kvp::op_attention_workspace(shape, batch, bytes); });
+}
+
+int kv_attention_mass(const kvp_cache_shape *shape, const kvp_batch *batch, const void *q, uint64_t q_stride,
+                      const void *k_cache, float scale, uint32_t window, const float *lse, uint32_t last,
+                      const float *score_in, float *score_out, uint32_t score_stride, void *stream)
+{
+    return guarded([&] {
+        kvp::op_attention_mass(shape, batch, q, q_stride, k_cache, scale, window, lse, last, score_in, score_out,
+                               score_stride, stream);
+    });
+}
+
+int kv_evict(const kvp_cache_shape *shape, const kvp_batch *batch, const int32_t *keep, const int32_t *protect,
+             const float *score_in, float *score_out, uint32_t score_stride, const int32_t *pos_in, int32_t *pos_out,
+             uint32_t pos_stride, void *k_cache, void *v_cache, int32_t *len_out, void *workspace,
+             uint64_t workspace_bytes, void *stream)
+{
+    return guarded([&] {
+        kvp::op_evict(shape, batch, keep, protect, score_in, score_out, score_stride, pos_in, pos_out, pos_stride,
+                      k_cache, v_cache, len_out, workspace, workspace_bytes, stream);
+    });
+}
+
+int kv_evict_workspace(const kvp_cache_shape *shape, const kvp_batch *batch, uint64_t *bytes)
+{
+    return guarded([&] { kvp::op_evict_workspace(shape, batch, bytes); });
 }
 
 }  // extern "C"

@@ -1,0 +1,692 @@
+// Attention of new tokens over the paged cache, for gfx950 (MI355X).
+//
+// For a new token i of a sequence at cache index c_i, a query head and its KV head:
+//   S_j = scale * q_i . k_j   for the cached tokens j with c_i - window < j <= c_i
+//   o_i = sum_j exp(S_j - lse_i) v_j,   lse_i = log(sum_j exp S_j + exp sink)
+// in one pass over the keys, with a running maximum m and sum l per row (all in 32 bits; weights are
+// exp2(S log2e - m log2e), so the exponential is one instruction).
+//
+// The rows of a KV head are its (new token, query head of the group) pairs, token-major: every key and
+// value that is fetched serves the whole group.  Both kernels compute S transposed, S^T = K Q^T: a lane
+// then owns one row (column of the MFMA result), so maximum and sum are per-lane values, and the lane's
+// results, rounded to 16 bits, already are the B operand of O^T = V^T P^T, with no exchange between lanes:
+// the order of the keys inside a product is free, and V's transposed LDS reads follow the order that the
+// first product left.
+//
+// attention_rows: 32 rows to a wave, kTileRows to a workgroup, kTileKeys keys at a time through LDS.
+// attention_few: up to 16 rows (single tokens and very short chunks), where reading the cache is all that
+// counts: the waves of a workgroup split the keys, and a join in LDS ends the workgroup.
+// Where there are few row tiles both split the keys over workgroups as well; attention_join adds the parts.
+
+#include "wave.hpp"
+
+namespace kvp {
+
+namespace {
+
+// Sum of a row's weights with the sink's, and its logarithm: what a finished row needs.
+struct RowEnd {
+    float scale_o;   // of the accumulated output
+    float lse;
+};
+__device__ __forceinline__ RowEnd finish_row(float m, float l, const float *sinks, uint32_t head)
+{
+    float f = 1.0f;
+    if (sinks) {
+        const float s = sinks[head] * kLog2e;
+        const float top = fmaxf(m, s);
+        f = exp2_fast(m - top);
+        l = l * f + exp2_fast(s - top);
+        m = top;
+    }
+    // an empty row has l = 0 (and no sink): output 0, lse -inf
+    return {l == 0.0f ? 0.0f : f / l, l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2};
+}
+
+struct Split {
+    int32_t begin, end;   // keys
+};
+// Keys of one workgroup: what its rows can see, cut into the launch's parts.
+__device__ __forceinline__ Split keys_of(const AttentionArgs &a, const Seq &s, int32_t first_token, int32_t last_token,
+                                         uint32_t split)
+{
+    const int32_t shift = s.kv - s.n_q;
+    int32_t lo = 0;
+    if (a.window) lo = (int32_t)max((int64_t)0, (int64_t)(shift + first_token) + 1 - (int64_t)a.window);
+    lo &= ~(int32_t)(kTileKeys - 1);
+    const int32_t hi = min(shift + last_token + 1, s.kv);
+    const int64_t begin = (int64_t)lo + (int64_t)split * a.split_keys;
+    const int64_t end = split + 1 == a.splits ? (int64_t)hi : min((int64_t)hi, begin + (int64_t)a.split_keys);
+    return {(int32_t)min(begin, (int64_t)max(hi, 0)), (int32_t)max(end, (int64_t)0)};
+}
+
+// ---- 32 rows to a wave
+
+template <class T, int DP, int NW>
+__global__ __launch_bounds__(NW * 64, DP > 128 ? 1 : 2) void attention_rows(const AttentionArgs a)
+{
+    constexpr int TK = kTileKeys;
+    constexpr int CH = DP / 8;                       // 16-byte pieces of a row
+    constexpr int PASS = NW * 64 / CH;               // rows that the workgroup loads at once
+    constexpr int N = TK / PASS;
+    __shared__ __align__(16) uint16_t lds_k[2][TK * DP], lds_v[2][TK * DP];
+
+    const CacheView &c = a.c;
+    const uint32_t kv_head = blockIdx.x % c.kv_heads;
+    const uint32_t rest = blockIdx.x / c.kv_heads;
+    const uint32_t split = rest % a.splits;
+    // later tiles first: under a causal mask they have the most keys
+    const uint32_t tile = a.tiles - 1 - rest / a.splits;
+    const uint32_t seq = a.tiles == c.n_seq ? tile : seq_of_tile(c, tile, NW * 32);
+    const Seq s = load_seq(c, seq);
+    const uint32_t row0 = (tile - (a.tiles == c.n_seq ? tile : first_tile(c, seq, NW * 32))) * (NW * 32);
+    const uint32_t rows = (uint32_t)s.n_q * c.group;
+    if (row0 >= rows) return;
+    const uint32_t rows_here = min(rows - row0, (uint32_t)(NW * 32));
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int col = lane & 31, half = lane >> 5;
+    const uint32_t wave_row = wave * 32;
+    const bool wave_live = wave_row < rows_here;
+    const uint32_t row = row0 + min(wave_row + col, rows_here - 1);   // rows past the end repeat the last one
+    const bool live = wave_row + col < rows_here;
+    const int32_t token = (int32_t)(row / c.group);
+    const uint32_t head = kv_head * c.group + row % c.group;
+    const int32_t limit = min(s.kv - s.n_q + token, s.kv - 1);        // last key that this row sees
+    const int32_t floor_key = a.window ? (int32_t)max((int64_t)limit + 1 - (int64_t)a.window, (int64_t)0) : 0;
+
+    const Split keys = keys_of(a, s, (int32_t)(row0 / c.group), (int32_t)((row0 + rows_here - 1) / c.group), split);
+    // the wave's own range of limits
+    const int32_t wave_first = s.kv - s.n_q + (int32_t)((row0 + min(wave_row, rows_here - 1)) / c.group);
+    const int32_t wave_last = s.kv - s.n_q + (int32_t)((row0 + min(wave_row + 31, rows_here - 1)) / c.group);
+    const int64_t wave_low = a.window ? (int64_t)wave_first + 1 - (int64_t)a.window : 0;      // first key seen by any row
+    const int64_t wave_full = a.window ? (int64_t)wave_last + 1 - (int64_t)a.window : 0;      // and by every row
+
+    w4 q[DP / 16];
+    {
+        const uint16_t *p = a.q + (uint64_t)(s.q_begin + token) * a.q_stride + (uint64_t)head * c.head_dim;
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) {
+            const uint32_t at = 16 * i + 8 * half;
+            q[i] = at < c.head_dim ? load16g(p + at) : w4{0, 0, 0, 0};
+        }
+    }
+
+    v16f o[DP / 32];
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i) o[i] = v16f{};
+    float m = kLowest, l = 0.0f;
+
+    // loading: thread -> row load_row + i * PASS of a tile, piece load_piece
+    const int load_piece = tid % CH, load_row = tid / CH;
+    const bool piece_live = (uint32_t)load_piece * 8 < c.head_dim;
+    const uint32_t piece_at = piece_live ? load_piece * 8 : 0;
+    const int32_t *table = c.table + (uint64_t)seq * c.table_stride;
+    const int32_t tiles_n = keys.end > keys.begin ? (keys.end - keys.begin + TK - 1) / TK : 0;
+    w4 rk[N], rv[N];
+    uint64_t seen_next = 0, seen;                   // which keys of a tile are there
+
+    auto slot_at = [&](int32_t t) {                 // table entry of this lane's key of tile t
+        const int32_t key = keys.begin + t * TK + lane;
+        return key < keys.end ? load4g(table + block_of(c, key)) : -1;
+    };
+    auto load_tile = [&](int32_t t, int32_t slot) {
+        const int32_t key = keys.begin + t * TK + lane;
+        const uint32_t r = row_of(c, slot, kv_head, key);
+        const uint64_t ok = __ballot(r != kNoRow);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            uint32_t from = __shfl(r, load_row + i * PASS);
+            from = from == kNoRow ? 0 : from;       // loads are not predicated: a row that is there
+            const uint64_t at = (uint64_t)from * c.head_dim + piece_at;
+            rk[i] = load16g(a.k + at);
+            rv[i] = load16g(a.v + at);
+        }
+        return ok;
+    };
+    auto store_tile = [&](int buf, uint64_t ok) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int r = load_row + i * PASS;
+            // what is not there must be finite in V: its weight is 0
+            const bool there = piece_live && (ok >> r & 1);
+            const w4 zero = {0, 0, 0, 0};
+            const int kp = load_piece ^ (DP >= 128 ? r & 15 : (r >> 1) & 7);
+            const int vp = load_piece ^ (DP >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2);
+            *(w4 *)&lds_k[buf][r * DP + kp * 8] = piece_live ? rk[i] : zero;
+            *(w4 *)&lds_v[buf][r * DP + vp * 8] = there ? rv[i] : zero;
+        }
+    };
+
+    if (tiles_n) {
+        seen_next = load_tile(0, slot_at(0));
+        store_tile(0, seen_next);
+    }
+    int32_t slot_next = tiles_n > 1 ? slot_at(1) : -1;
+
+    for (int32_t t = 0; t < tiles_n; ++t) {
+        seen = seen_next;
+        const int buf = t & 1;
+        if (t + 1 < tiles_n) {
+            seen_next = load_tile(t + 1, slot_next);
+            if (t + 2 < tiles_n) slot_next = slot_at(t + 2);
+        }
+        __syncthreads();                            // tile t is in LDS; everyone has left tile t - 1
+        const int32_t k0 = keys.begin + t * TK;
+        if (wave_live && k0 <= wave_last && (int64_t)k0 + TK > wave_low) {
+            const uint16_t *ks = lds_k[buf], *vs = lds_v[buf];
+            v16f z[2];
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                z[kb] = v16f{};
+                const int r = kb * 32 + col;
+#pragma unroll
+                for (int i = 0; i < DP / 16; ++i) {
+                    const int piece = (2 * i + half) ^ (DP >= 128 ? r & 15 : (r >> 1) & 7);
+                    z[kb] = T::mma32(*(const w4 *)&ks[r * DP + piece * 8], q[i], z[kb]);
+                }
+            }
+            if (!(k0 + TK - 1 <= wave_first && (int64_t)k0 >= wave_full && seen == ~0ull)) {
+                const uint64_t mine = seen >> (4 * half);
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int at = kb * 32 + 8 * (r / 4) + r % 4;
+                        const int32_t key = k0 + at + 4 * half;
+                        const bool sees = key <= limit && key >= floor_key && (mine >> at & 1);
+                        z[kb][r] = sees ? z[kb][r] : -INFINITY;
+                    }
+            }
+            float top = z[0][0];
+#pragma unroll
+            for (int r = 1; r < 16; ++r) top = fmaxf(top, z[0][r]);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, z[1][r]);
+            top = fmaxf(top, other_half(top)) * a.scale_log2;
+            // The maximum moves only when it is passed by 2^8: weights up to 2^8 lose nothing in 32 bits, nor when
+            // rounded to 16 (their sum and the output keep the same factor), and rescaling becomes rare.
+            if (__any(top > m + 8.0f)) {
+                const float to = fmaxf(m, top);
+                const float f = exp2_fast(m - to);
+                m = to;
+                l *= f;
+#pragma unroll
+                for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[i][r] *= f;
+            }
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    z[kb][r] = exp2_fast(__builtin_fmaf(z[kb][r], a.scale_log2, -m));
+                    l += z[kb][r];
+                }
+            // The weights are rounded to the type of the values, as the matrix cores take them; their sum is not.
+            const int ti = lane & 15;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int cc = 0; cc < 2; ++cc) {
+                    w4 p;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) p[j] = T::pack(z[kb][8 * cc + 2 * j], z[kb][8 * cc + 2 * j + 1]);
+                    const int r = kb * 32 + cc * 16 + 4 * half + ti / 4;
+#pragma unroll
+                    for (int db = 0; db < DP / 32; ++db) {
+                        const int piece = db * 4 + 2 * (lane >> 4 & 1) + (ti % 4) / 2;
+                        const int at = (piece ^ (DP >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2)) * 8 + (ti & 1) * 4;
+                        const w2 x = read_down(&vs[r * DP + at]), y = read_down(&vs[(r + 8) * DP + at]);
+                        o[db] = T::mma32(w4{x[0], x[1], y[0], y[1]}, p, o[db]);
+                    }
+                }
+        }
+        if (t + 1 < tiles_n) store_tile(buf ^ 1, seen_next);
+    }
+
+    if (!wave_live) return;
+    l += other_half(l);
+    const uint64_t out_row = (uint64_t)(s.q_begin + token);
+    if (a.splits == 1) {
+        const RowEnd e = finish_row(m, l, a.sinks, head);
+        if (!live) return;
+        uint16_t *p = a.out + out_row * a.out_stride + (uint64_t)head * c.head_dim;
+#pragma unroll
+        for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t at = db * 32 + 8 * j + 4 * half;
+                if (at < c.head_dim) {
+                    const w2 w = {T::pack(o[db][4 * j] * e.scale_o, o[db][4 * j + 1] * e.scale_o),
+                                  T::pack(o[db][4 * j + 2] * e.scale_o, o[db][4 * j + 3] * e.scale_o)};
+                    *(w2 *)(p + at) = w;
+                }
+            }
+        if (a.lse && half == 0) a.lse[(uint64_t)head * c.total_q + out_row] = e.lse;
+    } else if (live) {
+        const uint64_t part = (uint64_t)split * c.total_q * c.heads + out_row * c.heads + head;
+        if (half == 0) *(v2f *)(a.part_ml + 2 * part) = v2f{m, l};
+        float *p = a.part_o + part * c.head_dim;
+#pragma unroll
+        for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t at = db * 32 + 8 * j + 4 * half;
+                if (at < c.head_dim)
+                    *(v4f *)(p + at) = v4f{o[db][4 * j], o[db][4 * j + 1], o[db][4 * j + 2], o[db][4 * j + 3]};
+            }
+    }
+}
+
+// ---- up to 16 rows, the waves split the keys
+
+constexpr int kFewWaves = 4;
+constexpr int kFewKeys = 32;    // to a wave at a time
+
+template <class T, int DP>
+__global__ __launch_bounds__(kFewWaves * 64, 2) void attention_few(const AttentionArgs a)
+{
+    constexpr int NW = kFewWaves, TK = kFewKeys;
+    constexpr int CH = DP / 8;
+    constexpr int PASS = 64 / CH;                    // rows that a wave loads at once
+    constexpr int N = TK / PASS;
+    constexpr int KS = DP / 32;
+    // each wave's values, and at the end its part of the output: [wave][16 rows][DP] in 32 bits
+    __shared__ __align__(16) uint16_t lds_v[NW][TK * DP];
+    __shared__ float lds_ml[NW][2][16];
+    static_assert(sizeof(lds_v) == NW * 16 * DP * sizeof(float), "the parts reuse the values' space");
+
+    const CacheView &c = a.c;
+    const uint32_t kv_head = blockIdx.x % c.kv_heads;
+    const uint32_t rest = blockIdx.x / c.kv_heads;
+    const uint32_t split = rest % a.splits;
+    const uint32_t seq = rest / a.splits;
+    const Seq s = load_seq(c, seq);
+    const uint32_t rows = (uint32_t)s.n_q * c.group;   // at most 16
+    if (!rows) return;
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int col = lane & 15, quad = lane >> 4;
+    const uint32_t row = min((uint32_t)col, rows - 1);
+    const int32_t token = (int32_t)(row / c.group);
+    const uint32_t head = kv_head * c.group + row % c.group;
+    const int32_t limit = min(s.kv - s.n_q + token, s.kv - 1);
+    const int32_t floor_key = a.window ? (int32_t)max((int64_t)limit + 1 - (int64_t)a.window, (int64_t)0) : 0;
+    const Split keys = keys_of(a, s, 0, s.n_q - 1, split);
+    const int32_t all_first = s.kv - s.n_q;          // last key that every row sees
+    const int64_t all_full = a.window ? (int64_t)s.kv - (int64_t)a.window : 0;   // first key that every row sees
+
+    w4 q[KS];
+    {
+        const uint16_t *p = a.q + (uint64_t)(s.q_begin + token) * a.q_stride + (uint64_t)head * c.head_dim;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            const uint32_t at = 32 * i + 8 * quad;
+            q[i] = at < c.head_dim ? load16g(p + at) : w4{0, 0, 0, 0};
+        }
+    }
+    v4f o[DP / 16];
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) o[i] = v4f{};
+    float m = kLowest, l = 0.0f;
+
+    const int load_piece = lane % CH, load_row = lane / CH;
+    const bool piece_live = (uint32_t)load_piece * 8 < c.head_dim;
+    const uint32_t piece_at = piece_live ? load_piece * 8 : 0;
+    const int32_t *table = c.table + (uint64_t)seq * c.table_stride;
+    const int32_t mine = keys.begin + wave * TK;     // this wave's first keys; then every NW * TK
+    const int32_t steps = keys.end > mine ? (keys.end - mine + NW * TK - 1) / (NW * TK) : 0;
+
+    w4 rk[2][KS], rv[N];
+    uint32_t seen_next = 0;
+    auto slot_at = [&](int32_t t) {
+        const int32_t key = mine + t * (NW * TK) + (lane & 31);
+        return key < keys.end ? load4g(table + block_of(c, key)) : -1;
+    };
+    auto load_tile = [&](int32_t t, int32_t slot) {
+        const int32_t key = mine + t * (NW * TK) + (lane & 31);
+        const uint32_t r = row_of(c, slot, kv_head, key);
+        const uint32_t ok = (uint32_t)__ballot(r != kNoRow);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            uint32_t from = __shfl(r, b * 16 + col);
+            from = from == kNoRow ? 0 : from;
+            const uint16_t *p = a.k + (uint64_t)from * c.head_dim;
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                const uint32_t at = 32 * i + 8 * quad;
+                rk[b][i] = load16g(p + (at < c.head_dim ? at : 0));   // past the end: q is 0 there
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            uint32_t from = __shfl(r, load_row + i * PASS);
+            from = from == kNoRow ? 0 : from;
+            rv[i] = load16g(a.v + (uint64_t)from * c.head_dim + piece_at);
+        }
+        return ok;
+    };
+
+    if (steps) seen_next = load_tile(0, slot_at(0));
+    int32_t slot_next = steps > 1 ? slot_at(1) : -1;
+    uint16_t *vs = lds_v[wave];
+
+    for (int32_t t = 0; t < steps; ++t) {
+        const uint32_t seen = seen_next;
+        const int32_t k0 = mine + t * (NW * TK);
+        v4f z[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            z[b] = v4f{};
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                w4 k = rk[b][i];
+                if (c.head_dim != DP && 32u * i + 8 * quad >= c.head_dim) k = w4{0, 0, 0, 0};
+                z[b] = T::mma16(k, q[i], z[b]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int r = load_row + i * PASS;
+            const bool there = piece_live && (seen >> r & 1);
+            const int vp = load_piece ^ (DP >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2);
+            *(w4 *)&vs[r * DP + vp * 8] = there ? rv[i] : w4{0, 0, 0, 0};
+        }
+        if (t + 1 < steps) {
+            seen_next = load_tile(t + 1, slot_next);
+            if (t + 2 < steps) slot_next = slot_at(t + 2);
+        }
+        if (!(k0 + TK - 1 <= all_first && (int64_t)k0 >= all_full && seen == ~0u)) {
+            const uint32_t here = seen >> (4 * quad);
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int32_t key = k0 + b * 16 + 4 * quad + r;
+                    const bool sees = key <= limit && key >= floor_key && (here >> (b * 16 + r) & 1);
+                    z[b][r] = sees ? z[b][r] : -INFINITY;
+                }
+        }
+        float top = z[0][0];
+#pragma unroll
+        for (int r = 1; r < 4; ++r) top = fmaxf(top, z[0][r]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) top = fmaxf(top, z[1][r]);
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, other_half(top)) * a.scale_log2;
+        if (__any(top > m + 8.0f)) {
+            const float to = fmaxf(m, top);
+            const float f = exp2_fast(m - to);
+            m = to;
+            l *= f;
+#pragma unroll
+            for (int i = 0; i < DP / 16; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[i][r] *= f;
+        }
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                z[b][r] = exp2_fast(__builtin_fmaf(z[b][r], a.scale_log2, -m));
+                l += z[b][r];
+            }
+        const w4 p = {T::pack(z[0][0], z[0][1]), T::pack(z[0][2], z[0][3]), T::pack(z[1][0], z[1][1]),
+                      T::pack(z[1][2], z[1][3])};
+        // the wave's own values: LDS keeps a wave's accesses in order
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        const int r = 4 * quad + col / 4;
+#pragma unroll
+        for (int db = 0; db < DP / 16; ++db) {
+            const int piece = db * 2 + (col % 4) / 2;
+            const int at = (piece ^ (DP >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2)) * 8 + (col & 1) * 4;
+            const w2 x = read_down(&vs[r * DP + at]), y = read_down(&vs[(r + 16) * DP + at]);
+            o[db] = T::mma16(w4{x[0], x[1], y[0], y[1]}, p, o[db]);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+
+    // join the waves: scale each part to the common maximum, then add
+    l += __shfl_xor(l, 16);
+    l += other_half(l);
+    if (quad == 0) {
+        lds_ml[wave][0][col] = m;
+        lds_ml[wave][1][col] = l;
+    }
+    __syncthreads();
+    float top = lds_ml[0][0][col];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) top = fmaxf(top, lds_ml[w][0][col]);
+    const float f = exp2_fast(m - top);
+    float *parts = (float *)&lds_v[0][0];
+#pragma unroll
+    for (int db = 0; db < DP / 16; ++db)
+        *(v4f *)&parts[(wave * 16 + col) * DP + db * 16 + 4 * quad] =
+            v4f{o[db][0] * f, o[db][1] * f, o[db][2] * f, o[db][3] * f};
+    __syncthreads();
+    for (uint32_t i = tid; i < rows * (DP / 4); i += NW * 64) {
+        const uint32_t r = i / (DP / 4), at = i % (DP / 4) * 4;
+        if (at >= c.head_dim) continue;
+        v4f sum = *(v4f *)&parts[r * DP + at];
+        float mm = lds_ml[0][0][r], ll = 0.0f;
+#pragma unroll
+        for (int w = 1; w < NW; ++w) {
+            sum += *(v4f *)&parts[(w * 16 + r) * DP + at];
+            mm = fmaxf(mm, lds_ml[w][0][r]);
+        }
+#pragma unroll
+        for (int w = 0; w < NW; ++w) ll += lds_ml[w][1][r] * exp2_fast(lds_ml[w][0][r] - mm);
+        const uint64_t out_row = (uint64_t)(s.q_begin + (int32_t)(r / c.group));
+        const uint32_t h = kv_head * c.group + r % c.group;
+        if (a.splits == 1) {
+            const RowEnd e = finish_row(mm, ll, a.sinks, h);
+            uint16_t *p = a.out + out_row * a.out_stride + (uint64_t)h * c.head_dim + at;
+            *(w2 *)p = w2{T::pack(sum[0] * e.scale_o, sum[1] * e.scale_o), T::pack(sum[2] * e.scale_o, sum[3] * e.scale_o)};
+            if (a.lse && at == 0) a.lse[(uint64_t)h * c.total_q + out_row] = e.lse;
+        } else {
+            const uint64_t part = (uint64_t)split * c.total_q * c.heads + out_row * c.heads + h;
+            *(v4f *)(a.part_o + part * c.head_dim + at) = sum;
+            if (at == 0) *(v2f *)(a.part_ml + 2 * part) = v2f{mm, ll};
+        }
+    }
+}
+
+// Adds the parts of a row: a wave to a row, lanes over the parts for the sums, then over head_dim.
+template <class T>
+__global__ __launch_bounds__(256) void attention_join(const AttentionArgs a)
+{
+    const CacheView &c = a.c;
+    const uint32_t rows = c.total_q * c.heads;
+    const uint32_t row = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= rows) return;
+    const int lane = threadIdx.x & 63;
+    const uint32_t head = row % c.heads;
+    float m = kLowest;
+    for (uint32_t i = lane; i < a.splits; i += 64) {
+        const v2f ml = *(const v2f *)(a.part_ml + 2 * ((uint64_t)i * rows + row));
+        m = fmaxf(m, ml[0]);
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    float l = 0.0f;
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};       // head_dim lane, lane + 64, ..
+    for (uint32_t i0 = 0; i0 < a.splits; i0 += 64) {
+        float w = 0.0f, part_l = 0.0f;
+        if (i0 + lane < a.splits) {
+            const v2f ml = *(const v2f *)(a.part_ml + 2 * ((uint64_t)(i0 + lane) * rows + row));
+            w = exp2_fast(ml[0] - m);
+            part_l = ml[1];
+        }
+        l += part_l * w;
+        const uint32_t n = min(64u, a.splits - i0);
+        for (uint32_t i = 0; i < n; ++i) {
+            const float wi = __shfl(w, i), li = __shfl(part_l, i);
+            if (li == 0.0f) continue;               // an empty part wrote no output
+            const float *p = a.part_o + ((uint64_t)(i0 + i) * rows + row) * c.head_dim;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (lane + 64u * j < c.head_dim) sum[j] += p[lane + 64 * j] * wi;
+        }
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d);
+    const RowEnd e = finish_row(m, l, a.sinks, head);
+    const uint32_t token = row / c.heads;
+    uint16_t *p = a.out + (uint64_t)token * a.out_stride + (uint64_t)head * c.head_dim;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (lane + 64u * j < c.head_dim) p[lane + 64 * j] = (uint16_t)T::pack(sum[j] * e.scale_o, 0.0f);
+    if (a.lse && lane == 0) a.lse[(uint64_t)head * c.total_q + token] = e.lse;
+}
+
+// ---- attention weight of the cached tokens
+
+constexpr int kMassWaves = 4;
+
+// A wave holds 32 keys as the A operand and goes over the rows, 32 at a time: S^T again, so every lane adds up
+// the weights of its own 16 keys for one row of each 32, in a fixed order, and the lanes are added at the end.
+template <class T, int DP>
+__global__ __launch_bounds__(kMassWaves * 64, DP > 128 ? 1 : 2) void attention_mass(const MassArgs a)
+{
+    const CacheView &c = a.c;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int col = lane & 31, half = lane >> 5;
+    const uint32_t kv_head = blockIdx.x % c.kv_heads;
+    const uint32_t tile = blockIdx.x / c.kv_heads;
+    const uint32_t tiles = (c.max_kv + kMassWaves * 32 - 1) / (kMassWaves * 32);
+    const uint32_t seq = tile / tiles;
+    const Seq s = load_seq(c, seq);
+    const int32_t k0 = (int32_t)(tile % tiles * (kMassWaves * 32)) + wave * 32;
+    if (k0 >= s.kv) return;
+
+    w4 k[DP / 16];
+    bool there;
+    {
+        const int32_t key = min(k0 + col, s.kv - 1);
+        const uint32_t r = row_of(c, load4g(c.table + (uint64_t)seq * c.table_stride + block_of(c, key)), kv_head, key);
+        there = r != kNoRow;
+        const uint16_t *p = a.k + (uint64_t)(there ? r : 0) * c.head_dim;
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) {
+            const uint32_t at = 16 * i + 8 * half;
+            k[i] = at < c.head_dim ? load16g(p + at) : w4{0, 0, 0, 0};
+        }
+    }
+    const uint32_t seen = (uint32_t)__ballot(there) >> (4 * half);   // bit of key 8*(r/4) + r%4
+
+    const int32_t shift = s.kv - s.n_q;
+    int32_t first = a.last ? max(0, s.n_q - (int32_t)min(a.last, 0x7FFFFFFFu)) : 0;
+    first = max(first, k0 - shift);                  // earlier tokens see none of these keys
+    int32_t last = s.n_q - 1;
+    if (a.window) last = (int32_t)min((int64_t)last, (int64_t)k0 + 31 + a.window - 1 - shift);
+    float acc[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
+
+    const int64_t row_begin = (int64_t)first * c.group, row_end = ((int64_t)last + 1) * c.group;
+    for (int64_t r0 = row_begin; r0 < row_end; r0 += 32) {
+        const uint32_t row = (uint32_t)min(r0 + col, row_end - 1);
+        const int32_t token = (int32_t)(row / c.group);
+        const uint32_t head = kv_head * c.group + row % c.group;
+        const uint16_t *p = a.q + (uint64_t)(s.q_begin + token) * a.q_stride + (uint64_t)head * c.head_dim;
+        const float lse = a.lse[(uint64_t)head * c.total_q + s.q_begin + token] * kLog2e;
+        v16f z{};
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) {
+            const uint32_t at = 16 * i + 8 * half;
+            const w4 q = at < c.head_dim ? load16g(p + at) : w4{0, 0, 0, 0};
+            z = T::mma32(k[i], q, z);
+        }
+        const bool live = r0 + col < row_end && lse > -INFINITY;   // a row without keys gives nothing
+        const int32_t limit = shift + token;
+        const int32_t floor_key = a.window ? (int32_t)max((int64_t)limit + 1 - (int64_t)a.window, (int64_t)0) : 0;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int at = 8 * (r / 4) + r % 4;
+            const int32_t key = k0 + at + 4 * half;
+            const bool sees = live && key <= limit && key >= floor_key && (seen >> at & 1);
+            acc[r] += sees ? exp2_fast(__builtin_fmaf(z[r], a.scale_log2, -lse)) : 0.0f;
+        }
+    }
+    // over the 32 lanes of each half
+#pragma unroll
+    for (int d = 16; d; d >>= 1)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[r] += __shfl_xor(acc[r], d);
+    float sum = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sum = col == r ? acc[r] : sum;      // lane r of a half writes key r's
+    const int32_t key = k0 + 8 * (col / 4) + 4 * half + col % 4;
+    if (col < 16 && key < s.kv) {
+        const uint64_t at = ((uint64_t)seq * c.kv_heads + kv_head) * a.score_stride + key;
+        a.score_out[at] = (a.score_in ? a.score_in[at] : 0.0f) + sum;
+    }
+}
+
+template <template <class, int> class Launch, class Args>
+hipError_t by_type(uint32_t dtype, uint32_t head_dim, const Args &a, hipStream_t stream)
+{
+    if (dtype == KVP_BF16) {
+        if (head_dim <= 64) return Launch<BF16, 64>::go(a, stream);
+        if (head_dim <= 128) return Launch<BF16, 128>::go(a, stream);
+        return Launch<BF16, 256>::go(a, stream);
+    }
+    if (head_dim <= 64) return Launch<F16, 64>::go(a, stream);
+    if (head_dim <= 128) return Launch<F16, 128>::go(a, stream);
+    return Launch<F16, 256>::go(a, stream);
+}
+
+template <class T, int DP>
+struct Rows {
+    static hipError_t go(const AttentionArgs &a, hipStream_t stream)
+    {
+        attention_rows<T, DP, kTileRows / 32><<<a.tiles * a.splits * a.c.kv_heads, kTileRows * 2, 0, stream>>>(a);
+        return hipGetLastError();
+    }
+};
+template <class T, int DP>
+struct Few {
+    static hipError_t go(const AttentionArgs &a, hipStream_t stream)
+    {
+        attention_few<T, DP><<<a.tiles * a.splits * a.c.kv_heads, kFewWaves * 64, 0, stream>>>(a);
+        return hipGetLastError();
+    }
+};
+template <class T, int DP>
+struct Mass {
+    static hipError_t go(const MassArgs &a, hipStream_t stream)
+    {
+        const uint32_t tiles = (a.c.max_kv + kMassWaves * 32 - 1) / (kMassWaves * 32);
+        attention_mass<T, DP><<<tiles * a.c.n_seq * a.c.kv_heads, kMassWaves * 64, 0, stream>>>(a);
+        return hipGetLastError();
+    }
+};
+
+}  // namespace
+
+hipError_t launch_attention(const AttentionArgs &a, uint32_t dtype, bool few_rows, hipStream_t stream)
+{
+    return few_rows ? by_type<Few>(dtype, a.c.head_dim, a, stream) : by_type<Rows>(dtype, a.c.head_dim, a, stream);
+}
+
+hipError_t launch_attention_join(const AttentionArgs &a, uint32_t dtype, hipStream_t stream)
+{
+    const uint32_t groups = (a.c.total_q * a.c.heads + 3) / 4;
+    if (dtype == KVP_BF16)
+        attention_join<BF16><<<groups, 256, 0, stream>>>(a);
+    else
+        attention_join<F16><<<groups, 256, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_mass(const MassArgs &a, uint32_t dtype, hipStream_t stream)
+{
+    return by_type<Mass>(dtype, a.c.head_dim, a, stream);
+}
+
+}  // namespace kvp

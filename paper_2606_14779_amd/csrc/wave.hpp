@@ -1,0 +1,144 @@
+// Device helpers of the matrix kernels: element types, MFMA operands, transposed
+// LDS reads and the two-halves exchanges of a 64-lane wavefront (gfx950).
+//
+// Operand layouts, lane l:
+//   32x32x16  A: row l%32, k = 8*(l/32)..+7   B: column l%32, same k
+//             C: column l%32, register r holds row 8*(r/4) + 4*(l/32) + r%4
+//   16x16x32  A: row l%16, k = 8*(l/16)..+7   B: column l%16, same k
+//             C: column l%16, register r holds row 4*(l/16) + r
+#ifndef KVP_WAVE_HPP
+#define KVP_WAVE_HPP
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "cache_ops.hpp"
+
+namespace kvp {
+
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef short v8s __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef uint32_t w4 __attribute__((ext_vector_type(4)));
+typedef uint32_t w2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(1))) const w4 gw4;
+typedef __attribute__((address_space(1))) const int32_t gi32;
+
+struct BF16 {
+    typedef __bf16 x8 __attribute__((ext_vector_type(8)));
+    typedef __bf16 x2 __attribute__((ext_vector_type(2)));
+    static __device__ __forceinline__ v16f mma32(w4 a, w4 b, v16f c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ v4f mma16(w4 a, w4 b, v4f c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t pack(float a, float b)   // to nearest even
+    {
+        const v2f f = {a, b};
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, x2));
+    }
+    static __device__ __forceinline__ float unpack(uint32_t w, int i)
+    {
+        return __builtin_bit_cast(float, i ? (w & 0xFFFF0000u) : (w << 16));
+    }
+};
+
+struct F16 {
+    typedef _Float16 x8 __attribute__((ext_vector_type(8)));
+    typedef _Float16 x2 __attribute__((ext_vector_type(2)));
+    static __device__ __forceinline__ v16f mma32(w4 a, w4 b, v16f c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ v4f mma16(w4 a, w4 b, v4f c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t pack(float a, float b)   // to nearest even
+    {
+        const v2f f = {a, b};
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, x2));
+    }
+    static __device__ __forceinline__ float unpack(uint32_t w, int i)
+    {
+        return (float)__builtin_bit_cast(x2, w)[i];
+    }
+};
+
+__device__ __forceinline__ w4 load16g(const uint16_t *p) { return *(gw4 *)p; }
+__device__ __forceinline__ int32_t load4g(const int32_t *p) { return *(gi32 *)p; }
+
+// Four 16-bit elements down a column: within 16 lanes, lane i names 4 elements of row i/4
+// (columns 4*(i%4)..+3 of a 4x16 tile) and receives column i of the tile's four rows.
+__device__ __forceinline__ w2 read_down(const uint16_t *lds)
+{
+    return __builtin_bit_cast(w2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)lds));
+}
+
+// The other 32 lanes' value.
+__device__ __forceinline__ float other_half(float x)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto p = __builtin_amdgcn_permlane32_swap(u, u, false, false);   // p[0]: low halves twice, p[1]: high halves twice
+    return __builtin_bit_cast(float, (uint32_t)(threadIdx.x & 32 ? p[0] : p[1]));
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+constexpr float kLowest = -3.0e38f;        // start of a running maximum: finite, so that -inf minus it is -inf
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// A sequence of a batch.  Device arrays are not trusted: lengths are clamped to what the host was told.
+struct Seq {
+    int32_t q_begin, n_q, kv;
+};
+__device__ __forceinline__ Seq load_seq(const CacheView &c, uint32_t s)
+{
+    const int32_t total = (int32_t)c.total_q;
+    const int32_t b = min(max(load4g(c.cu_q + s), 0), total);
+    const int32_t e = min(max(load4g(c.cu_q + s + 1), b), total);
+    const int32_t kv = min(max(load4g(c.kv_len + s), 0), (int32_t)c.max_kv);
+    return {b, min(e - b, (int32_t)c.max_q), kv};
+}
+
+// Row number (of head_dim elements) of a sequence's cached token, or kNoRow where its slot is none of the cache's.
+__device__ __forceinline__ uint32_t block_of(const CacheView &c, uint32_t token)
+{
+    return c.block_shift != kNoShift ? token >> c.block_shift : token / c.block;
+}
+__device__ __forceinline__ uint32_t row_of(const CacheView &c, int32_t slot, uint32_t kv_head, uint32_t token)
+{
+    const uint32_t off = c.block_shift != kNoShift ? token & (c.block - 1) : token % c.block;
+    return (uint32_t)slot < c.num_slots ? ((uint32_t)slot * c.kv_heads + kv_head) * c.block + off : kNoRow;
+}
+
+// Sequence of a row tile: sequence s owns the tiles from floor(rows before it / tile) + s on, at least as many
+// as its rows need, so no prefix of tile counts has to be made.
+__device__ __forceinline__ uint32_t first_tile(const CacheView &c, uint32_t s, uint32_t tile_rows)
+{
+    const uint32_t before = (uint32_t)min(max(load4g(c.cu_q + s), 0), (int32_t)c.total_q);
+    return (uint32_t)((uint64_t)before * c.group / tile_rows) + s;
+}
+__device__ __forceinline__ uint32_t seq_of_tile(const CacheView &c, uint32_t tile, uint32_t tile_rows)
+{
+    uint32_t lo = 0, hi = c.n_seq;              // first_tile(lo) <= tile < first_tile(hi)
+    while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (first_tile(c, mid, tile_rows) <= tile)
+            lo = mid;
+        else
+            hi = mid;
+    }
+    return lo;
+}
+
+}  // namespace kvp
+
+#endif

@@ -37,6 +37,10 @@ MEASURE_SHARED_LINK = 1
 MEASURE_SHARED_HBM = 4       # staging regions share the one GPU's HBM: their rate divided by their count
 MEASURE_FILES_TOGETHER = 2   # file regions read all at once, as a retrieve reads them
 
+DTYPES = {"bf16": 0, "f16": 1}
+ROPE_KINDS = {"plain": 0, "linear": 1, "by_parts": 2, "by_parts_index": 3}
+ROPE_INTERLEAVED = 1
+
 LOC_DTYPE = np.dtype([("region", "<u4"), ("gen", "<u4"), ("offset", "<u8")])
 
 
@@ -72,6 +76,25 @@ class _TimingSummary(ctypes.Structure):
                 ("staging_ms_max", ctypes.c_float)]
 
 
+class _CacheShape(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_uint32), ("num_q_heads", ctypes.c_uint32), ("num_kv_heads", ctypes.c_uint32),
+                ("head_dim", ctypes.c_uint32), ("block_size", ctypes.c_uint32), ("num_slots", ctypes.c_uint32),
+                ("reserved", ctypes.c_uint32)]
+
+
+class _Batch(ctypes.Structure):
+    _fields_ = [("n_seq", ctypes.c_uint32), ("total_q", ctypes.c_uint32), ("max_q", ctypes.c_uint32),
+                ("max_kv", ctypes.c_uint32), ("table_stride", ctypes.c_uint32), ("reserved", ctypes.c_uint32),
+                ("cu_q", ctypes.c_uint64), ("kv_len", ctypes.c_uint64), ("block_table", ctypes.c_uint64)]
+
+
+class _RopeScaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_uint32), ("reserved", ctypes.c_uint32), ("base", ctypes.c_double),
+                ("factor", ctypes.c_double), ("original_length", ctypes.c_double), ("alpha", ctypes.c_double),
+                ("beta", ctypes.c_double), ("magnitude", ctypes.c_double)]
+
+
+assert ctypes.sizeof(_CacheShape) == 28 and ctypes.sizeof(_Batch) == 48 and ctypes.sizeof(_RopeScaling) == 56
 assert ctypes.sizeof(_RegionDesc) == 24 and ctypes.sizeof(_KVSpec) == 24
 assert LOC_DTYPE.itemsize == 16
 
@@ -109,6 +132,7 @@ def _close_live_pools():
 atexit.register(_close_live_pools)
 
 _u32, _u64, _i32, _vp = ctypes.c_uint32, ctypes.c_uint64, ctypes.c_int, ctypes.c_void_p
+_f32 = ctypes.c_float
 _SIGS = {
     "kv_pool_create": (_i32, [_vp, _vp, _u32, _vp, _i32, _vp]),
     "kv_pool_create_files": (_i32, [_vp, _vp, _u32, _vp, _i32, _vp, _vp]),
@@ -137,6 +161,14 @@ _SIGS = {
     "kv_pool_timing_summary": (_i32, [_vp, _vp]),
     "kv_probe_copy_kernel": (_i32, [_vp, _vp, _u64, _u32, _u32, _vp]),
     "kv_probe_memcpy": (_i32, [_vp, _vp, _u64, _vp]),
+    "kv_rope_table": (_i32, [_vp, _u32, _u32, _vp, _vp]),
+    "kv_rope_append": (_i32, [_vp, _vp, _vp, _u32, _u32, _u32, _vp, _vp, _u64, _vp, _u64, _vp, _u64, _vp, _u64, _vp,
+                              _vp, _vp, _u32, _vp]),
+    "kv_attention": (_i32, [_vp, _vp, _vp, _u64, _vp, _vp, _f32, _u32, _vp, _vp, _u64, _vp, _vp, _u64, _vp]),
+    "kv_attention_workspace": (_i32, [_vp, _vp, _vp]),
+    "kv_attention_mass": (_i32, [_vp, _vp, _vp, _u64, _vp, _f32, _u32, _vp, _u32, _vp, _vp, _u32, _vp]),
+    "kv_evict": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _u32, _vp, _vp, _u32, _vp, _vp, _vp, _vp, _u64, _vp]),
+    "kv_evict_workspace": (_i32, [_vp, _vp, _vp]),
 }
 # ctypes wraps an integer outside its C type's range silently (-1 becomes
 # 2^32-1 for a uint32_t: a slot count that every table entry passes), so every
@@ -270,6 +302,85 @@ def probe_copy_kernel(dst: int, src: int, nbytes: int, grid: int = 0, flags: int
 
 def probe_memcpy(dst: int, src: int, nbytes: int, stream: int = 0):
     _check(_lib.kv_probe_memcpy(dst, src, nbytes, stream or None))
+
+
+# ---- operators on the engine's paged cache (device memory as integers: tensor.data_ptr())
+
+class CacheShape:
+    """The cache of a layer and the heads over it (kvp_cache_shape); dtype "bf16" or "f16"."""
+
+    def __init__(self, dtype: str, num_q_heads: int, num_kv_heads: int, head_dim: int, block_size: int, num_slots: int):
+        if dtype not in DTYPES:
+            raise ValueError("dtype %r is none of %s" % (dtype, ", ".join(DTYPES)))
+        self._c = _struct(_CacheShape, DTYPES[dtype], num_q_heads, num_kv_heads, head_dim, block_size, num_slots, 0)
+        self._p = ctypes.addressof(self._c)
+
+
+class Batch:
+    """A batch of sequences over the cache (kvp_batch): sizes on the host, lengths and tables in device memory
+    that the caller keeps alive."""
+
+    def __init__(self, n_seq: int, total_q: int, max_q: int, max_kv: int, cu_q: int, kv_len: int, block_table: int,
+                 table_stride: int):
+        self._c = _struct(_Batch, n_seq, total_q, max_q, max_kv, table_stride, 0, cu_q, kv_len, block_table)
+        self._p = ctypes.addressof(self._c)
+
+
+def rope_table(table: int, n_positions: int, rot_dim: int, base: float = 10000.0, kind: str = "plain",
+               factor: float = 1.0, original_length: float = 0.0, alpha: float = 0.0, beta: float = 0.0,
+               magnitude: float = 1.0, stream: int = 0):
+    """kv_rope_table: cosines and sines of every position, [n_positions][rot_dim / 2][2] of 32 bits."""
+    if kind not in ROPE_KINDS:
+        raise ValueError("kind %r is none of %s" % (kind, ", ".join(ROPE_KINDS)))
+    r = _RopeScaling(ROPE_KINDS[kind], 0, base, factor, original_length, alpha, beta, magnitude)
+    _check(_lib.kv_rope_table(table or None, n_positions, rot_dim, ctypes.addressof(r), stream or None))
+
+
+def rope_append(shape: CacheShape, batch: Batch, table: int, n_positions: int, rot_dim: int, positions: int, k: int,
+                k_stride: int, v: int, v_stride: int, k_cache: int, v_cache: int, *, q: int = 0, q_stride: int = 0,
+                q_out: int = 0, q_out_stride: int = 0, pos: int = 0, pos_stride: int = 0, interleaved: bool = False,
+                stream: int = 0):
+    """kv_rope_append: rotated queries to q_out, rotated keys, values and positions to the cache."""
+    _check(_lib.kv_rope_append(shape._p, batch._p, table, n_positions, rot_dim, ROPE_INTERLEAVED if interleaved else 0,
+                               positions, q, q_stride, q_out, q_out_stride, k, k_stride, v, v_stride, k_cache, v_cache,
+                               pos, pos_stride, stream))
+
+
+def attention_workspace(shape: CacheShape, batch: Batch) -> int:
+    """Bytes of workspace that attention needs for this shape and batch."""
+    n = ctypes.c_uint64()
+    _check(_lib.kv_attention_workspace(shape._p, batch._p, ctypes.addressof(n)))
+    return n.value
+
+
+def attention(shape: CacheShape, batch: Batch, q: int, q_stride: int, k_cache: int, v_cache: int, scale: float, out: int,
+              out_stride: int, *, window: int = 0, sinks: int = 0, lse: int = 0, workspace: int = 0,
+              workspace_bytes: int = 0, stream: int = 0):
+    """kv_attention: causal attention of the new tokens over the cached ones."""
+    _check(_lib.kv_attention(shape._p, batch._p, q, q_stride, k_cache, v_cache, scale, window, sinks, out, out_stride,
+                             lse, workspace, workspace_bytes, stream))
+
+
+def attention_mass(shape: CacheShape, batch: Batch, q: int, q_stride: int, k_cache: int, scale: float, lse: int,
+                   score_in: int, score_out: int, score_stride: int, *, window: int = 0, last: int = 0, stream: int = 0):
+    """kv_attention_mass: the attention weight that each cached token collects, added to its score."""
+    _check(_lib.kv_attention_mass(shape._p, batch._p, q, q_stride, k_cache, scale, window, lse, last, score_in, score_out,
+                                  score_stride, stream))
+
+
+def evict_workspace(shape: CacheShape, batch: Batch) -> int:
+    """Bytes of workspace that evict needs for this shape and batch."""
+    n = ctypes.c_uint64()
+    _check(_lib.kv_evict_workspace(shape._p, batch._p, ctypes.addressof(n)))
+    return n.value
+
+
+def evict(shape: CacheShape, batch: Batch, keep: int, score_in: int, score_out: int, score_stride: int, k_cache: int,
+          v_cache: int, len_out: int, workspace: int, workspace_bytes: int, *, protect: int = 0, pos_in: int = 0,
+          pos_out: int = 0, pos_stride: int = 0, stream: int = 0):
+    """kv_evict: keeps the tokens of largest score and compacts the cache in place."""
+    _check(_lib.kv_evict(shape._p, batch._p, keep, protect, score_in, score_out, score_stride, pos_in, pos_out, pos_stride,
+                         k_cache, v_cache, len_out, workspace, workspace_bytes, stream))
 
 
 class KVPool:
