@@ -40,6 +40,7 @@ def _hipcc() -> str:
 def _compile(src: str, extra: list[str]) -> str:
     obj = os.path.join(BUILD, os.path.basename(src) + ".o")
     if src.endswith(".hip"):
+        obj = os.path.join(BUILD, "part-" + os.path.basename(obj))
         cmd = [_hipcc()] + HIPCC_FLAGS + extra + ["-I", INCLUDE, "-I", CSRC, "-c", src, "-o", obj]
     else:
         cmd = ["g++"] + CXX_FLAGS + extra + ["-I", INCLUDE, "-I", CSRC, "-c", src, "-o", obj]
@@ -55,6 +56,13 @@ def build(verbose: bool = False, extra: list[str] | None = None) -> str:
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")) + glob.glob(os.path.join(CSRC, "*.cpp")))
     with cf.ThreadPoolExecutor(max_workers=min(8, len(srcs))) as ex:
         objs = list(ex.map(lambda s: _compile(s, extra or []), srcs))
+    # the device code as one object: programs that link the host sources by themselves need no other
+    parts = [o for o in objs if os.path.basename(o).startswith("part-")]
+    kernels = os.path.join(BUILD, "kernels.hip.o")
+    r = subprocess.run(["ld", "-r", "-o", kernels] + parts, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("joining the device objects failed: %s%s" % (r.stdout, r.stderr))
+    objs = [o for o in objs if o not in parts] + [kernels]
     tmp = LIB + ".tmp%d" % os.getpid()
     cmd = [_hipcc(), "--offload-arch=" + ARCH, "-shared", "-fPIC", "-o", tmp] + objs + [
         "-L" + os.path.join(ROCM, "lib"), "-lamdhip64", "-Wl,-rpath," + os.path.join(ROCM, "lib")]
@@ -77,7 +85,7 @@ def build(verbose: bool = False, extra: list[str] | None = None) -> str:
         os.replace(exe + ".tmp", exe)
         # the same client over a host-sanitized build of the library (its own file: g++ only)
         from . import build_asan
-        build_asan.build([o for o in objs if o.endswith(".hip.o")])
+        build_asan.build(kernels)
     if verbose:
         print("built", LIB)
     return LIB

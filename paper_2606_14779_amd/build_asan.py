@@ -3,7 +3,7 @@ and of the plain C++ ABI client, for a GPU test of the library's host code.
 
 Only host C++ is instrumented, with g++ (GPU code cannot run under a sanitizer
 here): the library's .cpp sources are compiled with the sanitizers and linked
-with the already built, uninstrumented kernel objects.  The results sit under
+with the already built, uninstrumented kernels object.  The results sit under
 tests/abi_client/ and are used by tests/test_abi_client.py only.
 """
 from __future__ import annotations
@@ -26,7 +26,7 @@ def _run(cmd):
         raise RuntimeError("sanitizer build failed: %s\n%s%s" % (" ".join(cmd), r.stdout, r.stderr))
 
 
-def build(kernel_objs: list[str]) -> str:
+def build(kernels_obj: str) -> str:
     """Instrumented libkvpool.so and abi_client_asan; returns the client's path."""
     import concurrent.futures as cf
     os.makedirs(OUT, exist_ok=True)
@@ -39,7 +39,7 @@ def build(kernel_objs: list[str]) -> str:
     with cf.ThreadPoolExecutor(max_workers=min(8, len(names))) as ex:
         list(ex.map(one, names, objs))
     lib = os.path.join(OUT, "libkvpool.so")
-    _run(["g++", "-shared", "-fPIC"] + SAN + ["-o", lib + ".tmp"] + objs + kernel_objs + ["-L" + os.path.join(ROCM, "lib"),
+    _run(["g++", "-shared", "-fPIC"] + SAN + ["-o", lib + ".tmp"] + objs + [kernels_obj, "-L" + os.path.join(ROCM, "lib"),
          "-lamdhip64", "-Wl,-rpath," + os.path.join(ROCM, "lib")])
     os.replace(lib + ".tmp", lib)
     exe = os.path.join(ROOT, "tests", "abi_client", "abi_client_asan")
