@@ -118,11 +118,9 @@ Cut cut_of(const CacheView &c, uint32_t window)
 // Largest workspace over all windows: a window only shortens the span, and with it the number of parts.
 uint64_t attention_bytes(const CacheView &c) { return cut_of(c, 0).bytes; }
 
-uint32_t evict_room(const CacheView &c) { return c.max_kv / 2; }   // moves of a list: kept ones past keep, in holes before
-uint64_t evict_bytes(const CacheView &c)
-{
-    return (uint64_t)c.n_seq * c.kv_heads * (2 + 2 * (uint64_t)evict_room(c)) * 4;
-}
+// Words of workspace to a list: two of counts, two per token (candidates, then moves), a bit per token.
+uint64_t evict_words(const CacheView &c) { return 2 + 2 * (uint64_t)c.max_kv + 2 * (((uint64_t)c.max_kv + 63) / 64); }
+uint64_t evict_bytes(const CacheView &c) { return (uint64_t)c.n_seq * c.kv_heads * evict_words(c) * 4; }
 
 void need_scale(float scale) { need(std::isfinite(scale) && scale > 0, "scale is not a positive number"); }
 
@@ -336,7 +334,7 @@ void op_evict(const kvp_cache_shape *s, const kvp_batch *b, const int32_t *keep,
     a.v_cache = static_cast<uint16_t *>(v_cache);
     a.len_out = len_out;
     a.moves = static_cast<uint32_t *>(workspace);
-    a.room = evict_room(a.c);
+    a.list_words = evict_words(a.c);
     check_hip(launch_evict(a, static_cast<hipStream_t>(stream)), "eviction launch");
 }
 

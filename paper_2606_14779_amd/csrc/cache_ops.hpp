@@ -75,8 +75,8 @@ struct EvictArgs {
     uint32_t score_stride, pos_stride;
     uint16_t *k_cache, *v_cache;
     int32_t *len_out;
-    uint32_t *moves;                 // [n_seq * kv_heads][1 + 2 * room]: count, then (to, from) pairs
-    uint32_t room;
+    uint32_t *moves;                 // [n_seq * kv_heads][list_words]
+    uint64_t list_words;
 };
 
 // Each launcher enqueues on `stream` of the current device.
