@@ -74,9 +74,10 @@ __global__ __launch_bounds__(NW * 64, DP > 128 ? 1 : 2) void attention_rows(cons
     const CacheView &c = a.c;
     const uint32_t kv_head = blockIdx.x % c.kv_heads;
     const uint32_t rest = blockIdx.x / c.kv_heads;
-    const uint32_t split = rest % a.splits;
+    // the tiles of a part of the keys run side by side, so that its keys come from L2 for all but one of them;
     // later tiles first: under a causal mask they have the most keys
-    const uint32_t tile = a.tiles - 1 - rest / a.splits;
+    const uint32_t split = rest / a.tiles;
+    const uint32_t tile = a.tiles - 1 - rest % a.tiles;
     const uint32_t seq = a.tiles == c.n_seq ? tile : seq_of_tile(c, tile, NW * 32);
     const Seq s = load_seq(c, seq);
     const uint32_t row0 = (tile - (a.tiles == c.n_seq ? tile : first_tile(c, seq, NW * 32))) * (NW * 32);
@@ -108,7 +109,8 @@ __global__ __launch_bounds__(NW * 64, DP > 128 ? 1 : 2) void attention_rows(cons
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i) {
             const uint32_t at = 16 * i + 8 * half;
-            q[i] = at < c.head_dim ? load16g(p + at) : w4{0, 0, 0, 0};
+            q[i] = load16g(p + (at < c.head_dim ? at : 0));
+            if (c.head_dim != DP && at >= c.head_dim) q[i] = w4{0, 0, 0, 0};
         }
     }
 
@@ -128,11 +130,11 @@ __global__ __launch_bounds__(NW * 64, DP > 128 ? 1 : 2) void attention_rows(cons
 
     auto slot_at = [&](int32_t t) {                 // table entry of this lane's key of tile t
         const int32_t key = keys.begin + t * TK + lane;
-        return key < keys.end ? load4g(table + block_of(c, key)) : -1;
+        return load4g(table + block_of(c, min(key, keys.end - 1)));
     };
     auto load_tile = [&](int32_t t, int32_t slot) {
         const int32_t key = keys.begin + t * TK + lane;
-        const uint32_t r = row_of(c, slot, kv_head, key);
+        const uint32_t r = row_of(c, key < keys.end ? slot : -1, kv_head, key);
         const uint64_t ok = __ballot(r != kNoRow);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -158,18 +160,21 @@ __global__ __launch_bounds__(NW * 64, DP > 128 ? 1 : 2) void attention_rows(cons
         }
     };
 
+    int32_t slot_next = -1;
     if (tiles_n) {
-        seen_next = load_tile(0, slot_at(0));
+        const int32_t slot = slot_at(0);
+        slot_next = slot_at(1);
+        seen_next = load_tile(0, slot);
         store_tile(0, seen_next);
     }
-    int32_t slot_next = tiles_n > 1 ? slot_at(1) : -1;
+    loads_arrived();
 
     for (int32_t t = 0; t < tiles_n; ++t) {
         seen = seen_next;
         const int buf = t & 1;
         if (t + 1 < tiles_n) {
             seen_next = load_tile(t + 1, slot_next);
-            if (t + 2 < tiles_n) slot_next = slot_at(t + 2);
+            slot_next = slot_at(t + 2);
         }
         __syncthreads();                            // tile t is in LDS; everyone has left tile t - 1
         const int32_t k0 = keys.begin + t * TK;
@@ -323,7 +328,8 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attention_few(const Attenti
 #pragma unroll
         for (int i = 0; i < KS; ++i) {
             const uint32_t at = 32 * i + 8 * quad;
-            q[i] = at < c.head_dim ? load16g(p + at) : w4{0, 0, 0, 0};
+            q[i] = load16g(p + (at < c.head_dim ? at : 0));
+            if (c.head_dim != DP && at >= c.head_dim) q[i] = w4{0, 0, 0, 0};
         }
     }
     v4f o[DP / 16];
@@ -342,11 +348,11 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attention_few(const Attenti
     uint32_t seen_next = 0;
     auto slot_at = [&](int32_t t) {
         const int32_t key = mine + t * (NW * TK) + (lane & 31);
-        return key < keys.end ? load4g(table + block_of(c, key)) : -1;
+        return load4g(table + block_of(c, min(key, keys.end - 1)));
     };
     auto load_tile = [&](int32_t t, int32_t slot) {
         const int32_t key = mine + t * (NW * TK) + (lane & 31);
-        const uint32_t r = row_of(c, slot, kv_head, key);
+        const uint32_t r = row_of(c, key < keys.end ? slot : -1, kv_head, key);
         const uint32_t ok = (uint32_t)__ballot(r != kNoRow);
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
@@ -368,8 +374,13 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attention_few(const Attenti
         return ok;
     };
 
-    if (steps) seen_next = load_tile(0, slot_at(0));
-    int32_t slot_next = steps > 1 ? slot_at(1) : -1;
+    int32_t slot_next = -1;
+    if (steps) {
+        const int32_t slot = slot_at(0);
+        slot_next = slot_at(1);
+        loads_arrived();
+        seen_next = load_tile(0, slot);
+    }
     uint16_t *vs = lds_v[wave];
 
     for (int32_t t = 0; t < steps; ++t) {
@@ -395,7 +406,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attention_few(const Attenti
         }
         if (t + 1 < steps) {
             seen_next = load_tile(t + 1, slot_next);
-            if (t + 2 < steps) slot_next = slot_at(t + 2);
+            slot_next = slot_at(t + 2);
         }
         if (!(k0 + TK - 1 <= all_first && (int64_t)k0 >= all_full && seen == ~0u)) {
             const uint32_t here = seen >> (4 * quad);
@@ -496,135 +507,241 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attention_few(const Attenti
     }
 }
 
-// Adds the parts of a row: a wave to a row, lanes over the parts for the sums, then over head_dim.
-template <class T>
-__global__ __launch_bounds__(256) void attention_join(const AttentionArgs a)
+// Adds the parts of the rows.  A row is the work of `slices` times LANES neighbouring threads: a thread has 4
+// elements of head_dim and every slices-th part; the slices are added through LDS, always in the same order.
+template <class T, int LANES>
+__global__ __launch_bounds__(256) void attention_join(const AttentionArgs a, const uint32_t slices)
 {
+    constexpr int GROUPS = 256 / LANES;
+    __shared__ v4f lds_sum[256];
+    __shared__ float lds_l[GROUPS], lds_m[GROUPS];
     const CacheView &c = a.c;
     const uint32_t rows = c.total_q * c.heads;
-    const uint32_t row = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= rows) return;
-    const int lane = threadIdx.x & 63;
-    const uint32_t head = row % c.heads;
-    float m = kLowest;
-    for (uint32_t i = lane; i < a.splits; i += 64) {
-        const v2f ml = *(const v2f *)(a.part_ml + 2 * ((uint64_t)i * rows + row));
-        m = fmaxf(m, ml[0]);
-    }
+    const uint32_t group = threadIdx.x / LANES, lane = threadIdx.x % LANES;
+    const uint32_t slice = group % slices, at = lane * 4;
+    const uint32_t row = min(blockIdx.x * (GROUPS / slices) + group / slices, rows - 1);
+    const bool live = at < c.head_dim;
+    // a part of a group's own threads at a time: its maximum and sum first, to rescale by
+    float m = kLowest, l = 0.0f;
+    v4f sum{};
+    constexpr int U = 4;                            // parts in flight
+    for (uint32_t i0 = slice; i0 < a.splits; i0 += U * slices) {
+        v2f ml[U];
+        v4f o[U];
 #pragma unroll
-    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-    float l = 0.0f;
-    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};       // head_dim lane, lane + 64, ..
-    for (uint32_t i0 = 0; i0 < a.splits; i0 += 64) {
-        float w = 0.0f, part_l = 0.0f;
-        if (i0 + lane < a.splits) {
-            const v2f ml = *(const v2f *)(a.part_ml + 2 * ((uint64_t)(i0 + lane) * rows + row));
-            w = exp2_fast(ml[0] - m);
-            part_l = ml[1];
+        for (int u = 0; u < U; ++u) {
+            const uint64_t part = (uint64_t)min(i0 + u * slices, a.splits - 1) * rows + row;
+            ml[u] = *(const v2f *)(a.part_ml + 2 * part);
+            o[u] = *(const v4f *)(a.part_o + part * c.head_dim + (live ? at : 0));
         }
-        l += part_l * w;
-        const uint32_t n = min(64u, a.splits - i0);
-        for (uint32_t i = 0; i < n; ++i) {
-            const float wi = __shfl(w, i), li = __shfl(part_l, i);
-            if (li == 0.0f) continue;               // an empty part wrote no output
-            const float *p = a.part_o + ((uint64_t)(i0 + i) * rows + row) * c.head_dim;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (lane + 64u * j < c.head_dim) sum[j] += p[lane + 64 * j] * wi;
+        for (int u = 0; u < U; ++u) {
+            const bool there = i0 + u * slices < a.splits && ml[u][1] != 0.0f;   // an empty part wrote no output
+            const float to = there ? fmaxf(m, ml[u][0]) : m;
+            const float f = exp2_fast(m - to), g = there ? exp2_fast(ml[u][0] - to) : 0.0f;
+            m = to;
+            l = l * f + (there ? ml[u][1] : 0.0f) * g;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum[j] = sum[j] * f + (there ? o[u][j] : 0.0f) * g;
         }
     }
+    lds_sum[threadIdx.x] = sum;
+    if (lane == 0) lds_m[group] = m, lds_l[group] = l;
+    __syncthreads();
+    if (slice) return;
+    for (uint32_t i = 1; i < slices; ++i) {
+        const float to = fmaxf(m, lds_m[group + i]);
+        const float f = exp2_fast(m - to), g = exp2_fast(lds_m[group + i] - to);
+        const v4f o = lds_sum[threadIdx.x + i * LANES];
+        m = to;
+        l = l * f + lds_l[group + i] * g;
 #pragma unroll
-    for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d);
+        for (int j = 0; j < 4; ++j) sum[j] = sum[j] * f + o[j] * g;
+    }
+    const uint32_t head = row % c.heads, token = row / c.heads;
     const RowEnd e = finish_row(m, l, a.sinks, head);
-    const uint32_t token = row / c.heads;
-    uint16_t *p = a.out + (uint64_t)token * a.out_stride + (uint64_t)head * c.head_dim;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (lane + 64u * j < c.head_dim) p[lane + 64 * j] = (uint16_t)T::pack(sum[j] * e.scale_o, 0.0f);
+    if (blockIdx.x * (GROUPS / slices) + group / slices >= rows) return;
+    if (live)
+        *(w2 *)(a.out + (uint64_t)token * a.out_stride + (uint64_t)head * c.head_dim + at) =
+            w2{T::pack(sum[0] * e.scale_o, sum[1] * e.scale_o), T::pack(sum[2] * e.scale_o, sum[3] * e.scale_o)};
     if (a.lse && lane == 0) a.lse[(uint64_t)head * c.total_q + token] = e.lse;
 }
 
 // ---- attention weight of the cached tokens
 
 constexpr int kMassWaves = 4;
+constexpr int kMassKeys = 64;                        // to a wave
+constexpr int kMassRows = 64;                        // through LDS at a time
 
-// A wave holds 32 keys as the A operand and goes over the rows, 32 at a time: S^T again, so every lane adds up
-// the weights of its own 16 keys for one row of each 32, in a fixed order, and the lanes are added at the end.
+// One step of adding 2 D registers over the lanes: lanes with bit D set keep the upper half.
+template <int D>
+__device__ __forceinline__ void halve(float (&acc)[32], int lane)
+{
+    const bool up = lane & D;
+#pragma unroll
+    for (int r = 0; r < D; ++r) {
+        const float low = acc[r], high = acc[r + D];
+        acc[r] = (up ? high : low) + __shfl_xor(up ? low : high, D);
+    }
+}
+
+// A wave holds 64 keys as the A operand and goes over the rows, which come through LDS for all waves: S^T again,
+// so every lane adds up the weights of its own 32 keys, for one row of each 32, in a fixed order; the lanes are
+// added at the end.  Long rows of queries are bound by the exponentials and the sums around them (three
+// instructions to a weight), single tokens by reading the keys, which therefore come in whole rows, through LDS.
 template <class T, int DP>
 __global__ __launch_bounds__(kMassWaves * 64, DP > 128 ? 1 : 2) void attention_mass(const MassArgs a)
 {
+    constexpr int CH = DP / 8, TK = kMassKeys, TR = kMassRows, NT = kMassWaves * 64;
+    constexpr int PASS = NT / CH, N = TR / PASS;     // rows that the workgroup loads at once
+    __shared__ __align__(16) uint16_t lds[kMassWaves * TK * DP];    // the keys at first, then two tiles of rows
+    __shared__ float lds_lse[2][TR];
+    static_assert(2 * TR <= kMassWaves * TK, "two tiles of rows fit the keys' space");
+
     const CacheView &c = a.c;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int col = lane & 31, half = lane >> 5;
     const uint32_t kv_head = blockIdx.x % c.kv_heads;
     const uint32_t tile = blockIdx.x / c.kv_heads;
-    const uint32_t tiles = (c.max_kv + kMassWaves * 32 - 1) / (kMassWaves * 32);
+    const uint32_t tiles = (c.max_kv + kMassWaves * TK - 1) / (kMassWaves * TK);
     const uint32_t seq = tile / tiles;
     const Seq s = load_seq(c, seq);
-    const int32_t k0 = (int32_t)(tile % tiles * (kMassWaves * 32)) + wave * 32;
-    if (k0 >= s.kv) return;
+    const int32_t group_k0 = (int32_t)(tile % tiles * (kMassWaves * TK));
+    if (group_k0 >= s.kv) return;
+    const int32_t k0 = group_k0 + wave * TK;
 
-    w4 k[DP / 16];
-    bool there;
-    {
-        const int32_t key = min(k0 + col, s.kv - 1);
-        const uint32_t r = row_of(c, load4g(c.table + (uint64_t)seq * c.table_stride + block_of(c, key)), kv_head, key);
-        there = r != kNoRow;
-        const uint16_t *p = a.k + (uint64_t)(there ? r : 0) * c.head_dim;
-#pragma unroll
-        for (int i = 0; i < DP / 16; ++i) {
-            const uint32_t at = 16 * i + 8 * half;
-            k[i] = at < c.head_dim ? load16g(p + at) : w4{0, 0, 0, 0};
-        }
-    }
-    const uint32_t seen = (uint32_t)__ballot(there) >> (4 * half);   // bit of key 8*(r/4) + r%4
-
+    // rows that see some key of the workgroup
     const int32_t shift = s.kv - s.n_q;
     int32_t first = a.last ? max(0, s.n_q - (int32_t)min(a.last, 0x7FFFFFFFu)) : 0;
-    first = max(first, k0 - shift);                  // earlier tokens see none of these keys
+    first = max(first, group_k0 - shift);
     int32_t last = s.n_q - 1;
-    if (a.window) last = (int32_t)min((int64_t)last, (int64_t)k0 + 31 + a.window - 1 - shift);
-    float acc[16];
-#pragma unroll
-    for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
+    if (a.window)
+        last = (int32_t)min((int64_t)last, (int64_t)group_k0 + kMassWaves * TK - 1 + (int64_t)a.window - 1 - shift);
+    const uint32_t row_begin = (uint32_t)max(first, 0) * c.group;
+    const uint32_t row_end = last < first ? row_begin : (uint32_t)(last + 1) * c.group;
 
-    const int64_t row_begin = (int64_t)first * c.group, row_end = ((int64_t)last + 1) * c.group;
-    for (int64_t r0 = row_begin; r0 < row_end; r0 += 32) {
-        const uint32_t row = (uint32_t)min(r0 + col, row_end - 1);
-        const int32_t token = (int32_t)(row / c.group);
-        const uint32_t head = kv_head * c.group + row % c.group;
-        const uint16_t *p = a.q + (uint64_t)(s.q_begin + token) * a.q_stride + (uint64_t)head * c.head_dim;
-        const float lse = a.lse[(uint64_t)head * c.total_q + s.q_begin + token] * kLog2e;
-        v16f z{};
+    const int load_piece = tid % CH, load_row = tid / CH;
+    const bool piece_live = (uint32_t)load_piece * 8 < c.head_dim;
+    const uint32_t piece_at = piece_live ? load_piece * 8 : 0;
+    w4 rq[N];
+    float r_lse = 0.0f;
+    auto load_rows = [&](uint32_t r0) {
 #pragma unroll
-        for (int i = 0; i < DP / 16; ++i) {
-            const uint32_t at = 16 * i + 8 * half;
-            const w4 q = at < c.head_dim ? load16g(p + at) : w4{0, 0, 0, 0};
-            z = T::mma32(k[i], q, z);
+        for (int i = 0; i < N; ++i) {
+            const uint32_t row = min(r0 + load_row + i * PASS, row_end - 1), token = token_of(c, row);
+            const uint32_t head = kv_head * c.group + row - token * c.group;
+            rq[i] = load16g(a.q + (uint64_t)(s.q_begin + token) * a.q_stride + (uint64_t)head * c.head_dim + piece_at);
         }
-        const bool live = r0 + col < row_end && lse > -INFINITY;   // a row without keys gives nothing
-        const int32_t limit = shift + token;
-        const int32_t floor_key = a.window ? (int32_t)max((int64_t)limit + 1 - (int64_t)a.window, (int64_t)0) : 0;
+        const uint32_t row = min(r0 + (tid & (TR - 1)), row_end - 1), token = token_of(c, row);
+        r_lse = a.lse[(uint64_t)(kv_head * c.group + row - token * c.group) * c.total_q + s.q_begin + token];
+    };
+    auto store_rows = [&](int buf, uint32_t r0) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int at = 8 * (r / 4) + r % 4;
-            const int32_t key = k0 + at + 4 * half;
-            const bool sees = live && key <= limit && key >= floor_key && (seen >> at & 1);
-            acc[r] += sees ? exp2_fast(__builtin_fmaf(z[r], a.scale_log2, -lse)) : 0.0f;
+        for (int i = 0; i < N; ++i) {
+            const int r = load_row + i * PASS;
+            const int qp = load_piece ^ (DP >= 128 ? r & 15 : (r >> 1) & 7);
+            *(w4 *)&lds[(buf * TR + r) * DP + qp * 8] = piece_live ? rq[i] : w4{0, 0, 0, 0};
         }
+        // a row past the end, or without keys, gives no weight: exp2(-inf)
+        if (tid < TR) lds_lse[buf][tid] = r0 + tid < row_end && r_lse > -INFINITY ? r_lse * kLog2e : INFINITY;
+    };
+
+    uint64_t seen = 0;
+    w4 k[2][DP / 16];
+    {
+        constexpr int KPASS = 64 / CH;               // rows that a wave loads at once
+        const int piece = lane % CH, load_key = lane / CH;
+        const bool live = (uint32_t)piece * 8 < c.head_dim;
+        const int32_t key = k0 + lane;
+        const int32_t slot = load4g(c.table + (uint64_t)seq * c.table_stride + block_of(c, min(key, s.kv - 1)));
+        const uint32_t r = row_of(c, key < s.kv ? slot : -1, kv_head, key);
+        seen = __ballot(r != kNoRow);
+        uint16_t *ks = lds + wave * TK * DP;
+        w4 rk[TK / KPASS];
+#pragma unroll
+        for (int i = 0; i < TK / KPASS; ++i) {
+            uint32_t from = __shfl(r, load_key + i * KPASS);
+            from = from == kNoRow ? 0 : from;
+            rk[i] = load16g(a.k + (uint64_t)from * c.head_dim + (live ? piece * 8 : 0));
+        }
+        if (row_begin < row_end) load_rows(row_begin);
+#pragma unroll
+        for (int i = 0; i < TK / KPASS; ++i) {
+            const int at = load_key + i * KPASS;
+            const int kp = piece ^ (DP >= 128 ? at & 15 : (at >> 1) & 7);
+            *(w4 *)&ks[at * DP + kp * 8] = live ? rk[i] : w4{0, 0, 0, 0};
+        }
+        __syncthreads();
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < DP / 16; ++i) {
+                const int at = kb * 32 + col;
+                const int kp = (2 * i + half) ^ (DP >= 128 ? at & 15 : (at >> 1) & 7);
+                k[kb][i] = *(const w4 *)&ks[at * DP + kp * 8];
+            }
+        __syncthreads();
     }
-    // over the 32 lanes of each half
+
+    float acc[32];
 #pragma unroll
-    for (int d = 16; d; d >>= 1)
+    for (int r = 0; r < 32; ++r) acc[r] = 0.0f;
+    if (row_begin < row_end) store_rows(0, row_begin);
+    loads_arrived();
+    int buf = 0;
+    for (uint32_t r0 = row_begin; r0 < row_end; r0 += TR, buf ^= 1) {
+        if (r0 + TR < row_end) load_rows(r0 + TR);
+        __syncthreads();                             // the rows are in LDS; everyone has left the tile before
+        const int32_t t_first = (int32_t)token_of(c, r0), t_last = (int32_t)token_of(c, min(r0 + TR, row_end) - 1);
+        const bool some = k0 <= shift + t_last && (!a.window || (int64_t)k0 + TK - 1 > (int64_t)shift + t_first - a.window);
+        const bool full = k0 + TK - 1 <= shift + t_first && (!a.window || (int64_t)k0 > (int64_t)shift + t_last - a.window);
+        if (some) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[r] += __shfl_xor(acc[r], d);
-    float sum = 0.0f;
+            for (int rb = 0; rb < TR / 32; ++rb) {
+                if (r0 + rb * 32 >= row_end) break;
+                const int at = rb * 32 + col;
+                const float lse = lds_lse[buf][at];
+                v16f z[2] = {v16f{}, v16f{}};
 #pragma unroll
-    for (int r = 0; r < 16; ++r) sum = col == r ? acc[r] : sum;      // lane r of a half writes key r's
-    const int32_t key = k0 + 8 * (col / 4) + 4 * half + col % 4;
-    if (col < 16 && key < s.kv) {
-        const uint64_t at = ((uint64_t)seq * c.kv_heads + kv_head) * a.score_stride + key;
-        a.score_out[at] = (a.score_in ? a.score_in[at] : 0.0f) + sum;
+                for (int i = 0; i < DP / 16; ++i) {
+                    const int qp = (2 * i + half) ^ (DP >= 128 ? at & 15 : (at >> 1) & 7);
+                    const w4 q = *(const w4 *)&lds[(buf * TR + at) * DP + qp * 8];
+                    z[0] = T::mma32(k[0][i], q, z[0]);
+                    z[1] = T::mma32(k[1][i], q, z[1]);
+                }
+                if (full) {
+#pragma unroll
+                    for (int r = 0; r < 32; ++r)
+                        acc[r] += exp2_fast(__builtin_fmaf(z[r / 16][r % 16], a.scale_log2, -lse));
+                } else {
+                    const int32_t limit = shift + (int32_t)token_of(c, r0 + at);
+                    const int32_t floor_key = a.window ? (int32_t)max((int64_t)limit + 1 - (int64_t)a.window, (int64_t)0) : 0;
+#pragma unroll
+                    for (int r = 0; r < 32; ++r) {
+                        const int32_t key = k0 + 32 * (r / 16) + 8 * (r % 16 / 4) + r % 4 + 4 * half;
+                        const bool sees = key <= limit && key >= floor_key;
+                        const float z1 = sees ? __builtin_fmaf(z[r / 16][r % 16], a.scale_log2, -lse) : -INFINITY;
+                        acc[r] += exp2_fast(z1);
+                    }
+                }
+            }
+        }
+        if (r0 + TR < row_end) store_rows(buf ^ 1, r0 + TR);
+    }
+
+    // over the 32 lanes of each half: at every step a lane keeps half of its keys and gives the others away, so
+    // that lane i ends with the sum of register i
+    halve<16>(acc, lane);
+    halve<8>(acc, lane);
+    halve<4>(acc, lane);
+    halve<2>(acc, lane);
+    halve<1>(acc, lane);
+    const int at = 32 * (col / 16) + 8 * (col % 16 / 4) + col % 4 + 4 * half;
+    const int32_t key = k0 + at;
+    if (key < s.kv) {
+        const uint64_t to = ((uint64_t)seq * c.kv_heads + kv_head) * a.score_stride + key;
+        const float sum = seen >> at & 1 ? acc[0] : 0.0f;            // an absent key may have been anything
+        a.score_out[to] = (a.score_in ? a.score_in[to] : 0.0f) + sum;
     }
 }
 
@@ -658,10 +775,22 @@ struct Few {
     }
 };
 template <class T, int DP>
+struct Join {
+    static hipError_t go(const AttentionArgs &a, hipStream_t stream)
+    {
+        constexpr uint32_t groups = 256 / (DP / 4);
+        uint32_t slices = 1;
+        while (slices < groups && slices * 2 <= a.splits) slices *= 2;
+        const uint32_t per = groups / slices, rows = a.c.total_q * a.c.heads;
+        attention_join<T, DP / 4><<<(rows + per - 1) / per, 256, 0, stream>>>(a, slices);
+        return hipGetLastError();
+    }
+};
+template <class T, int DP>
 struct Mass {
     static hipError_t go(const MassArgs &a, hipStream_t stream)
     {
-        const uint32_t tiles = (a.c.max_kv + kMassWaves * 32 - 1) / (kMassWaves * 32);
+        const uint32_t tiles = (a.c.max_kv + kMassWaves * kMassKeys - 1) / (kMassWaves * kMassKeys);
         attention_mass<T, DP><<<tiles * a.c.n_seq * a.c.kv_heads, kMassWaves * 64, 0, stream>>>(a);
         return hipGetLastError();
     }
@@ -676,12 +805,7 @@ hipError_t launch_attention(const AttentionArgs &a, uint32_t dtype, bool few_row
 
 hipError_t launch_attention_join(const AttentionArgs &a, uint32_t dtype, hipStream_t stream)
 {
-    const uint32_t groups = (a.c.total_q * a.c.heads + 3) / 4;
-    if (dtype == KVP_BF16)
-        attention_join<BF16><<<groups, 256, 0, stream>>>(a);
-    else
-        attention_join<F16><<<groups, 256, 0, stream>>>(a);
-    return hipGetLastError();
+    return by_type<Join>(dtype, a.c.head_dim, a, stream);
 }
 
 hipError_t launch_mass(const MassArgs &a, uint32_t dtype, hipStream_t stream)

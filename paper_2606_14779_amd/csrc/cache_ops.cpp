@@ -25,6 +25,15 @@ void need_pointer(const void *p, uintptr_t align, const char *what)
     if (!aligned(p, align)) fail(KVP_ERR_INVALID, std::string(what) + " is not aligned to " + std::to_string(align) + " bytes");
 }
 
+// x / d for x below 2^31 as (2 x * magic) >> 32 >> shift: with 2^(shift - 1) < d <= 2^shift and
+// magic = ceil(2^(31 + shift) / d), the product is too large by less than x / 2^31 / d, so by less than 1 / d.
+void divide_by(uint32_t d, uint32_t *magic, uint32_t *shift)
+{
+    *shift = 0;
+    while ((1u << *shift) < d) ++*shift;
+    *magic = (uint32_t)(((1ull << (31 + *shift)) + d - 1) / d);
+}
+
 constexpr uint64_t kMostRows = 1ull << 30;   // new tokens times query heads: what a launch's grid can count
 
 // Checks the shape and the batch; queries says whether cu_q is used.
@@ -69,9 +78,8 @@ CacheView view_of(const kvp_cache_shape *s, const kvp_batch *b, bool queries)
     c.group = s->num_q_heads / s->num_kv_heads;
     c.head_dim = s->head_dim;
     c.block = s->block_size;
-    c.block_shift = kNoShift;
-    if (!(c.block & (c.block - 1)))
-        for (c.block_shift = 0; (1u << c.block_shift) < c.block;) ++c.block_shift;
+    divide_by(c.block, &c.block_magic, &c.block_shift);
+    divide_by(c.group, &c.group_magic, &c.group_shift);
     return c;
 }
 
@@ -101,10 +109,11 @@ Cut cut_of(const CacheView &c, uint32_t window)
     const uint64_t tile_tokens = p.few ? c.max_q : std::min<uint64_t>(c.max_q, kTileRows / c.group + 2);
     uint64_t span = c.max_kv;
     if (window) span = std::min<uint64_t>(span, (uint64_t)window + tile_tokens + kTileKeys);
-    const uint64_t units = std::max<uint64_t>(1, (uint64_t)p.tiles * c.kv_heads);
-    const uint64_t fill = p.few ? 1024 : 512;
-    const uint64_t least = p.few ? 128 : 256;        // keys of a part
-    uint64_t splits = units >= fill ? 1 : fill / units;
+    // workgroups that have work if all sequences are alike
+    const uint64_t units = std::max<uint64_t>(1, (p.few ? c.n_seq : (rows + kTileRows - 1) / kTileRows) * c.kv_heads);
+    const uint64_t fill = p.few ? 4096 : 2048;       // workgroups wanted
+    const uint64_t least = p.few ? 128 : 512;        // keys of a part
+    uint64_t splits = (fill + units / 2) / units;
     splits = std::max<uint64_t>(1, std::min(splits, span / least));
     uint64_t keys = (span + splits - 1) / splits;
     const uint64_t unit = p.few ? 128 : kTileKeys;

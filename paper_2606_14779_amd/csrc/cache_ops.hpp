@@ -16,9 +16,9 @@ struct CacheView {
     const int32_t *cu_q, *kv_len, *table;
     uint32_t n_seq, total_q, max_q, max_kv, table_stride;
     uint32_t num_slots, heads, kv_heads, group, head_dim, block;
-    uint32_t block_shift;      // log2(block), or kNoShift
+    // x / block = (2 x * magic) >> 32 >> shift for x below 2^31, and the same for group
+    uint32_t block_magic, block_shift, group_magic, group_shift;
 };
-constexpr uint32_t kNoShift = 32;
 constexpr uint32_t kNoRow = 0xFFFFFFFFu;
 
 struct AttentionArgs {

@@ -111,13 +111,23 @@ __device__ __forceinline__ Seq load_seq(const CacheView &c, uint32_t s)
 // Row number (of head_dim elements) of a sequence's cached token, or kNoRow where its slot is none of the cache's.
 __device__ __forceinline__ uint32_t block_of(const CacheView &c, uint32_t token)
 {
-    return c.block_shift != kNoShift ? token >> c.block_shift : token / c.block;
+    return __umulhi(2 * token, c.block_magic) >> c.block_shift;
 }
 __device__ __forceinline__ uint32_t row_of(const CacheView &c, int32_t slot, uint32_t kv_head, uint32_t token)
 {
-    const uint32_t off = c.block_shift != kNoShift ? token & (c.block - 1) : token % c.block;
+    const uint32_t off = token - block_of(c, token) * c.block;
     return (uint32_t)slot < c.num_slots ? ((uint32_t)slot * c.kv_heads + kv_head) * c.block + off : kNoRow;
 }
+
+// New token of a KV head's row (its rows are token-major).
+__device__ __forceinline__ uint32_t token_of(const CacheView &c, uint32_t row)
+{
+    return __umulhi(2 * row, c.group_magic) >> c.group_shift;
+}
+
+// All loads so far have arrived (vmcnt 0): said before a loop, so that the loop does not wait for its own prefetches
+// on behalf of loads that were issued before it.
+__device__ __forceinline__ void loads_arrived() { __builtin_amdgcn_s_waitcnt(0x0F70); }
 
 // Sequence of a row tile: sequence s owns the tiles from floor(rows before it / tile) + s on, at least as many
 // as its rows need, so no prefix of tile counts has to be made.
