@@ -18,6 +18,8 @@
 // counts: the waves of a workgroup split the keys, and a join in LDS ends the workgroup.
 // Where there are few row tiles both split the keys over workgroups as well; attention_join adds the parts.
 
+#include <type_traits>
+
 #include "wave.hpp"
 
 namespace kvp {
@@ -60,12 +62,19 @@ __device__ __forceinline__ Split keys_of(const AttentionArgs &a, const Seq &s, i
     return {(int32_t)min(begin, (int64_t)max(hi, 0)), (int32_t)max(end, (int64_t)0)};
 }
 
-// ---- 32 rows to a wave
+// ---- many rows
 
-template <class T, int DP, int NW>
-__global__ __launch_bounds__(NW * 64, DP > 128 ? 1 : 2) void attention_rows(const AttentionArgs a)
+constexpr int kRowWaves = kTileRows / 32;
+
+// 32 rows to a wave.  The vector unit, not the matrix cores, bounds this kernel: a tile of 64 keys at head_dim 128 is
+// 32 products of 32 cycles, and beside them about 140 vector instructions for the softmax alone (a maximum, a scaled
+// difference, an exponential, a sum and half a rounding per logit).  So the rest is kept off the vector unit: 32-bit
+// offsets from scalar bases where a buffer has less than 2^32 bytes (Offset), buffers of LDS known at compile time
+// (the loop is written for two tiles), masks and zeros only in the tiles that need them.
+template <class T, int DP, class Offset>
+__global__ __launch_bounds__(kRowWaves * 64, DP > 128 ? 1 : 2) void attention_rows(const AttentionArgs a)
 {
-    constexpr int TK = kTileKeys;
+    constexpr int TK = kTileKeys, NW = kRowWaves, TR = kTileRows;
     constexpr int CH = DP / 8;                       // 16-byte pieces of a row
     constexpr int PASS = NW * 64 / CH;               // rows that the workgroup loads at once
     constexpr int N = TK / PASS;
@@ -78,30 +87,31 @@ __global__ __launch_bounds__(NW * 64, DP > 128 ? 1 : 2) void attention_rows(cons
     // later tiles first: under a causal mask they have the most keys
     const uint32_t split = rest / a.tiles;
     const uint32_t tile = a.tiles - 1 - rest % a.tiles;
-    const uint32_t seq = a.tiles == c.n_seq ? tile : seq_of_tile(c, tile, NW * 32);
+    const uint32_t seq = a.tiles == c.n_seq ? tile : seq_of_tile(c, tile, TR);
     const Seq s = load_seq(c, seq);
-    const uint32_t row0 = (tile - (a.tiles == c.n_seq ? tile : first_tile(c, seq, NW * 32))) * (NW * 32);
+    const uint32_t row0 = (tile - (a.tiles == c.n_seq ? tile : first_tile(c, seq, TR))) * TR;
     const uint32_t rows = (uint32_t)s.n_q * c.group;
     if (row0 >= rows) return;
-    const uint32_t rows_here = min(rows - row0, (uint32_t)(NW * 32));
+    const uint32_t rows_here = min(rows - row0, (uint32_t)TR);
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
     const uint32_t wave_row = wave * 32;
     const bool wave_live = wave_row < rows_here;
+    const int32_t shift = s.kv - s.n_q;
     const uint32_t row = row0 + min(wave_row + col, rows_here - 1);   // rows past the end repeat the last one
-    const bool live = wave_row + col < rows_here;
-    const int32_t token = (int32_t)(row / c.group);
-    const uint32_t head = kv_head * c.group + row % c.group;
-    const int32_t limit = min(s.kv - s.n_q + token, s.kv - 1);        // last key that this row sees
+    const int32_t token = (int32_t)token_of(c, row);
+    const uint32_t head = kv_head * c.group + row - (uint32_t)token * c.group;
+    const int32_t limit = min(shift + token, s.kv - 1);               // last key that this row sees
     const int32_t floor_key = a.window ? (int32_t)max((int64_t)limit + 1 - (int64_t)a.window, (int64_t)0) : 0;
 
-    const Split keys = keys_of(a, s, (int32_t)(row0 / c.group), (int32_t)((row0 + rows_here - 1) / c.group), split);
-    // the wave's own range of limits
-    const int32_t wave_first = s.kv - s.n_q + (int32_t)((row0 + min(wave_row, rows_here - 1)) / c.group);
-    const int32_t wave_last = s.kv - s.n_q + (int32_t)((row0 + min(wave_row + 31, rows_here - 1)) / c.group);
-    const int64_t wave_low = a.window ? (int64_t)wave_first + 1 - (int64_t)a.window : 0;      // first key seen by any row
-    const int64_t wave_full = a.window ? (int64_t)wave_last + 1 - (int64_t)a.window : 0;      // and by every row
+    const Split keys = keys_of(a, s, (int32_t)token_of(c, row0), (int32_t)token_of(c, row0 + rows_here - 1), split);
+    const int32_t tiles_n = keys.end > keys.begin ? (keys.end - keys.begin + TK - 1) / TK : 0;
+    // what the wave's rows see: keys of [wave_low, wave_last], all of them those of [wave_full, wave_first]
+    const int32_t wave_first = shift + (int32_t)token_of(c, row0 + min(wave_row, rows_here - 1));
+    const int32_t wave_last = wave_live ? shift + (int32_t)token_of(c, row0 + min(wave_row + 31, rows_here - 1)) : -1;
+    const int32_t wave_low = a.window ? (int32_t)max((int64_t)wave_first + 1 - (int64_t)a.window, (int64_t)0) : 0;
+    const int32_t wave_full = a.window ? (int32_t)max((int64_t)wave_last + 1 - (int64_t)a.window, (int64_t)0) : 0;
 
     w4 q[DP / 16];
     {
@@ -113,7 +123,6 @@ __global__ __launch_bounds__(NW * 64, DP > 128 ? 1 : 2) void attention_rows(cons
             if (c.head_dim != DP && at >= c.head_dim) q[i] = w4{0, 0, 0, 0};
         }
     }
-
     v16f o[DP / 32];
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i) o[i] = v16f{};
@@ -122,135 +131,140 @@ __global__ __launch_bounds__(NW * 64, DP > 128 ? 1 : 2) void attention_rows(cons
     // loading: thread -> row load_row + i * PASS of a tile, piece load_piece
     const int load_piece = tid % CH, load_row = tid / CH;
     const bool piece_live = (uint32_t)load_piece * 8 < c.head_dim;
-    const uint32_t piece_at = piece_live ? load_piece * 8 : 0;
+    const Offset piece_at = piece_live ? load_piece * 16 : 0;
     const int32_t *table = c.table + (uint64_t)seq * c.table_stride;
-    const int32_t tiles_n = keys.end > keys.begin ? (keys.end - keys.begin + TK - 1) / TK : 0;
     w4 rk[N], rv[N];
-    uint64_t seen_next = 0, seen;                   // which keys of a tile are there
 
-    auto slot_at = [&](int32_t t) {                 // table entry of this lane's key of tile t
-        const int32_t key = keys.begin + t * TK + lane;
-        return load4g(table + block_of(c, min(key, keys.end - 1)));
+    auto slot_at = [&](int32_t t) __attribute__((always_inline)) {                 // table entry of this lane's key of tile t
+        return load4g(table + block_of(c, min(keys.begin + t * TK + lane, keys.end - 1)));
     };
-    auto load_tile = [&](int32_t t, int32_t slot) {
+    // Starts the loads of tile t from its table entries; returns which of its keys are there.
+    auto load_tile = [&](int32_t t, int32_t slot) __attribute__((always_inline)) {
         const int32_t key = keys.begin + t * TK + lane;
         const uint32_t r = row_of(c, key < keys.end ? slot : -1, kv_head, key);
-        const uint64_t ok = __ballot(r != kNoRow);
+        const Offset at = (Offset)(r == kNoRow ? 0 : r) * (c.head_dim * 2);   // not there: a row that is
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            uint32_t from = __shfl(r, load_row + i * PASS);
-            from = from == kNoRow ? 0 : from;       // loads are not predicated: a row that is there
-            const uint64_t at = (uint64_t)from * c.head_dim + piece_at;
-            rk[i] = load16g(a.k + at);
-            rv[i] = load16g(a.v + at);
+            const Offset from = lane_value(at, load_row + i * PASS) + piece_at;
+            rk[i] = load16g((const uint16_t *)((const char *)a.k + from));
+            rv[i] = load16g((const uint16_t *)((const char *)a.v + from));
         }
-        return ok;
+        return __ballot(r != kNoRow);
     };
-    auto store_tile = [&](int buf, uint64_t ok) {
+    // Rows of 64 elements lie two to 64 banks of LDS, longer ones fill them: the pieces of a row change places with
+    // its number, so that 16 rows read at one place of K, and four at four places of V, meet different banks.
+    auto store_tile = [&](uint16_t *ks, uint16_t *vs, uint64_t seen) __attribute__((always_inline)) {
+        if (__builtin_expect(c.head_dim != DP || seen != ~0ull, 0)) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if (!piece_live) rk[i] = w4{0, 0, 0, 0};
+                // what is not there must be finite in V: its weight is 0
+                if (!piece_live || !(seen >> (load_row + i * PASS) & 1)) rv[i] = w4{0, 0, 0, 0};
+            }
+        }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int r = load_row + i * PASS;
-            // what is not there must be finite in V: its weight is 0
-            const bool there = piece_live && (ok >> r & 1);
-            const w4 zero = {0, 0, 0, 0};
-            const int kp = load_piece ^ (DP >= 128 ? r & 15 : (r >> 1) & 7);
-            const int vp = load_piece ^ (DP >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2);
-            *(w4 *)&lds_k[buf][r * DP + kp * 8] = piece_live ? rk[i] : zero;
-            *(w4 *)&lds_v[buf][r * DP + vp * 8] = there ? rv[i] : zero;
+            *(w4 *)&ks[r * DP + (load_piece ^ (DP >= 128 ? r & 15 : (r >> 1) & 7)) * 8] = rk[i];
+            *(w4 *)&vs[r * DP + (load_piece ^ (DP >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2)) * 8] = rv[i];
         }
     };
-
-    int32_t slot_next = -1;
-    if (tiles_n) {
-        const int32_t slot = slot_at(0);
-        slot_next = slot_at(1);
-        seen_next = load_tile(0, slot);
-        store_tile(0, seen_next);
-    }
-    loads_arrived();
-
-    for (int32_t t = 0; t < tiles_n; ++t) {
-        seen = seen_next;
-        const int buf = t & 1;
-        if (t + 1 < tiles_n) {
-            seen_next = load_tile(t + 1, slot_next);
-            slot_next = slot_at(t + 2);
+    auto compute = [&](const uint16_t *ks, const uint16_t *vs, int32_t k0, uint64_t seen) __attribute__((always_inline)) {
+        v16f z[2];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            z[kb] = v16f{};
+            const int r = kb * 32 + col;
+#pragma unroll
+            for (int i = 0; i < DP / 16; ++i) {
+                const int piece = (2 * i + half) ^ (DP >= 128 ? r & 15 : (r >> 1) & 7);
+                z[kb] = T::mma32(*(const w4 *)&ks[r * DP + piece * 8], q[i], z[kb]);
+            }
         }
-        __syncthreads();                            // tile t is in LDS; everyone has left tile t - 1
-        const int32_t k0 = keys.begin + t * TK;
-        if (wave_live && k0 <= wave_last && (int64_t)k0 + TK > wave_low) {
-            const uint16_t *ks = lds_k[buf], *vs = lds_v[buf];
-            v16f z[2];
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
-                z[kb] = v16f{};
-                const int r = kb * 32 + col;
-#pragma unroll
-                for (int i = 0; i < DP / 16; ++i) {
-                    const int piece = (2 * i + half) ^ (DP >= 128 ? r & 15 : (r >> 1) & 7);
-                    z[kb] = T::mma32(*(const w4 *)&ks[r * DP + piece * 8], q[i], z[kb]);
-                }
-            }
-            if (!(k0 + TK - 1 <= wave_first && (int64_t)k0 >= wave_full && seen == ~0ull)) {
-                const uint64_t mine = seen >> (4 * half);
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int at = kb * 32 + 8 * (r / 4) + r % 4;
-                        const int32_t key = k0 + at + 4 * half;
-                        const bool sees = key <= limit && key >= floor_key && (mine >> at & 1);
-                        z[kb][r] = sees ? z[kb][r] : -INFINITY;
-                    }
-            }
-            float top = z[0][0];
-#pragma unroll
-            for (int r = 1; r < 16; ++r) top = fmaxf(top, z[0][r]);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(top, z[1][r]);
-            top = fmaxf(top, other_half(top)) * a.scale_log2;
-            // The maximum moves only when it is passed by 2^8: weights up to 2^8 lose nothing in 32 bits, nor when
-            // rounded to 16 (their sum and the output keep the same factor), and rescaling becomes rare.
-            if (__any(top > m + 8.0f)) {
-                const float to = fmaxf(m, top);
-                const float f = exp2_fast(m - to);
-                m = to;
-                l *= f;
-#pragma unroll
-                for (int i = 0; i < DP / 32; ++i)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[i][r] *= f;
-            }
+        if (__builtin_expect(!(k0 + TK - 1 <= wave_first && k0 >= wave_full && seen == ~0ull), 0)) {
+            const uint64_t mine = seen >> (4 * half);
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    z[kb][r] = exp2_fast(__builtin_fmaf(z[kb][r], a.scale_log2, -m));
-                    l += z[kb][r];
-                }
-            // The weights are rounded to the type of the values, as the matrix cores take them; their sum is not.
-            const int ti = lane & 15;
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int cc = 0; cc < 2; ++cc) {
-                    w4 p;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) p[j] = T::pack(z[kb][8 * cc + 2 * j], z[kb][8 * cc + 2 * j + 1]);
-                    const int r = kb * 32 + cc * 16 + 4 * half + ti / 4;
-#pragma unroll
-                    for (int db = 0; db < DP / 32; ++db) {
-                        const int piece = db * 4 + 2 * (lane >> 4 & 1) + (ti % 4) / 2;
-                        const int at = (piece ^ (DP >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2)) * 8 + (ti & 1) * 4;
-                        const w2 x = read_down(&vs[r * DP + at]), y = read_down(&vs[(r + 8) * DP + at]);
-                        o[db] = T::mma32(w4{x[0], x[1], y[0], y[1]}, p, o[db]);
-                    }
+                    const int at = kb * 32 + 8 * (r / 4) + r % 4;
+                    const int32_t key = k0 + at + 4 * half;
+                    const bool sees = key <= limit && key >= floor_key && (mine >> at & 1);
+                    z[kb][r] = sees ? z[kb][r] : -INFINITY;
                 }
         }
-        if (t + 1 < tiles_n) store_tile(buf ^ 1, seen_next);
+        float top = z[0][0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) top = fmaxf(top, z[0][r]);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, z[1][r]);
+        top = fmaxf(top, other_half(top)) * a.scale_log2;
+        // The maximum moves only when it is passed by 2^8: weights up to 2^8 lose nothing in 32 bits, nor when
+        // rounded to 16 (their sum and the output keep the same factor), and rescaling becomes rare.
+        if (__builtin_expect(__any(top > m + 8.0f), 0)) {
+            const float to = fmaxf(m, top);
+            const float f = exp2_fast(m - to);
+            m = to;
+            l *= f;
+#pragma unroll
+            for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[i][r] *= f;
+        }
+        // The weights are rounded to the type of the values, as the matrix cores take them; their sum is not.
+        const int ti = lane & 15;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int cc = 0; cc < 2; ++cc) {
+                w4 p;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float x = exp2_fast(__builtin_fmaf(z[kb][8 * cc + 2 * j], a.scale_log2, -m));
+                    const float y = exp2_fast(__builtin_fmaf(z[kb][8 * cc + 2 * j + 1], a.scale_log2, -m));
+                    l += x;
+                    l += y;
+                    p[j] = T::pack(x, y);
+                }
+                const int r = kb * 32 + cc * 16 + 4 * half + ti / 4;
+#pragma unroll
+                for (int db = 0; db < DP / 32; ++db) {
+                    const int piece = db * 4 + 2 * (lane >> 4 & 1) + (ti % 4) / 2;
+                    const int at = (piece ^ (DP >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2)) * 8 + (ti & 1) * 4;
+                    const w2 x = read_down(&vs[r * DP + at]), y = read_down(&vs[(r + 8) * DP + at]);
+                    o[db] = T::mma32(w4{x[0], x[1], y[0], y[1]}, p, o[db]);
+                }
+            }
+    };
+
+    uint64_t seen_next = 0;
+    int32_t slot = -1;
+    if (tiles_n) {
+        const int32_t slot0 = slot_at(0);
+        slot = slot_at(1);
+        seen_next = load_tile(0, slot0);
+        store_tile(lds_k[0], lds_v[0], seen_next);
+    }
+    loads_arrived();
+    auto iteration = [&](int32_t t, auto buffer) __attribute__((always_inline)) {
+        constexpr int buf = decltype(buffer)::value;
+        const uint64_t seen = seen_next;
+        if (t + 1 < tiles_n) {
+            seen_next = load_tile(t + 1, slot);
+            slot = slot_at(t + 2);
+        }
+        __syncthreads();                            // tile t is in LDS; everyone has left tile t - 1
+        const int32_t k0 = keys.begin + t * TK;
+        if (k0 <= wave_last && k0 + (TK - 1) >= wave_low) compute(lds_k[buf], lds_v[buf], k0, seen);
+        if (t + 1 < tiles_n) store_tile(lds_k[buf ^ 1], lds_v[buf ^ 1], seen_next);
+    };
+    for (int32_t t = 0; t < tiles_n; t += 2) {
+        iteration(t, std::integral_constant<int, 0>());
+        if (t + 1 < tiles_n) iteration(t + 1, std::integral_constant<int, 1>());
     }
 
     if (!wave_live) return;
+    const bool live = wave_row + col < rows_here;
     l += other_half(l);
     const uint64_t out_row = (uint64_t)(s.q_begin + token);
     if (a.splits == 1) {
@@ -262,11 +276,9 @@ __global__ __launch_bounds__(NW * 64, DP > 128 ? 1 : 2) void attention_rows(cons
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const uint32_t at = db * 32 + 8 * j + 4 * half;
-                if (at < c.head_dim) {
-                    const w2 w = {T::pack(o[db][4 * j] * e.scale_o, o[db][4 * j + 1] * e.scale_o),
-                                  T::pack(o[db][4 * j + 2] * e.scale_o, o[db][4 * j + 3] * e.scale_o)};
-                    *(w2 *)(p + at) = w;
-                }
+                if (at < c.head_dim)
+                    *(w2 *)(p + at) = w2{T::pack(o[db][4 * j] * e.scale_o, o[db][4 * j + 1] * e.scale_o),
+                                         T::pack(o[db][4 * j + 2] * e.scale_o, o[db][4 * j + 3] * e.scale_o)};
             }
         if (a.lse && half == 0) a.lse[(uint64_t)head * c.total_q + out_row] = e.lse;
     } else if (live) {
@@ -762,7 +774,12 @@ template <class T, int DP>
 struct Rows {
     static hipError_t go(const AttentionArgs &a, hipStream_t stream)
     {
-        attention_rows<T, DP, kTileRows / 32><<<a.tiles * a.splits * a.c.kv_heads, kTileRows * 2, 0, stream>>>(a);
+        const uint32_t grid = a.tiles * a.splits * a.c.kv_heads;
+        const uint64_t bytes = (uint64_t)a.c.num_slots * a.c.kv_heads * a.c.block * a.c.head_dim * 2;
+        if (bytes <= 0xFFFFFFFFull)
+            attention_rows<T, DP, uint32_t><<<grid, kRowWaves * 64, 0, stream>>>(a);
+        else
+            attention_rows<T, DP, uint64_t><<<grid, kRowWaves * 64, 0, stream>>>(a);
         return hipGetLastError();
     }
 };
@@ -798,9 +815,9 @@ struct Mass {
 
 }  // namespace
 
-hipError_t launch_attention(const AttentionArgs &a, uint32_t dtype, bool few_rows, hipStream_t stream)
+hipError_t launch_attention(const AttentionArgs &a, uint32_t dtype, hipStream_t stream)
 {
-    return few_rows ? by_type<Few>(dtype, a.c.head_dim, a, stream) : by_type<Rows>(dtype, a.c.head_dim, a, stream);
+    return a.few_rows ? by_type<Few>(dtype, a.c.head_dim, a, stream) : by_type<Rows>(dtype, a.c.head_dim, a, stream);
 }
 
 hipError_t launch_attention_join(const AttentionArgs &a, uint32_t dtype, hipStream_t stream)

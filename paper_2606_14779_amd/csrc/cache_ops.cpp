@@ -103,20 +103,20 @@ struct Cut {
 Cut cut_of(const CacheView &c, uint32_t window)
 {
     Cut p{};
-    p.few = (uint64_t)c.max_q * c.group <= kFewRows;
     const uint64_t rows = (uint64_t)c.total_q * c.group;
-    p.tiles = p.few ? c.n_seq : (uint32_t)(rows / kTileRows + c.n_seq);
-    const uint64_t tile_tokens = p.few ? c.max_q : std::min<uint64_t>(c.max_q, kTileRows / c.group + 2);
+    const bool few = p.few = (uint64_t)c.max_q * c.group <= kFewRows;
+    p.tiles = few ? c.n_seq : (uint32_t)(rows / kTileRows + c.n_seq);
+    const uint64_t tile_tokens = few ? c.max_q : std::min<uint64_t>(c.max_q, kTileRows / c.group + 2);
     uint64_t span = c.max_kv;
     if (window) span = std::min<uint64_t>(span, (uint64_t)window + tile_tokens + kTileKeys);
     // workgroups that have work if all sequences are alike
-    const uint64_t units = std::max<uint64_t>(1, (p.few ? c.n_seq : (rows + kTileRows - 1) / kTileRows) * c.kv_heads);
-    const uint64_t fill = p.few ? 4096 : 2048;       // workgroups wanted
-    const uint64_t least = p.few ? 128 : 512;        // keys of a part
+    const uint64_t units = std::max<uint64_t>(1, (few ? c.n_seq : (rows + kTileRows - 1) / kTileRows) * c.kv_heads);
+    const uint64_t fill = few ? 4096 : 2048;       // workgroups wanted
+    const uint64_t least = few ? 128 : 512;        // keys of a part
     uint64_t splits = (fill + units / 2) / units;
     splits = std::max<uint64_t>(1, std::min(splits, span / least));
     uint64_t keys = (span + splits - 1) / splits;
-    const uint64_t unit = p.few ? 128 : kTileKeys;
+    const uint64_t unit = few ? 128 : kTileKeys;
     keys = std::max(unit, (keys + unit - 1) / unit * unit);
     p.splits = (uint32_t)std::max<uint64_t>(1, (span + keys - 1) / keys);
     p.split_keys = (uint32_t)keys;
@@ -171,6 +171,7 @@ void op_attention(const kvp_cache_shape *s, const kvp_batch *b, const void *q, u
     a.sinks = sinks;
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     a.window = window;
+    a.few_rows = p.few;
     a.tiles = p.tiles;
     a.splits = p.splits;
     a.split_keys = p.split_keys;
@@ -178,7 +179,7 @@ void op_attention(const kvp_cache_shape *s, const kvp_batch *b, const void *q, u
     a.part_o = static_cast<float *>(workspace);
     a.part_ml = a.part_o ? a.part_o + parts * a.c.head_dim : nullptr;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    check_hip(launch_attention(a, s->dtype, p.few, st), "attention launch");
+    check_hip(launch_attention(a, s->dtype, st), "attention launch");
     if (p.splits > 1) check_hip(launch_attention_join(a, s->dtype, st), "attention join launch");
 }
 

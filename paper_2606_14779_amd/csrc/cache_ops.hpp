@@ -30,6 +30,7 @@ struct AttentionArgs {
     const float *sinks;              // [heads] or null
     float scale_log2;                // scale * log2(e)
     uint32_t window;                 // 0: none
+    uint32_t few_rows;               // attention_few, else attention_rows
     uint32_t tiles, splits, split_keys;
     float *part_o;                   // [splits][total_q * heads][head_dim]
     float *part_ml;                  // [splits][total_q * heads][2]
@@ -80,7 +81,7 @@ struct EvictArgs {
 };
 
 // Each launcher enqueues on `stream` of the current device.
-hipError_t launch_attention(const AttentionArgs &a, uint32_t dtype, bool few_rows, hipStream_t stream);
+hipError_t launch_attention(const AttentionArgs &a, uint32_t dtype, hipStream_t stream);
 hipError_t launch_attention_join(const AttentionArgs &a, uint32_t dtype, hipStream_t stream);
 hipError_t launch_mass(const MassArgs &a, uint32_t dtype, hipStream_t stream);
 hipError_t launch_rope(const RopeArgs &a, uint32_t dtype, hipStream_t stream);

@@ -89,6 +89,13 @@ __device__ __forceinline__ float other_half(float x)
     return __builtin_bit_cast(float, (uint32_t)(threadIdx.x & 32 ? p[0] : p[1]));
 }
 
+// Another lane's value.
+__device__ __forceinline__ uint32_t lane_value(uint32_t x, int lane) { return __shfl(x, lane); }
+__device__ __forceinline__ uint64_t lane_value(uint64_t x, int lane)
+{
+    return (uint64_t)(uint32_t)__shfl((uint32_t)(x >> 32), lane) << 32 | (uint32_t)__shfl((uint32_t)x, lane);
+}
+
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 constexpr float kLowest = -3.0e38f;        // start of a running maximum: finite, so that -inf minus it is -inf
