@@ -13,7 +13,7 @@
 // the order of the keys inside a product is free, and V's transposed LDS reads follow the order that the
 // first product left.
 //
-// attention_rows: 32 rows to a wave, kTileRows to a workgroup, kTileKeys keys at a time through LDS.
+// attention_rows: 32 rows to a wave, 256 to a workgroup, kTileKeys keys at a time through LDS.
 // attention_few: up to 16 rows (single tokens and very short chunks), where reading the cache is all that
 // counts: the waves of a workgroup split the keys, and a join in LDS ends the workgroup.
 // Where there are few row tiles both split the keys over workgroups as well; attention_join adds the parts.
@@ -64,21 +64,26 @@ __device__ __forceinline__ Split keys_of(const AttentionArgs &a, const Seq &s, i
 
 // ---- many rows
 
-constexpr int kRowWaves = kTileRows / 32;
-
-// 32 rows to a wave.  The vector unit, not the matrix cores, bounds this kernel: a tile of 64 keys at head_dim 128 is
-// 32 products of 32 cycles, and beside them about 140 vector instructions for the softmax alone (a maximum, a scaled
-// difference, an exponential, a sum and half a rounding per logit).  So the rest is kept off the vector unit: 32-bit
-// offsets from scalar bases where a buffer has less than 2^32 bytes (Offset), buffers of LDS known at compile time
-// (the loop is written for two tiles), masks and zeros only in the tiles that need them.
+// 32 rows to a wave, two waves to a SIMD that work in turns: while one feeds the matrix cores (the products of tile
+// t with K and of tile t - 1 with V), the other's vector unit turns its logits into weights; a barrier ends each
+// stage.  A tile of 64 keys at head_dim 128 is 32 products of 32 cycles, and beside them about 140 vector
+// instructions for the softmax alone (a maximum, a scaled difference, an exponential, a sum and half a rounding per
+// logit), so the rest is kept off the vector unit: 32-bit offsets from scalar bases where a buffer has less than
+// 2^32 bytes (Offset), buffers of LDS known at compile time (the loop is written for two tiles), masks and zeros
+// only in the tiles that need them.
+//
+// Stages: the first half of the waves has products(t) in stage 2t and softmax(t) in 2t + 1, the second half one
+// stage later.  What the products of stage 2t read, K(t) and V(t - 1), is stored by the first half in stage 2t - 1
+// and by the second in 2t - 2; the buffers' last readers are done at the end of stage 2t - 3.
 template <class T, int DP, class Offset>
-__global__ __launch_bounds__(kRowWaves * 64, DP > 128 ? 1 : 2) void attention_rows(const AttentionArgs a)
+__global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attention_rows(const AttentionArgs a)
 {
-    constexpr int TK = kTileKeys, NW = kRowWaves, TR = kTileRows;
+    constexpr int TK = kTileKeys, NW = row_waves(DP), TR = NW * 32;
     constexpr int CH = DP / 8;                       // 16-byte pieces of a row
     constexpr int PASS = NW * 64 / CH;               // rows that the workgroup loads at once
     constexpr int N = TK / PASS;
-    __shared__ __align__(16) uint16_t lds_k[2][TK * DP], lds_v[2][TK * DP];
+    constexpr uint32_t BUF = TK * DP * 2;            // bytes of a tile: buffers K0, K1, V0, V1
+    __shared__ __align__(16) char lds[4 * BUF];
 
     const CacheView &c = a.c;
     const uint32_t kv_head = blockIdx.x % c.kv_heads;
@@ -96,6 +101,7 @@ __global__ __launch_bounds__(kRowWaves * 64, DP > 128 ? 1 : 2) void attention_ro
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
+    const bool second = wave >= NW / 2;
     const uint32_t wave_row = wave * 32;
     const bool wave_live = wave_row < rows_here;
     const int32_t shift = s.kv - s.n_q;
@@ -107,10 +113,9 @@ __global__ __launch_bounds__(kRowWaves * 64, DP > 128 ? 1 : 2) void attention_ro
 
     const Split keys = keys_of(a, s, (int32_t)token_of(c, row0), (int32_t)token_of(c, row0 + rows_here - 1), split);
     const int32_t tiles_n = keys.end > keys.begin ? (keys.end - keys.begin + TK - 1) / TK : 0;
-    // what the wave's rows see: keys of [wave_low, wave_last], all of them those of [wave_full, wave_first]
+    // all of the wave's rows see the keys of [wave_full, wave_first]
     const int32_t wave_first = shift + (int32_t)token_of(c, row0 + min(wave_row, rows_here - 1));
     const int32_t wave_last = wave_live ? shift + (int32_t)token_of(c, row0 + min(wave_row + 31, rows_here - 1)) : -1;
-    const int32_t wave_low = a.window ? (int32_t)max((int64_t)wave_first + 1 - (int64_t)a.window, (int64_t)0) : 0;
     const int32_t wave_full = a.window ? (int32_t)max((int64_t)wave_last + 1 - (int64_t)a.window, (int64_t)0) : 0;
 
     w4 q[DP / 16];
@@ -123,9 +128,12 @@ __global__ __launch_bounds__(kRowWaves * 64, DP > 128 ? 1 : 2) void attention_ro
             if (c.head_dim != DP && at >= c.head_dim) q[i] = w4{0, 0, 0, 0};
         }
     }
-    v16f o[DP / 32];
+    v16f o[DP / 32], z[2];
+    w4 p[4];                                         // weights of 16 keys each
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i) o[i] = v16f{};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = w4{0, 0, 0, 0};
     float m = kLowest, l = 0.0f;
 
     // loading: thread -> row load_row + i * PASS of a tile, piece load_piece
@@ -135,52 +143,77 @@ __global__ __launch_bounds__(kRowWaves * 64, DP > 128 ? 1 : 2) void attention_ro
     const int32_t *table = c.table + (uint64_t)seq * c.table_stride;
     w4 rk[N], rv[N];
 
-    auto slot_at = [&](int32_t t) __attribute__((always_inline)) {                 // table entry of this lane's key of tile t
+    auto slot_at = [&](int32_t t) __attribute__((always_inline)) {   // table entry of this lane's key of tile t
         return load4g(table + block_of(c, min(keys.begin + t * TK + lane, keys.end - 1)));
     };
-    // Starts the loads of tile t from its table entries; returns which of its keys are there.
-    auto load_tile = [&](int32_t t, int32_t slot) __attribute__((always_inline)) {
+    auto row_at = [&](int32_t t, int32_t slot) __attribute__((always_inline)) {
         const int32_t key = keys.begin + t * TK + lane;
-        const uint32_t r = row_of(c, key < keys.end ? slot : -1, kv_head, key);
-        const Offset at = (Offset)(r == kNoRow ? 0 : r) * (c.head_dim * 2);   // not there: a row that is
+        return row_of(c, key < keys.end ? slot : -1, kv_head, key);
+    };
+    auto offset_of = [&](uint32_t r) __attribute__((always_inline)) {
+        return (Offset)(r == kNoRow ? 0 : r) * (c.head_dim * 2);     // not there: a row that is
+    };
+    auto load = [&](const uint16_t *cache, Offset at, w4 (&to)[N]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const Offset from = lane_value(at, load_row + i * PASS) + piece_at;
-            rk[i] = load16g((const uint16_t *)((const char *)a.k + from));
-            rv[i] = load16g((const uint16_t *)((const char *)a.v + from));
-        }
-        return __ballot(r != kNoRow);
+        for (int i = 0; i < N; ++i)
+            to[i] = load16g((const uint16_t *)((const char *)cache + (lane_value(at, load_row + i * PASS) + piece_at)));
     };
     // Rows of 64 elements lie two to 64 banks of LDS, longer ones fill them: the pieces of a row change places with
-    // its number, so that 16 rows read at one place of K, and four at four places of V, meet different banks.
-    auto store_tile = [&](uint16_t *ks, uint16_t *vs, uint64_t seen) __attribute__((always_inline)) {
+    // its number, so that 16 rows read at one place of K, and four at four places of V, meet different banks.  PASS
+    // and the steps between the rows that a lane reads leave the number's low bits as they are: one place to a lane.
+    auto k_place = [&](int r) __attribute__((always_inline)) { return DP >= 128 ? r & (PASS >= 16 ? 15 : 7) : (r >> 1) & 7; };
+    auto v_place = [&](int r) __attribute__((always_inline)) { return DP >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2; };
+    const uint32_t k_store = load_row * DP * 2 + (load_piece ^ k_place(load_row)) * 16;
+    const uint32_t v_store = load_row * DP * 2 + (load_piece ^ v_place(load_row)) * 16;
+    uint32_t k_read[DP / 16], v_read[DP / 32];
+    {
+        const int ti = lane & 15, r = 4 * half + ti / 4;
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) k_read[i] = col * DP * 2 + ((2 * i + half) ^ k_place(col)) * 16;
+#pragma unroll
+        for (int i = 0; i < DP / 32; ++i)
+            v_read[i] = r * DP * 2 + ((4 * i + 2 * (lane >> 4 & 1) + (ti % 4) / 2) ^ v_place(r)) * 16 + (ti & 1) * 8;
+    }
+    auto store_k = [&](uint32_t buffer) __attribute__((always_inline)) {
+        if (__builtin_expect(c.head_dim != DP, 0) && !piece_live) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) rk[i] = w4{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) *(w4 *)(lds + (k_store + buffer) + i * PASS * DP * 2) = rk[i];
+    };
+    auto store_v = [&](uint32_t buffer, uint64_t seen) __attribute__((always_inline)) {
         if (__builtin_expect(c.head_dim != DP || seen != ~0ull, 0)) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                if (!piece_live) rk[i] = w4{0, 0, 0, 0};
-                // what is not there must be finite in V: its weight is 0
+            for (int i = 0; i < N; ++i)              // what is not there must be finite: its weight is 0
                 if (!piece_live || !(seen >> (load_row + i * PASS) & 1)) rv[i] = w4{0, 0, 0, 0};
-            }
         }
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int r = load_row + i * PASS;
-            *(w4 *)&ks[r * DP + (load_piece ^ (DP >= 128 ? r & 15 : (r >> 1) & 7)) * 8] = rk[i];
-            *(w4 *)&vs[r * DP + (load_piece ^ (DP >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2)) * 8] = rv[i];
-        }
+        for (int i = 0; i < N; ++i) *(w4 *)(lds + (v_store + buffer) + i * PASS * DP * 2) = rv[i];
     };
-    auto compute = [&](const uint16_t *ks, const uint16_t *vs, int32_t k0, uint64_t seen) __attribute__((always_inline)) {
-        v16f z[2];
+
+    auto product_k = [&](uint32_t buffer, int j) __attribute__((always_inline)) {
+        const w4 k = *(const w4 *)(lds + k_read[j / 2] + (buffer + (j & 1) * 32 * DP * 2));
+        z[j & 1] = T::mma32(k, q[j / 2], j < 2 ? v16f{} : z[j & 1]);
+    };
+    auto product_v = [&](uint32_t buffer, int j) __attribute__((always_inline)) {
+        const int db = j % (DP / 32), i = j / (DP / 32);
+        const char *v = lds + v_read[db] + (buffer + i * 16 * DP * 2);
+        const w2 x = read_down((const uint16_t *)v), y = read_down((const uint16_t *)(v + 8 * DP * 2));
+        o[db] = T::mma32(w4{x[0], x[1], y[0], y[1]}, p[i], o[db]);
+    };
+    // V(t - 1) and K(t): always both, so that the registers of o stay where they are.  Weights that are not there are
+    // 0, and logits that are not there are not looked at.
+    auto products = [&](uint32_t ks, uint32_t vs) __attribute__((always_inline)) {
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            z[kb] = v16f{};
-            const int r = kb * 32 + col;
+        for (int j = 0; j < DP / 8; ++j) product_v(vs, j);
 #pragma unroll
-            for (int i = 0; i < DP / 16; ++i) {
-                const int piece = (2 * i + half) ^ (DP >= 128 ? r & 15 : (r >> 1) & 7);
-                z[kb] = T::mma32(*(const w4 *)&ks[r * DP + piece * 8], q[i], z[kb]);
-            }
-        }
+        for (int j = 0; j < DP / 8; ++j) product_k(ks, j);
+        __builtin_amdgcn_s_setprio(0);
+    };
+    auto softmax = [&](int32_t t, uint64_t seen) __attribute__((always_inline)) {
+        const int32_t k0 = keys.begin + t * TK;
         if (__builtin_expect(!(k0 + TK - 1 <= wave_first && k0 >= wave_full && seen == ~0ull), 0)) {
             const uint64_t mine = seen >> (4 * half);
 #pragma unroll
@@ -212,55 +245,71 @@ __global__ __launch_bounds__(kRowWaves * 64, DP > 128 ? 1 : 2) void attention_ro
                 for (int r = 0; r < 16; ++r) o[i][r] *= f;
         }
         // The weights are rounded to the type of the values, as the matrix cores take them; their sum is not.
-        const int ti = lane & 15;
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int cc = 0; cc < 2; ++cc) {
-                w4 p;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float x = exp2_fast(__builtin_fmaf(z[kb][8 * cc + 2 * j], a.scale_log2, -m));
-                    const float y = exp2_fast(__builtin_fmaf(z[kb][8 * cc + 2 * j + 1], a.scale_log2, -m));
-                    l += x;
-                    l += y;
-                    p[j] = T::pack(x, y);
-                }
-                const int r = kb * 32 + cc * 16 + 4 * half + ti / 4;
-#pragma unroll
-                for (int db = 0; db < DP / 32; ++db) {
-                    const int piece = db * 4 + 2 * (lane >> 4 & 1) + (ti % 4) / 2;
-                    const int at = (piece ^ (DP >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2)) * 8 + (ti & 1) * 4;
-                    const w2 x = read_down(&vs[r * DP + at]), y = read_down(&vs[(r + 8) * DP + at]);
-                    o[db] = T::mma32(w4{x[0], x[1], y[0], y[1]}, p, o[db]);
-                }
+            for (int j = 0; j < 4; ++j) {
+                const int r = 8 * (i & 1) + 2 * j;
+                const float x = exp2_fast(__builtin_fmaf(z[i / 2][r], a.scale_log2, -m));
+                const float y = exp2_fast(__builtin_fmaf(z[i / 2][r + 1], a.scale_log2, -m));
+                l += x;
+                l += y;
+                p[i][j] = T::pack(x, y);
             }
     };
 
-    uint64_t seen_next = 0;
-    int32_t slot = -1;
     if (tiles_n) {
-        const int32_t slot0 = slot_at(0);
-        slot = slot_at(1);
-        seen_next = load_tile(0, slot0);
-        store_tile(lds_k[0], lds_v[0], seen_next);
-    }
-    loads_arrived();
-    auto iteration = [&](int32_t t, auto buffer) __attribute__((always_inline)) {
-        constexpr int buf = decltype(buffer)::value;
-        const uint64_t seen = seen_next;
-        if (t + 1 < tiles_n) {
-            seen_next = load_tile(t + 1, slot);
-            slot = slot_at(t + 2);
+        // which keys of tiles t to t + 2 are there; the first half of the waves does not use the last
+        uint64_t seen0, seen1, seen2 = 0;
+        uint32_t r0 = row_at(0, slot_at(0)), r1 = row_at(1, slot_at(1));
+        int32_t slot = slot_at(2);
+        seen0 = __ballot(r0 != kNoRow);
+        seen1 = __ballot(r1 != kNoRow);
+        Offset at_v = offset_of(r0), at_k = offset_of(r1);
+        load(a.k, at_v, rk);
+        load(a.v, at_v, rv);
+        store_k(0);
+#pragma unroll
+        for (int i = 0; i < N; ++i) *(w4 *)(lds + (v_store + 3 * BUF) + i * PASS * DP * 2) = w4{0, 0, 0, 0};   // "V(-1)"
+        load(a.k, at_k, rk);
+        int32_t next = 2;                            // tile of the next K to load; slot is its table entry
+        // stores the pair that was loaded to the buffers of parity odd and starts the next one's loads
+        auto pass_on = [&](bool odd, uint64_t seen) __attribute__((always_inline)) {
+            const uint32_t r = row_at(next, slot);   // before the loads: so that it does not wait for them
+            at_v = at_k;
+            at_k = offset_of(r);
+            store_v(odd ? 3 * BUF : 2 * BUF, seen);
+            store_k(odd ? 0 : BUF);
+            load(a.v, at_v, rv);                     // past the last tile: some row
+            load(a.k, at_k, rk);
+            ++next;
+            slot = slot_at(next);
+            return __ballot(r != kNoRow);
+        };
+        if (second) seen2 = pass_on(false, seen0);
+        __syncthreads();
+        if (second) __syncthreads();
+        auto iteration = [&](int32_t t, auto buffer) __attribute__((always_inline)) {
+            constexpr int buf = decltype(buffer)::value;
+            products(buf * BUF, (3 - buf) * BUF);
+            __syncthreads();
+            softmax(t, seen0);
+            const uint64_t after = pass_on(second != (buf == 1), second ? seen1 : seen0);
+            seen0 = seen1;
+            seen1 = second ? seen2 : after;
+            seen2 = after;
+            __syncthreads();
+        };
+        for (int32_t t = 0;; t += 2) {
+            iteration(t, std::integral_constant<int, 0>());
+            if (t + 1 >= tiles_n) break;
+            iteration(t + 1, std::integral_constant<int, 1>());
+            if (t + 2 >= tiles_n) break;
         }
-        __syncthreads();                            // tile t is in LDS; everyone has left tile t - 1
-        const int32_t k0 = keys.begin + t * TK;
-        if (k0 <= wave_last && k0 + (TK - 1) >= wave_low) compute(lds_k[buf], lds_v[buf], k0, seen);
-        if (t + 1 < tiles_n) store_tile(lds_k[buf ^ 1], lds_v[buf ^ 1], seen_next);
-    };
-    for (int32_t t = 0; t < tiles_n; t += 2) {
-        iteration(t, std::integral_constant<int, 0>());
-        if (t + 1 < tiles_n) iteration(t + 1, std::integral_constant<int, 1>());
+        const uint32_t last = tiles_n & 1 ? 2 * BUF : 3 * BUF;
+#pragma unroll
+        for (int j = 0; j < DP / 8; ++j) product_v(last, j);
+        if (!second) __syncthreads();                // the second half's last stage
     }
 
     if (!wave_live) return;
@@ -777,9 +826,9 @@ struct Rows {
         const uint32_t grid = a.tiles * a.splits * a.c.kv_heads;
         const uint64_t bytes = (uint64_t)a.c.num_slots * a.c.kv_heads * a.c.block * a.c.head_dim * 2;
         if (bytes <= 0xFFFFFFFFull)
-            attention_rows<T, DP, uint32_t><<<grid, kRowWaves * 64, 0, stream>>>(a);
+            attention_rows<T, DP, uint32_t><<<grid, row_waves(DP) * 64, 0, stream>>>(a);
         else
-            attention_rows<T, DP, uint64_t><<<grid, kRowWaves * 64, 0, stream>>>(a);
+            attention_rows<T, DP, uint64_t><<<grid, row_waves(DP) * 64, 0, stream>>>(a);
         return hipGetLastError();
     }
 };

@@ -98,22 +98,24 @@ struct Cut {
 };
 
 // How an attention call is cut.  A KV head's rows (new tokens x group) go to attention_few if no sequence has
-// more than a 16-row product holds, else to tiles of kTileRows.  Where the tiles do not fill the chip, the keys
+// more than a 16-row product holds, else to tiles of 256 (128 at a head_dim of more than 128).  Where the tiles do not fill the chip, the keys
 // are split, as far as a part still holds enough keys to be worth its output's way through memory.
 Cut cut_of(const CacheView &c, uint32_t window)
 {
     Cut p{};
     const uint64_t rows = (uint64_t)c.total_q * c.group;
+    const uint32_t tile_rows = row_waves(c.head_dim) * 32;
     const bool few = p.few = (uint64_t)c.max_q * c.group <= kFewRows;
-    p.tiles = few ? c.n_seq : (uint32_t)(rows / kTileRows + c.n_seq);
-    const uint64_t tile_tokens = few ? c.max_q : std::min<uint64_t>(c.max_q, kTileRows / c.group + 2);
+    p.tiles = few ? c.n_seq : (uint32_t)(rows / tile_rows + c.n_seq);
+    const uint64_t tile_tokens = few ? c.max_q : std::min<uint64_t>(c.max_q, tile_rows / c.group + 2);
     uint64_t span = c.max_kv;
     if (window) span = std::min<uint64_t>(span, (uint64_t)window + tile_tokens + kTileKeys);
     // workgroups that have work if all sequences are alike
-    const uint64_t units = std::max<uint64_t>(1, (few ? c.n_seq : (rows + kTileRows - 1) / kTileRows) * c.kv_heads);
-    const uint64_t fill = few ? 4096 : 2048;       // workgroups wanted
-    const uint64_t least = few ? 128 : 512;        // keys of a part
-    uint64_t splits = (fill + units / 2) / units;
+    const uint64_t units = std::max<uint64_t>(1, (few ? c.n_seq : (rows + tile_rows - 1) / tile_rows) * c.kv_heads);
+    const uint64_t fill = few ? 4096 : 1024;         // workgroups wanted
+    const uint64_t least = few ? 128 : 512;          // keys of a part
+    // parts are written and read again: not where every CU has two tiles anyway
+    uint64_t splits = !few && units >= 512 ? 1 : (fill + units / 2) / units;
     splits = std::max<uint64_t>(1, std::min(splits, span / least));
     uint64_t keys = (span + splits - 1) / splits;
     const uint64_t unit = few ? 128 : kTileKeys;

@@ -90,7 +90,8 @@ hipError_t launch_evict(const EvictArgs &a, hipStream_t stream);
 
 // Rows (new tokens times the heads of a KV head) and keys of the attention kernels' tiles.
 constexpr uint32_t kFewRows = 16;
-constexpr uint32_t kTileRows = 128;
+// 32 rows to a wave, two waves to a SIMD; at a head_dim of more than 128 the registers hold one.
+constexpr int row_waves(uint32_t head_dim) { return head_dim > 128 ? 4 : 8; }
 constexpr uint32_t kTileKeys = 64;
 
 }  // namespace kvp
