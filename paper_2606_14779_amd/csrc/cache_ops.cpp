@@ -129,8 +129,13 @@ Cut cut_of(const CacheView &c, uint32_t window)
 // Largest workspace over all windows: a window only shortens the span, and with it the number of parts.
 uint64_t attention_bytes(const CacheView &c) { return cut_of(c, 0).bytes; }
 
-// Words of workspace to a list: two of counts, two per token (candidates, then moves), a bit per token.
-uint64_t evict_words(const CacheView &c) { return 2 + 2 * (uint64_t)c.max_kv + 2 * (((uint64_t)c.max_kv + 63) / 64); }
+// Words of workspace to a list: four of counts, two per token (candidates, then moves), a bit per token, and for
+// long lists the counts of 2^11 digits per part and of four waves' candidates.
+uint64_t evict_words(const CacheView &c)
+{
+    const uint64_t n = c.max_kv;
+    return 4 + 2 * n + 2 * ((n + 63) / 64) + (n > kEvictShort ? kEvictParts * (2048 + 4) : 0);
+}
 uint64_t evict_bytes(const CacheView &c) { return (uint64_t)c.n_seq * c.kv_heads * evict_words(c) * 4; }
 
 void need_scale(float scale) { need(std::isfinite(scale) && scale > 0, "scale is not a positive number"); }
@@ -243,13 +248,15 @@ void op_rope_append(const kvp_cache_shape *s, const kvp_batch *b, const float *a
         need_pointer(pos, 4, "pos");
         need(pos_stride >= a.c.max_kv, "pos_stride is less than max_kv");
     }
-    const uint64_t units = (uint64_t)((q ? a.c.heads : 0) + 2 * a.c.kv_heads) * (a.c.head_dim / 8);
-    need(a.c.total_q * units / 256 < 1u << 24, "too many new tokens for one call");
+    need(a.c.total_q < 1u << 24, "2^24 new tokens or more in one call");
     a.angles = angles;
     a.positions = positions;
     a.n_positions = n_positions;
     a.rot = rot;
     a.interleaved = flags & KVP_ROPE_INTERLEAVED ? 1 : 0;
+    // 16-byte pieces, or pairs of them where both of a pair are whole
+    a.per_head = a.c.head_dim / 8 - (!a.interleaved && rot % 16 == 0 ? rot / 16 : 0);
+    divide_by(a.per_head, &a.per_magic, &a.per_shift);
     a.q = static_cast<const uint16_t *>(q);
     a.k = static_cast<const uint16_t *>(k);
     a.v = static_cast<const uint16_t *>(v);

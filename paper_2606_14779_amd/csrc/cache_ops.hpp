@@ -51,6 +51,7 @@ struct RopeArgs {
     const float *angles;             // [n_positions][rot / 2][2]
     const int32_t *positions;
     uint32_t n_positions, rot, interleaved;
+    uint32_t per_head, per_magic, per_shift;   // units of a rotated head, and its division
     const uint16_t *q, *k, *v;
     uint16_t *q_out, *k_cache, *v_cache;
     uint64_t q_stride, q_out_stride, k_stride, v_stride;
@@ -93,6 +94,10 @@ constexpr uint32_t kFewRows = 16;
 // 32 rows to a wave, two waves to a SIMD; at a head_dim of more than 128 the registers hold one.
 constexpr int row_waves(uint32_t head_dim) { return head_dim > 128 ? 4 : 8; }
 constexpr uint32_t kTileKeys = 64;
+
+// Eviction: tokens that one workgroup holds in registers, and the workgroups that a longer list is spread over.
+constexpr uint32_t kEvictShort = 8192;
+constexpr uint32_t kEvictParts = 32;
 
 }  // namespace kvp
 
