@@ -62,6 +62,75 @@ __device__ __forceinline__ Split keys_of(const AttentionArgs &a, const Seq &s, i
     return {(int32_t)min(begin, (int64_t)max(hi, 0)), (int32_t)max(end, (int64_t)0)};
 }
 
+// Rows row0 .. row0 + count of a KV head, one to a wave at a time, without matrix products.
+//
+// A row must not meet the infinities and NaN of values that it does not see, but a weight of 0 times them is NaN,
+// and in a product every row meets every value of a tile.  So both kernels look at the values of the tiles that not
+// all of their rows see, and where one is not finite, what they computed is replaced by this.
+template <class T>
+__device__ __forceinline__ void rows_one_by_one(const AttentionArgs &a, const Seq &s, uint32_t seq, uint32_t kv_head,
+                                                uint32_t split, Split keys, uint32_t row0, uint32_t count)
+{
+    const CacheView &c = a.c;
+    const int lane = threadIdx.x & 63;
+    const int32_t *table = c.table + (uint64_t)seq * c.table_stride;
+    for (uint32_t i = threadIdx.x >> 6; i < count; i += blockDim.x >> 6) {
+        const uint32_t token = token_of(c, row0 + i), head = kv_head * c.group + row0 + i - token * c.group;
+        const int32_t limit = min(s.kv - s.n_q + (int32_t)token, s.kv - 1);
+        const int64_t floor_key = a.window ? (int64_t)limit + 1 - (int64_t)a.window : 0;
+        const uint64_t out_row = (uint64_t)(s.q_begin + (int32_t)token);
+        const uint16_t *q = a.q + out_row * a.q_stride + (uint64_t)head * c.head_dim;
+        float m = kLowest, l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};   // head_dim lane, lane + 64, ..
+        for (int32_t k0 = keys.begin; k0 < keys.end; k0 += 64) {
+            const int32_t key = k0 + lane;
+            const bool inside = key < keys.end && key <= limit && key >= floor_key;
+            const uint32_t r = inside ? row_of(c, load4g(table + block_of(c, key)), kv_head, key) : kNoRow;
+            const uint16_t *k = a.k + (uint64_t)(r == kNoRow ? 0 : r) * c.head_dim;
+            float z = 0.0f;
+            for (uint32_t d = 0; d < c.head_dim; d += 8) {
+                const w4 x = load16g(q + d), y = load16g(k + d);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) z += T::unpack(x[e / 2], e & 1) * T::unpack(y[e / 2], e & 1);
+            }
+            z = r == kNoRow ? -INFINITY : z * a.scale_log2;
+            float top = z;
+#pragma unroll
+            for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+            const float to = fmaxf(m, top), f = exp2_fast(m - to);
+            const float p = exp2_fast(z - to);
+            float sum = p;
+#pragma unroll
+            for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+            m = to;
+            l = l * f + sum;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] *= f;
+            for (uint64_t left = __ballot(r != kNoRow); left; left &= left - 1) {
+                const int j = __ffsll((unsigned long long)left) - 1;
+                const float weight = __shfl(p, j);
+                const uint16_t *v = a.v + (uint64_t)(uint32_t)__shfl(r, j) * c.head_dim;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (lane + 64u * e < c.head_dim) o[e] += weight * T::unpack(v[lane + 64 * e], 0);
+            }
+        }
+        if (a.splits == 1) {
+            const RowEnd end = finish_row(m, l, a.sinks, head);
+            uint16_t *p = a.out + out_row * a.out_stride + (uint64_t)head * c.head_dim;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (lane + 64u * e < c.head_dim) p[lane + 64 * e] = (uint16_t)T::pack(o[e] * end.scale_o, 0.0f);
+            if (a.lse && lane == 0) a.lse[(uint64_t)head * c.total_q + out_row] = end.lse;
+        } else {
+            const uint64_t part = (uint64_t)split * c.total_q * c.heads + out_row * c.heads + head;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (lane + 64u * e < c.head_dim) a.part_o[part * c.head_dim + lane + 64 * e] = o[e];
+            if (lane == 0) *(v2f *)(a.part_ml + 2 * part) = v2f{m, l};
+        }
+    }
+}
+
 // ---- many rows
 
 // 32 rows to a wave, two waves to a SIMD that work in turns: while one feeds the matrix cores (the products of tile
@@ -117,6 +186,12 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
     const int32_t wave_first = shift + (int32_t)token_of(c, row0 + min(wave_row, rows_here - 1));
     const int32_t wave_last = wave_live ? shift + (int32_t)token_of(c, row0 + min(wave_row + 31, rows_here - 1)) : -1;
     const int32_t wave_full = a.window ? (int32_t)max((int64_t)wave_last + 1 - (int64_t)a.window, (int64_t)0) : 0;
+
+    // and all of the workgroup's rows those of [all_full, all_first]
+    const int32_t all_first = shift + (int32_t)token_of(c, row0);
+    const int32_t all_last = shift + (int32_t)token_of(c, row0 + rows_here - 1);
+    const int32_t all_full = a.window ? (int32_t)max((int64_t)all_last + 1 - (int64_t)a.window, (int64_t)0) : 0;
+    bool bounded = true;                             // the values of tiles that not all rows see are finite
 
     w4 q[DP / 16];
     {
@@ -182,11 +257,16 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
 #pragma unroll
         for (int i = 0; i < N; ++i) *(w4 *)(lds + (k_store + buffer) + i * PASS * DP * 2) = rk[i];
     };
-    auto store_v = [&](uint32_t buffer, uint64_t seen) __attribute__((always_inline)) {
+    auto store_v = [&](int32_t t, uint32_t buffer, uint64_t seen) __attribute__((always_inline)) {
         if (__builtin_expect(c.head_dim != DP || seen != ~0ull, 0)) {
 #pragma unroll
             for (int i = 0; i < N; ++i)              // what is not there must be finite: its weight is 0
                 if (!piece_live || !(seen >> (load_row + i * PASS) & 1)) rv[i] = w4{0, 0, 0, 0};
+        }
+        const int32_t k0 = keys.begin + t * TK;
+        if (__builtin_expect(k0 + TK - 1 > all_first || k0 < all_full, 0)) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) bounded &= T::finite(rv[i]);
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) *(w4 *)(lds + (v_store + buffer) + i * PASS * DP * 2) = rv[i];
@@ -274,11 +354,11 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
         load(a.k, at_k, rk);
         int32_t next = 2;                            // tile of the next K to load; slot is its table entry
         // stores the pair that was loaded to the buffers of parity odd and starts the next one's loads
-        auto pass_on = [&](bool odd, uint64_t seen) __attribute__((always_inline)) {
+        auto pass_on = [&](int32_t t, bool odd, uint64_t seen) __attribute__((always_inline)) {   // t: V's tile
             const uint32_t r = row_at(next, slot);   // before the loads: so that it does not wait for them
             at_v = at_k;
             at_k = offset_of(r);
-            store_v(odd ? 3 * BUF : 2 * BUF, seen);
+            store_v(t, odd ? 3 * BUF : 2 * BUF, seen);
             store_k(odd ? 0 : BUF);
             load(a.v, at_v, rv);                     // past the last tile: some row
             load(a.k, at_k, rk);
@@ -286,7 +366,7 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
             slot = slot_at(next);
             return __ballot(r != kNoRow);
         };
-        if (second) seen2 = pass_on(false, seen0);
+        if (second) seen2 = pass_on(0, false, seen0);
         __syncthreads();
         if (second) __syncthreads();
         auto iteration = [&](int32_t t, auto buffer) __attribute__((always_inline)) {
@@ -294,7 +374,7 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
             products(buf * BUF, (3 - buf) * BUF);
             __syncthreads();
             softmax(t, seen0);
-            const uint64_t after = pass_on(second != (buf == 1), second ? seen1 : seen0);
+            const uint64_t after = pass_on(second ? t + 1 : t, second != (buf == 1), second ? seen1 : seen0);
             seen0 = seen1;
             seen1 = second ? seen2 : after;
             seen2 = after;
@@ -310,6 +390,10 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
 #pragma unroll
         for (int j = 0; j < DP / 8; ++j) product_v(last, j);
         if (!second) __syncthreads();                // the second half's last stage
+        if (__syncthreads_or(!bounded)) {
+            rows_one_by_one<T>(a, s, seq, kv_head, split, keys, row0, rows_here);
+            return;
+        }
     }
 
     if (!wave_live) return;
@@ -405,6 +489,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attention_few(const Attenti
     const int32_t mine = keys.begin + wave * TK;     // this wave's first keys; then every NW * TK
     const int32_t steps = keys.end > mine ? (keys.end - mine + NW * TK - 1) / (NW * TK) : 0;
 
+    bool bounded = true;                             // the values of tiles that not all rows see are finite
     w4 rk[2][KS], rv[N];
     uint32_t seen_next = 0;
     auto slot_at = [&](int32_t t) {
@@ -447,6 +532,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attention_few(const Attenti
     for (int32_t t = 0; t < steps; ++t) {
         const uint32_t seen = seen_next;
         const int32_t k0 = mine + t * (NW * TK);
+        const bool edge = !(k0 + TK - 1 <= all_first && (int64_t)k0 >= all_full);   // not all rows see these keys
         v4f z[2];
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
@@ -463,13 +549,15 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attention_few(const Attenti
             const int r = load_row + i * PASS;
             const bool there = piece_live && (seen >> r & 1);
             const int vp = load_piece ^ (DP >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2);
-            *(w4 *)&vs[r * DP + vp * 8] = there ? rv[i] : w4{0, 0, 0, 0};
+            const w4 v = there ? rv[i] : w4{0, 0, 0, 0};
+            if (__builtin_expect(edge, 0)) bounded &= T::finite(v);
+            *(w4 *)&vs[r * DP + vp * 8] = v;
         }
         if (t + 1 < steps) {
             seen_next = load_tile(t + 1, slot_next);
             slot_next = slot_at(t + 2);
         }
-        if (!(k0 + TK - 1 <= all_first && (int64_t)k0 >= all_full && seen == ~0u)) {
+        if (edge || seen != ~0u) {
             const uint32_t here = seen >> (4 * quad);
 #pragma unroll
             for (int b = 0; b < 2; ++b)
@@ -507,9 +595,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attention_few(const Attenti
         const w4 p = {T::pack(z[0][0], z[0][1]), T::pack(z[0][2], z[0][3]), T::pack(z[1][0], z[1][1]),
                       T::pack(z[1][2], z[1][3])};
         // the wave's own values: LDS keeps a wave's accesses in order
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        wave_lds_order();
         const int r = 4 * quad + col / 4;
 #pragma unroll
         for (int db = 0; db < DP / 16; ++db) {
@@ -518,9 +604,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attention_few(const Attenti
             const w2 x = read_down(&vs[r * DP + at]), y = read_down(&vs[(r + 16) * DP + at]);
             o[db] = T::mma16(w4{x[0], x[1], y[0], y[1]}, p, o[db]);
         }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        wave_lds_order();
     }
 
     // join the waves: scale each part to the common maximum, then add
@@ -530,7 +614,10 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attention_few(const Attenti
         lds_ml[wave][0][col] = m;
         lds_ml[wave][1][col] = l;
     }
-    __syncthreads();
+    if (__syncthreads_or(!bounded)) {
+        rows_one_by_one<T>(a, s, seq, kv_head, split, keys, 0, rows);
+        return;
+    }
     float top = lds_ml[0][0][col];
 #pragma unroll
     for (int w = 1; w < NW; ++w) top = fmaxf(top, lds_ml[w][0][col]);

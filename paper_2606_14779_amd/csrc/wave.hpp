@@ -27,6 +27,15 @@ typedef uint32_t w2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(1))) const w4 gw4;
 typedef __attribute__((address_space(1))) const int32_t gi32;
 
+// Whether eight 16-bit floats of this exponent are all finite.
+__device__ __forceinline__ bool finite_to(w4 x, uint32_t exponent)
+{
+    bool all = true;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) all &= (x[i] & exponent) != exponent && (x[i] >> 16 & exponent) != exponent;
+    return all;
+}
+
 struct BF16 {
     typedef __bf16 x8 __attribute__((ext_vector_type(8)));
     typedef __bf16 x2 __attribute__((ext_vector_type(2)));
@@ -47,6 +56,7 @@ struct BF16 {
     {
         return __builtin_bit_cast(float, i ? (w & 0xFFFF0000u) : (w << 16));
     }
+    static __device__ __forceinline__ bool finite(w4 x) { return finite_to(x, 0x7F80u); }
 };
 
 struct F16 {
@@ -69,10 +79,19 @@ struct F16 {
     {
         return (float)__builtin_bit_cast(x2, w)[i];
     }
+    static __device__ __forceinline__ bool finite(w4 x) { return finite_to(x, 0x7C00u); }
 };
 
 __device__ __forceinline__ w4 load16g(const uint16_t *p) { return *(gw4 *)p; }
 __device__ __forceinline__ int32_t load4g(const int32_t *p) { return *(gi32 *)p; }
+
+// Orders a wave's own accesses of LDS, which the hardware keeps in order, for the compiler.
+__device__ __forceinline__ void wave_lds_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 
 // Four 16-bit elements down a column: within 16 lanes, lane i names 4 elements of row i/4
 // (columns 4*(i%4)..+3 of a 4x16 tile) and receives column i of the tile's four rows.

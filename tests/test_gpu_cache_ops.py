@@ -516,3 +516,40 @@ def test_chain_in_a_graph_and_on_another_stream():
         if i == 0:
             for a, b in zip(streamed, want):
                 assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("window", [0, 40])
+@pytest.mark.parametrize("lens,heads,head_dim", [([(3, 200), (2, 9)], 8, 64), ([(4, 500)], 8, 128), ([(100, 333), (70, 70)], 8, 64),
+                                                 ([(300, 300)], 2, 128), ([(40, 90)], 4, 256), ([(3, 90)], 4, 200)])
+def test_attention_unseen_values_do_not_leak(lens, heads, head_dim, window, dtype):
+    """Infinities and NaN among keys and values of tokens that some queries see and others, in the same tile, do not:
+    the others are as without them, and those that see a value's element are not finite there."""
+    c = R.Case(lens, heads=heads, kv_heads=2, head_dim=head_dim, dtype=dtype, seed=60)
+    q = c.normal(c.total, heads, head_dim, std=2.0)
+    want, want_lse, tol, tol_lse = R.attention(c, q, 0.1, window)
+    marks = {}
+    for s, (new, kv) in enumerate(lens):
+        slot, off = c.places(s, kv)
+        for at, value in ((kv - 1, math.nan), (kv - 2, math.inf), (max(0, kv - new - 30), -math.inf), (kv - new, math.inf)):
+            marks.setdefault(s, []).append(at)
+            c.v_cache[slot[at], 1, off[at], 5] = value
+            c.v_cache[slot[at], 1, off[at], head_dim - 1] = value
+        c.k_cache[slot[kv - 1], 0, off[kv - 1], 3] = math.nan         # a key of the first KV head
+    out, lse = run_attention(c, q, 0.1, window)
+    group = heads // 2
+    for s, (new, kv) in enumerate(lens):
+        for i in range(new):
+            t, index = int(c.cu_host[s]) + i, kv - new + i
+            sees = [index >= at and (not window or at > index - window) for at in marks[s]]
+            ok = torch.ones(heads, head_dim, dtype=torch.bool, device="cuda")
+            if any(sees):
+                ok[group:, 5] = ok[group:, head_dim - 1] = False
+            if i == new - 1:
+                ok[:group] = False
+                assert torch.isnan(out[t, :group]).all() and torch.isnan(lse[:group, t]).all()
+            off = (out[t].double() - want[t]).abs()
+            assert (off <= tol[t])[ok].all(), (s, i)
+            assert not torch.isfinite(out[t])[group:][~ok[group:]].any()
+            heads_ok = slice(group if i == new - 1 else 0, heads)
+            assert ((lse[heads_ok, t].double() - want_lse[heads_ok, t]).abs() <= tol_lse[heads_ok, t]).all()
