@@ -431,13 +431,15 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
 
 // ---- up to 16 rows, the waves split the keys
 
-constexpr int kFewWaves = 4;
 constexpr int kFewKeys = 32;    // to a wave at a time
 
-template <class T, int DP>
-__global__ __launch_bounds__(kFewWaves * 64, 2) void attention_few(const AttentionArgs a)
+// Bound by reading the cache: 16 KB in flight to a wave (head_dim 128), each loaded as soon as its registers are free.
+// Short contexts are bound by what has to be known before the first key can be asked for, so the block table's
+// entries are asked for together with the sequence's length wherever they do not depend on it.
+template <class T, int DP, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void attention_few(const AttentionArgs a)
 {
-    constexpr int NW = kFewWaves, TK = kFewKeys;
+    constexpr int TK = kFewKeys;
     constexpr int CH = DP / 8;
     constexpr int PASS = 64 / CH;                    // rows that a wave loads at once
     constexpr int N = TK / PASS;
@@ -452,11 +454,18 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attention_few(const Attenti
     const uint32_t rest = blockIdx.x / c.kv_heads;
     const uint32_t split = rest % a.splits;
     const uint32_t seq = rest / a.splits;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int32_t *table = c.table + (uint64_t)seq * c.table_stride;
+    int32_t slot0 = -1, slot1 = -1;                  // table entries of this lane's first two keys
+    if (!a.window && c.max_kv) {
+        const int64_t key = (int64_t)split * a.split_keys + wave * TK + (lane & 31);
+        slot0 = load4g(table + block_of(c, (uint32_t)min(key, (int64_t)c.max_kv - 1)));
+        slot1 = load4g(table + block_of(c, (uint32_t)min(key + NW * TK, (int64_t)c.max_kv - 1)));
+    }
     const Seq s = load_seq(c, seq);
     const uint32_t rows = (uint32_t)s.n_q * c.group;   // at most 16
     if (!rows) return;
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int col = lane & 15, quad = lane >> 4;
     const uint32_t row = min((uint32_t)col, rows - 1);
     const int32_t token = (int32_t)(row / c.group);
@@ -485,7 +494,6 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attention_few(const Attenti
     const int load_piece = lane % CH, load_row = lane / CH;
     const bool piece_live = (uint32_t)load_piece * 8 < c.head_dim;
     const uint32_t piece_at = piece_live ? load_piece * 8 : 0;
-    const int32_t *table = c.table + (uint64_t)seq * c.table_stride;
     const int32_t mine = keys.begin + wave * TK;     // this wave's first keys; then every NW * TK
     const int32_t steps = keys.end > mine ? (keys.end - mine + NW * TK - 1) / (NW * TK) : 0;
 
@@ -522,10 +530,13 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attention_few(const Attenti
 
     int32_t slot_next = -1;
     if (steps) {
-        const int32_t slot = slot_at(0);
-        slot_next = slot_at(1);
+        if (a.window) {
+            slot0 = slot_at(0);
+            slot1 = slot_at(1);
+        }
+        slot_next = slot1;
         loads_arrived();
-        seen_next = load_tile(0, slot);
+        seen_next = load_tile(0, slot0);
     }
     uint16_t *vs = lds_v[wave];
 
@@ -656,8 +667,9 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attention_few(const Attenti
 }
 
 // Adds the parts of the rows.  A row is the work of `slices` times LANES neighbouring threads: a thread has 4
-// elements of head_dim and every slices-th part; the slices are added through LDS, always in the same order.
-template <class T, int LANES>
+// elements of head_dim and every slices-th part, U of them in flight; the slices are added through LDS, always in
+// the same order.
+template <class T, int LANES, int U>
 __global__ __launch_bounds__(256) void attention_join(const AttentionArgs a, const uint32_t slices)
 {
     constexpr int GROUPS = 256 / LANES;
@@ -672,7 +684,6 @@ __global__ __launch_bounds__(256) void attention_join(const AttentionArgs a, con
     // a part of a group's own threads at a time: its maximum and sum first, to rescale by
     float m = kLowest, l = 0.0f;
     v4f sum{};
-    constexpr int U = 4;                            // parts in flight
     for (uint32_t i0 = slice; i0 < a.splits; i0 += U * slices) {
         v2f ml[U];
         v4f o[U];
@@ -923,7 +934,14 @@ template <class T, int DP>
 struct Few {
     static hipError_t go(const AttentionArgs &a, hipStream_t stream)
     {
-        attention_few<T, DP><<<a.tiles * a.splits * a.c.kv_heads, kFewWaves * 64, 0, stream>>>(a);
+        const uint32_t grid = a.tiles * a.splits * a.c.kv_heads;
+        if constexpr (DP <= 128) {
+            if (a.splits == 1) {
+                attention_few<T, DP, 8><<<grid, 8 * 64, 0, stream>>>(a);
+                return hipGetLastError();
+            }
+        }
+        attention_few<T, DP, 4><<<grid, 4 * 64, 0, stream>>>(a);
         return hipGetLastError();
     }
 };
@@ -933,9 +951,12 @@ struct Join {
     {
         constexpr uint32_t groups = 256 / (DP / 4);
         uint32_t slices = 1;
-        while (slices < groups && slices * 2 <= a.splits) slices *= 2;
+        while (slices < groups && slices * 4 < a.splits) slices *= 2;
         const uint32_t per = groups / slices, rows = a.c.total_q * a.c.heads;
-        attention_join<T, DP / 4><<<(rows + per - 1) / per, 256, 0, stream>>>(a, slices);
+        if (a.splits <= 2)
+            attention_join<T, DP / 4, 2><<<(rows + per - 1) / per, 256, 0, stream>>>(a, slices);
+        else
+            attention_join<T, DP / 4, 4><<<(rows + per - 1) / per, 256, 0, stream>>>(a, slices);
         return hipGetLastError();
     }
 };

@@ -97,9 +97,9 @@ struct Cut {
     uint64_t bytes;   // of workspace
 };
 
-// How an attention call is cut.  A KV head's rows (new tokens x group) go to attention_few if no sequence has
-// more than a 16-row product holds, else to tiles of 256 (128 at a head_dim of more than 128).  Where the tiles do not fill the chip, the keys
-// are split, as far as a part still holds enough keys to be worth its output's way through memory.
+// How an attention call is cut.  A KV head's rows (new tokens x group) go to attention_few if no sequence has more
+// than a 16-row product holds, else to tiles of 256 (128 at a head_dim of more than 128).  Where the tiles do not
+// fill the chip, the keys are split, as far as a part holds enough keys to be worth its output's way through memory.
 Cut cut_of(const CacheView &c, uint32_t window)
 {
     Cut p{};
@@ -112,12 +112,27 @@ Cut cut_of(const CacheView &c, uint32_t window)
     if (window) span = std::min<uint64_t>(span, (uint64_t)window + tile_tokens + kTileKeys);
     // workgroups that have work if all sequences are alike
     const uint64_t units = std::max<uint64_t>(1, (few ? c.n_seq : (rows + tile_rows - 1) / tile_rows) * c.kv_heads);
-    const uint64_t fill = few ? 4096 : 1024;         // workgroups wanted
-    const uint64_t least = few ? 128 : 512;          // keys of a part
-    // parts are written and read again: not where every CU has two tiles anyway
-    uint64_t splits = !few && units >= 512 ? 1 : (fill + units / 2) / units;
-    splits = std::max<uint64_t>(1, std::min(splits, span / least));
-    uint64_t keys = (span + splits - 1) / splits;
+    uint64_t keys = span;                            // of a part
+    if (few) {
+        // about 1024 parts, which read the cache at its full rate, and not above 1024 keys where lengths may differ, so
+        // that none is left alone at the end.  32 sequences of up to 16K: 191 us at 1024 keys, 210 at 512, 223 at 4096;
+        // one of 128K: 47 us at 1024, 49 at 512, 67 at 128.  256 keys are one step of a workgroup and stay whole.
+        if (span > 256) {
+            keys = std::max<uint64_t>(128, units * span / 1024);
+            if (c.n_seq > 1) keys = std::min<uint64_t>(keys, 1024);
+        }
+    } else if (units < 512) {
+        // The fewest parts that keep 19 of 20 CUs busy, of 512 keys or more: parts are written and read again, and a
+        // workgroup takes some us to begin.  512 new tokens over 128K: 1064 us at 4 parts (256 workgroups), 1096 at 16,
+        // 1293 at 64.
+        const uint64_t most = std::min(1024 / units, span / 512);
+        uint64_t best = 1, filled = 0;               // of 1000
+        for (uint64_t n = 1; n <= most && filled < 950; ++n) {
+            const uint64_t f = units * n * 1000 / ((units * n + 255) / 256 * 256);
+            if (f > filled) best = n, filled = f;
+        }
+        keys = (span + best - 1) / best;
+    }
     const uint64_t unit = few ? 128 : kTileKeys;
     keys = std::max(unit, (keys + unit - 1) / unit * unit);
     p.splits = (uint32_t)std::max<uint64_t>(1, (span + keys - 1) / keys);
