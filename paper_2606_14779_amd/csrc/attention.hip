@@ -158,12 +158,26 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
     const uint32_t kv_head = blockIdx.x % c.kv_heads;
     const uint32_t rest = blockIdx.x / c.kv_heads;
     // the tiles of a part of the keys run side by side, so that its keys come from L2 for all but one of them;
-    // later tiles first: under a causal mask they have the most keys
-    const uint32_t split = rest / a.tiles;
-    const uint32_t tile = a.tiles - 1 - rest % a.tiles;
-    const uint32_t seq = a.tiles == c.n_seq ? tile : seq_of_tile(c, tile, TR);
-    const Seq s = load_seq(c, seq);
-    const uint32_t row0 = (tile - (a.tiles == c.n_seq ? tile : first_tile(c, seq, TR))) * TR;
+    // under a causal mask later tiles have more keys
+    const uint32_t split = rest / a.tiles, rank = rest % a.tiles;
+    uint32_t seq, row0;
+    Seq s;
+    if (c.n_seq > 1 && c.n_seq <= 64) {
+        const Tile t = tile_by_length(c, rank, TR, TK);
+        if (t.tile == kNoTile) return;
+        seq = t.seq;
+        s = t.s;
+        row0 = t.tile * TR;
+    } else {
+        const uint32_t tile = a.tiles - 1 - rank;
+        seq = seq_of_tile(c, tile, TR);
+        s = load_seq(c, seq);
+        row0 = (tile - first_tile(c, seq, TR)) * TR;
+    }
+    // the same for all lanes, whichever way they came
+    seq = __builtin_amdgcn_readfirstlane(seq);
+    row0 = __builtin_amdgcn_readfirstlane(row0);
+    s = {__builtin_amdgcn_readfirstlane(s.q_begin), __builtin_amdgcn_readfirstlane(s.n_q), __builtin_amdgcn_readfirstlane(s.kv)};
     const uint32_t rows = (uint32_t)s.n_q * c.group;
     if (row0 >= rows) return;
     const uint32_t rows_here = min(rows - row0, (uint32_t)TR);

@@ -175,6 +175,57 @@ __device__ __forceinline__ uint32_t seq_of_tile(const CacheView &c, uint32_t til
     return lo;
 }
 
+// Inclusive sum over the lanes up to this one, within the vector unit.
+__device__ __forceinline__ uint32_t sum_upto(uint32_t x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);   // the lane 1 below in a row of 16, then 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // a row's last lane to the next row
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);  // lane 31 to the upper half
+    return x;
+}
+
+// The rank-th longest row tile of a batch of up to 64 sequences: tiles of tile_rows rows (of a KV head) by the keys
+// that a causal mask leaves them, in units of `keys`; of equal ones the earlier sequence's first.  Workgroups begin
+// in this order, so that none with much to do begins last.  Ranks past the last tile give tile == none.
+struct Tile {
+    uint32_t seq, tile;
+    Seq s;
+};
+constexpr uint32_t kNoTile = 0xFFFFFFFFu;
+__device__ __forceinline__ Tile tile_by_length(const CacheView &c, uint32_t rank, uint32_t tile_rows, uint32_t keys)
+{
+    const uint32_t lane = threadIdx.x & 63;
+    Seq s = load_seq(c, min(lane, c.n_seq - 1));
+    if (lane >= c.n_seq) s.n_q = 0;
+    const uint32_t tiles = (uint32_t)(((uint64_t)s.n_q * c.group + tile_rows - 1) / tile_rows);
+    // tiles of this lane's sequence with x or more units of keys: those whose last token sees key (x - 1) * keys
+    auto at_least = [&](uint32_t x) {
+        const int64_t token = ((int64_t)x - 1) * keys - (s.kv - s.n_q);
+        if (x == 0 || token <= 0) return tiles;
+        return token >= s.n_q ? 0u : tiles - (uint32_t)((uint64_t)token * c.group / tile_rows);
+    };
+    auto all = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane(sum_upto(x), 63); };
+    if (rank >= all(tiles)) return {0, kNoTile, s};
+    uint32_t lo = 0, hi = c.max_kv / keys + 2;       // all(at_least(lo)) > rank >= all(at_least(hi))
+    while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (all(at_least(mid)) > rank)
+            lo = mid;
+        else
+            hi = mid;
+    }
+    const uint32_t longer = at_least(hi), these = at_least(lo) - longer;
+    const uint32_t left = rank - all(longer), upto = sum_upto(these);
+    const uint64_t found = __ballot(upto > left);
+    const int who = __ffsll((unsigned long long)found) - 1;
+    auto from = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane(x, who); };
+    s = {(int32_t)from(s.q_begin), (int32_t)from(s.n_q), (int32_t)from(s.kv)};
+    return {(uint32_t)who, from(tiles) - from(longer + these) + left - (from(upto) - from(these)), s};
+}
+
 }  // namespace kvp
 
 #endif
