@@ -760,8 +760,7 @@ __device__ __forceinline__ void halve(float (&acc)[32], int lane)
 
 // A wave holds 64 keys as the A operand and goes over the rows, which come through LDS for all waves: S^T again,
 // so every lane adds up the weights of its own 32 keys, for one row of each 32, in a fixed order; the lanes are
-// added at the end.  Long rows of queries are bound by the exponentials and the sums around them (three
-// instructions to a weight), single tokens by reading the keys, which therefore come in whole rows, through LDS.
+// added at the end.  Bound by the vector unit: a difference, an exponential and a sum to a weight.
 template <class T, int DP>
 __global__ __launch_bounds__(kMassWaves * 64, DP > 128 ? 1 : 2) void attention_mass(const MassArgs a)
 {
@@ -772,7 +771,7 @@ __global__ __launch_bounds__(kMassWaves * 64, DP > 128 ? 1 : 2) void attention_m
     static_assert(2 * TR <= kMassWaves * TK, "two tiles of rows fit the keys' space");
 
     const CacheView &c = a.c;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
     const uint32_t kv_head = blockIdx.x % c.kv_heads;
     const uint32_t tile = blockIdx.x / c.kv_heads;
@@ -796,24 +795,43 @@ __global__ __launch_bounds__(kMassWaves * 64, DP > 128 ? 1 : 2) void attention_m
     const int load_piece = tid % CH, load_row = tid / CH;
     const bool piece_live = (uint32_t)load_piece * 8 < c.head_dim;
     const uint32_t piece_at = piece_live ? load_piece * 8 : 0;
+    // Where the heads of a group divide a tile, a thread's rows keep their heads from tile to tile and their places
+    // move by a constant; else, and for the last rows, they are worked out.
     w4 rq[N];
     float r_lse = 0.0f;
-    auto load_rows = [&](uint32_t r0) {
+    const uint16_t *q_at[N];
+    const float *lse_at = a.lse;
+    const bool steady = TR % c.group == 0;
+    const uint64_t q_step = TR / c.group * a.q_stride;
+    auto place_rows = [&](uint32_t r0) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const uint32_t row = min(r0 + load_row + i * PASS, row_end - 1), token = token_of(c, row);
             const uint32_t head = kv_head * c.group + row - token * c.group;
-            rq[i] = load16g(a.q + (uint64_t)(s.q_begin + token) * a.q_stride + (uint64_t)head * c.head_dim + piece_at);
+            q_at[i] = a.q + (uint64_t)(s.q_begin + token) * a.q_stride + (uint64_t)head * c.head_dim + piece_at;
         }
         const uint32_t row = min(r0 + (tid & (TR - 1)), row_end - 1), token = token_of(c, row);
-        r_lse = a.lse[(uint64_t)(kv_head * c.group + row - token * c.group) * c.total_q + s.q_begin + token];
+        lse_at = a.lse + (uint64_t)(kv_head * c.group + row - token * c.group) * c.total_q + s.q_begin + token;
+    };
+    auto load_rows = [&](uint32_t r0) __attribute__((always_inline)) {
+        if (r0 == row_begin || !steady || r0 + TR > row_end) {
+            place_rows(r0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) q_at[i] += q_step;
+            lse_at += TR / c.group;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) rq[i] = load16g(q_at[i]);
+        r_lse = *lse_at;
     };
     auto store_rows = [&](int buf, uint32_t r0) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int r = load_row + i * PASS;
             const int qp = load_piece ^ (DP >= 128 ? r & 15 : (r >> 1) & 7);
-            *(w4 *)&lds[(buf * TR + r) * DP + qp * 8] = piece_live ? rq[i] : w4{0, 0, 0, 0};
+            if (c.head_dim != DP && !piece_live) rq[i] = w4{0, 0, 0, 0};
+            *(w4 *)&lds[(buf * TR + r) * DP + qp * 8] = rq[i];
         }
         // a row past the end, or without keys, gives no weight: exp2(-inf)
         if (tid < TR) lds_lse[buf][tid] = r0 + tid < row_end && r_lse > -INFINITY ? r_lse * kLog2e : INFINITY;
@@ -866,36 +884,51 @@ __global__ __launch_bounds__(kMassWaves * 64, DP > 128 ? 1 : 2) void attention_m
         if (r0 + TR < row_end) load_rows(r0 + TR);
         __syncthreads();                             // the rows are in LDS; everyone has left the tile before
         const int32_t t_first = (int32_t)token_of(c, r0), t_last = (int32_t)token_of(c, min(r0 + TR, row_end) - 1);
-        const bool some = k0 <= shift + t_last && (!a.window || (int64_t)k0 + TK - 1 > (int64_t)shift + t_first - a.window);
-        const bool full = k0 + TK - 1 <= shift + t_first && (!a.window || (int64_t)k0 > (int64_t)shift + t_last - a.window);
-        if (some) {
+        const bool some = k0 < s.kv && k0 <= shift + t_last &&
+                          (!a.window || (int64_t)k0 + TK - 1 > (int64_t)shift + t_first - a.window);
+        const bool full = some && k0 + TK - 1 <= shift + t_first &&
+                          (!a.window || (int64_t)k0 > (int64_t)shift + t_last - a.window);
+        auto logits = [&](int rb, v16f (&z)[2]) __attribute__((always_inline)) {
+            const int at = rb * 32 + col;
+            z[0] = z[1] = v16f{};
+#pragma unroll
+            for (int i = 0; i < DP / 16; ++i) {
+                const int qp = (2 * i + half) ^ (DP >= 128 ? at & 15 : (at >> 1) & 7);
+                const w4 q = *(const w4 *)&lds[(buf * TR + at) * DP + qp * 8];
+                z[0] = T::mma32(k[0][i], q, z[0]);
+                z[1] = T::mma32(k[1][i], q, z[1]);
+            }
+        };
+        if (full) {
 #pragma unroll
             for (int rb = 0; rb < TR / 32; ++rb) {
-                if (r0 + rb * 32 >= row_end) break;
-                const int at = rb * 32 + col;
-                const float lse = lds_lse[buf][at];
-                v16f z[2] = {v16f{}, v16f{}};
+                v16f z[2];
+                logits(rb, z);
+                const float lse = lds_lse[buf][rb * 32 + col];
 #pragma unroll
-                for (int i = 0; i < DP / 16; ++i) {
-                    const int qp = (2 * i + half) ^ (DP >= 128 ? at & 15 : (at >> 1) & 7);
-                    const w4 q = *(const w4 *)&lds[(buf * TR + at) * DP + qp * 8];
-                    z[0] = T::mma32(k[0][i], q, z[0]);
-                    z[1] = T::mma32(k[1][i], q, z[1]);
+                for (int r = 0; r < 32; r += 8) {
+                    float w[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        w[i] = exp2_fast(__builtin_fmaf(z[(r + i) / 16][(r + i) % 16], a.scale_log2, -lse));
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) acc[r + i] += w[i];
                 }
-                if (full) {
+                __builtin_amdgcn_sched_barrier(0);   // mixed, the blocks' logits do not fit the registers
+            }
+        } else if (some) {
+            for (int rb = 0; rb < TR / 32; ++rb) {
+                v16f z[2];
+                logits(rb, z);
+                const float lse = lds_lse[buf][rb * 32 + col];
+                const int32_t limit = shift + (int32_t)token_of(c, r0 + rb * 32 + col);
+                const int32_t floor_key = a.window ? (int32_t)max((int64_t)limit + 1 - (int64_t)a.window, (int64_t)0) : 0;
 #pragma unroll
-                    for (int r = 0; r < 32; ++r)
-                        acc[r] += exp2_fast(__builtin_fmaf(z[r / 16][r % 16], a.scale_log2, -lse));
-                } else {
-                    const int32_t limit = shift + (int32_t)token_of(c, r0 + at);
-                    const int32_t floor_key = a.window ? (int32_t)max((int64_t)limit + 1 - (int64_t)a.window, (int64_t)0) : 0;
-#pragma unroll
-                    for (int r = 0; r < 32; ++r) {
-                        const int32_t key = k0 + 32 * (r / 16) + 8 * (r % 16 / 4) + r % 4 + 4 * half;
-                        const bool sees = key <= limit && key >= floor_key;
-                        const float z1 = sees ? __builtin_fmaf(z[r / 16][r % 16], a.scale_log2, -lse) : -INFINITY;
-                        acc[r] += exp2_fast(z1);
-                    }
+                for (int r = 0; r < 32; ++r) {
+                    const int32_t key = k0 + 32 * (r / 16) + 8 * (r % 16 / 4) + r % 4 + 4 * half;
+                    const bool sees = key <= limit && key >= floor_key;
+                    const float z1 = sees ? __builtin_fmaf(z[r / 16][r % 16], a.scale_log2, -lse) : -INFINITY;
+                    acc[r] += exp2_fast(z1);
                 }
             }
         }
@@ -915,6 +948,105 @@ __global__ __launch_bounds__(kMassWaves * 64, DP > 128 ? 1 : 2) void attention_m
         const uint64_t to = ((uint64_t)seq * c.kv_heads + kv_head) * a.score_stride + key;
         const float sum = seen >> at & 1 ? acc[0] : 0.0f;            // an absent key may have been anything
         a.score_out[to] = (a.score_in ? a.score_in[to] : 0.0f) + sum;
+    }
+}
+
+// Up to 16 rows: bound by reading the keys, which go from memory to the registers that the product takes them from.
+constexpr int kMassSteps = 4;                        // of 32 keys a wave
+
+template <class T, int DP>
+__global__ __launch_bounds__(kMassWaves * 64, 2) void attention_mass_few(const MassArgs a)
+{
+    constexpr int KS = DP / 32, NW = kMassWaves, S = kMassSteps;
+    const CacheView &c = a.c;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int col = lane & 15, quad = lane >> 4;
+    const uint32_t kv_head = blockIdx.x % c.kv_heads;
+    const uint32_t tile = blockIdx.x / c.kv_heads;
+    const uint32_t tiles = (c.max_kv + NW * 32 * S - 1) / (NW * 32 * S);
+    const uint32_t seq = tile / tiles;
+    const uint32_t first_key = tile % tiles * (NW * 32 * S) + wave * 32;   // then every NW * 32
+    int32_t slot[S];                                 // asked for before the sequence's length is known
+#pragma unroll
+    for (int t = 0; t < S; ++t)
+        slot[t] = load4g(c.table + (uint64_t)seq * c.table_stride +
+                         block_of(c, min(first_key + t * NW * 32 + (lane & 31), c.max_kv - 1)));
+    const Seq s = load_seq(c, seq);
+    if (first_key >= (uint32_t)s.kv) return;
+    const uint32_t rows = (uint32_t)s.n_q * c.group;                       // at most 16
+    const uint32_t row = rows ? min((uint32_t)col, rows - 1) : 0, token = token_of(c, row);
+    const uint32_t head = kv_head * c.group + row - token * c.group;
+    const int32_t limit = s.kv - s.n_q + (int32_t)token;
+    const int64_t floor_key = a.window ? (int64_t)limit + 1 - (int64_t)a.window : 0;
+    w4 q[KS];
+    float lse = INFINITY;                            // a row past the end, or without keys, gives no weight: exp2(-inf)
+    if (rows) {
+        const uint16_t *p = a.q + (uint64_t)(s.q_begin + token) * a.q_stride + (uint64_t)head * c.head_dim;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            const uint32_t at = 32 * i + 8 * quad;
+            q[i] = load16g(p + (at < c.head_dim ? at : 0));
+            if (c.head_dim != DP && at >= c.head_dim) q[i] = w4{0, 0, 0, 0};
+        }
+        const float x = a.lse[(uint64_t)head * c.total_q + s.q_begin + token];
+        const bool asked = a.last == 0 || (uint32_t)s.n_q - token <= a.last;
+        if ((uint32_t)col < rows && asked && x > -INFINITY) lse = x * kLog2e;
+    } else {
+#pragma unroll
+        for (int i = 0; i < KS; ++i) q[i] = w4{0, 0, 0, 0};
+    }
+    uint32_t seen[S];
+    w4 k[2][2][KS];
+    auto load = [&](int t, w4 (&to)[2][KS]) __attribute__((always_inline)) {
+        const uint32_t key = first_key + t * NW * 32 + (lane & 31);
+        const uint32_t r = row_of(c, key < (uint32_t)s.kv ? slot[t] : -1, kv_head, key);
+        seen[t] = (uint32_t)__ballot(r != kNoRow);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            uint32_t from = __shfl(r, b * 16 + col);
+            from = from == kNoRow ? 0 : from;
+            const uint16_t *p = a.k + (uint64_t)from * c.head_dim;
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                const uint32_t at = 32 * i + 8 * quad;
+                to[b][i] = load16g(p + (at < c.head_dim ? at : 0));
+            }
+        }
+    };
+    load(0, k[0]);
+#pragma unroll
+    for (int t = 0; t < S; ++t) {
+        if (t + 1 < S) load(t + 1, k[(t + 1) & 1]);
+        const uint32_t k0 = first_key + t * NW * 32;
+        float w[8];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            v4f z{};
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                w4 x = k[t & 1][b][i];
+                if (c.head_dim != DP && 32u * i + 8 * quad >= c.head_dim) x = w4{0, 0, 0, 0};
+                z = T::mma16(x, q[i], z);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int32_t key = (int32_t)k0 + 16 * b + 4 * quad + r;
+                const float x = key <= limit && key >= floor_key ? __builtin_fmaf(z[r], a.scale_log2, -lse) : -INFINITY;
+                w[4 * b + r] = exp2_fast(x);
+            }
+        }
+        // over the 16 rows: lanes with bit d keep the upper half of their keys; at the end both of a pair have the sum
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = (col & 8 ? w[i + 4] : w[i]) + __shfl_xor(col & 8 ? w[i] : w[i + 4], 8);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) w[i] = (col & 4 ? w[i + 2] : w[i]) + __shfl_xor(col & 4 ? w[i] : w[i + 2], 4);
+        w[0] = (col & 2 ? w[1] : w[0]) + __shfl_xor(col & 2 ? w[0] : w[1], 2);
+        w[0] += __shfl_xor(w[0], 1);
+        const int e = col >> 1, at = 16 * (e >> 2) + 4 * quad + (e & 3);
+        if (!(col & 1) && k0 + at < (uint32_t)s.kv) {
+            const uint64_t to = ((uint64_t)seq * c.kv_heads + kv_head) * a.score_stride + k0 + at;
+            a.score_out[to] = (a.score_in ? a.score_in[to] : 0.0f) + (seen[t] >> at & 1 ? w[0] : 0.0f);
+        }
     }
 }
 
@@ -978,6 +1110,11 @@ template <class T, int DP>
 struct Mass {
     static hipError_t go(const MassArgs &a, hipStream_t stream)
     {
+        if ((uint64_t)a.c.max_q * a.c.group <= kFewRows) {
+            const uint32_t tiles = (a.c.max_kv + kMassWaves * 32 * kMassSteps - 1) / (kMassWaves * 32 * kMassSteps);
+            attention_mass_few<T, DP><<<tiles * a.c.n_seq * a.c.kv_heads, kMassWaves * 64, 0, stream>>>(a);
+            return hipGetLastError();
+        }
         const uint32_t tiles = (a.c.max_kv + kMassWaves * kMassKeys - 1) / (kMassWaves * kMassKeys);
         attention_mass<T, DP><<<tiles * a.c.n_seq * a.c.kv_heads, kMassWaves * 64, 0, stream>>>(a);
         return hipGetLastError();
