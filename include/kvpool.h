@@ -616,13 +616,14 @@ typedef struct {
  * kv_len[s] - n_q + i.  Cached token j lies in slot
  * block_table[s * table_stride + j / block_size]; an entry outside
  * [0, num_slots) is absent: no query sees its tokens and nothing is written
- * there.  A sequence may have no new token, or no cached one.
+ * there.  A sequence may have no new token, or no cached one.  At most 2^18
+ * sequences times KV heads and 2^29 new tokens times query heads in a call.
  */
 typedef struct {
     uint32_t n_seq;
     uint32_t total_q;         /* cu_q[n_seq] */
     uint32_t max_q;           /* at least the new tokens of any sequence */
-    uint32_t max_kv;          /* at least the cached tokens of any sequence, at most table_stride * block_size */
+    uint32_t max_kv;          /* at least the cached tokens of any sequence, at most table_stride * block_size and 2^30 */
     uint32_t table_stride;
     uint32_t reserved;        /* 0 */
     const int32_t *cu_q;      /* [n_seq + 1], ascending from 0; not used by kv_evict */

@@ -34,7 +34,8 @@ void divide_by(uint32_t d, uint32_t *magic, uint32_t *shift)
     *magic = (uint32_t)(((1ull << (31 + *shift)) + d - 1) / d);
 }
 
-constexpr uint64_t kMostRows = 1ull << 30;   // new tokens times query heads: what a launch's grid can count
+// What a launch's grid can count, with room: new tokens times query heads, sequences times KV heads, parts of a call.
+constexpr uint64_t kMostRows = 1ull << 29, kMostLists = 1ull << 18, kMostParts = 1ull << 22;
 
 // Checks the shape and the batch; queries says whether cu_q is used.
 CacheView view_of(const kvp_cache_shape *s, const kvp_batch *b, bool queries)
@@ -49,9 +50,9 @@ CacheView view_of(const kvp_cache_shape *s, const kvp_batch *b, bool queries)
     need(s->num_q_heads <= 65536 && s->block_size <= 65536, "more than 65536 heads or tokens per block");
     need((uint64_t)s->num_slots * s->num_kv_heads <= 0xFFFFFFFEull / s->block_size, "a cache of 2^32 rows or more");
     need(s->reserved == 0 && b->reserved == 0, "reserved fields are not 0");
-    need(b->max_kv <= 0x7FFFFFFFu && b->max_q <= 0x7FFFFFFFu && b->total_q <= 0x7FFFFFFFu, "a length of 2^31 or more");
+    need(b->max_kv <= 1u << 30 && b->max_q <= 1u << 30 && b->total_q <= 1u << 30, "a length of more than 2^30");
     need((uint64_t)b->table_stride * s->block_size >= b->max_kv, "table_stride * block_size is less than max_kv");
-    need((uint64_t)b->n_seq * s->num_kv_heads <= 1u << 22, "more than 2^22 sequences times KV heads");
+    need((uint64_t)b->n_seq * s->num_kv_heads <= kMostLists, "more than 2^18 sequences times KV heads");
     CacheView c{};
     if (b->n_seq) {
         need_pointer(b->kv_len, 4, "kv_len");
@@ -59,7 +60,7 @@ CacheView view_of(const kvp_cache_shape *s, const kvp_batch *b, bool queries)
         if (queries) {
             need_pointer(b->cu_q, 4, "cu_q");
             need(b->max_q <= b->total_q, "max_q is more than total_q");
-            need((uint64_t)b->total_q * s->num_q_heads <= kMostRows, "more than 2^30 new tokens times query heads");
+            need((uint64_t)b->total_q * s->num_q_heads <= kMostRows, "more than 2^29 new tokens times query heads");
         }
     } else {
         need(!queries || b->total_q == 0, "new tokens without a sequence");
@@ -120,6 +121,7 @@ Cut cut_of(const CacheView &c, uint32_t window)
         if (span > 256) {
             keys = std::max<uint64_t>(128, units * span / 1024);
             if (c.n_seq > 1) keys = std::min<uint64_t>(keys, 1024);
+            keys = std::max(keys, units * span / kMostParts);
         }
     } else if (units < 512) {
         // The fewest parts that keep 19 of 20 CUs busy, of 512 keys or more: parts are written and read again, and a

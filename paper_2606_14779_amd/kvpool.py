@@ -305,6 +305,13 @@ def probe_memcpy(dst: int, src: int, nbytes: int, stream: int = 0):
 
 
 # ---- operators on the engine's paged cache (device memory as integers: tensor.data_ptr())
+#
+# These run once per layer and step, so the range checks of their integers are one expression each: an OR of integers
+# is negative if one of them is, and reaches past a type's bits if one of them does.
+
+def _out_of_range(what: str):
+    raise ValueError("%s: an integer argument is outside its type's range" % what)
+
 
 class CacheShape:
     """The cache of a layer and the heads over it (kvp_cache_shape); dtype "bf16" or "f16"."""
@@ -341,9 +348,13 @@ def rope_append(shape: CacheShape, batch: Batch, table: int, n_positions: int, r
                 q_out: int = 0, q_out_stride: int = 0, pos: int = 0, pos_stride: int = 0, interleaved: bool = False,
                 stream: int = 0):
     """kv_rope_append: rotated queries to q_out, rotated keys, values and positions to the cache."""
-    _check(_lib.kv_rope_append(shape._p, batch._p, table, n_positions, rot_dim, ROPE_INTERLEAVED if interleaved else 0,
-                               positions, q, q_stride, q_out, q_out_stride, k, k_stride, v, v_stride, k_cache, v_cache,
-                               pos, pos_stride, stream))
+    if (n_positions | rot_dim | pos_stride) >> 32 or (q_stride | q_out_stride | k_stride | v_stride) >> 64:
+        _out_of_range("rope_append")
+    rc = _cdll.kv_rope_append(shape._p, batch._p, table, n_positions, rot_dim, ROPE_INTERLEAVED if interleaved else 0,
+                              positions, q, q_stride, q_out, q_out_stride, k, k_stride, v, v_stride, k_cache, v_cache, pos,
+                              pos_stride, stream)
+    if rc:
+        _check(rc)
 
 
 def attention_workspace(shape: CacheShape, batch: Batch) -> int:
@@ -357,15 +368,23 @@ def attention(shape: CacheShape, batch: Batch, q: int, q_stride: int, k_cache: i
               out_stride: int, *, window: int = 0, sinks: int = 0, lse: int = 0, workspace: int = 0,
               workspace_bytes: int = 0, stream: int = 0):
     """kv_attention: causal attention of the new tokens over the cached ones."""
-    _check(_lib.kv_attention(shape._p, batch._p, q, q_stride, k_cache, v_cache, scale, window, sinks, out, out_stride,
-                             lse, workspace, workspace_bytes, stream))
+    if window >> 32 or (q_stride | out_stride | workspace_bytes) >> 64:
+        _out_of_range("attention")
+    rc = _cdll.kv_attention(shape._p, batch._p, q, q_stride, k_cache, v_cache, scale, window, sinks, out, out_stride, lse,
+                            workspace, workspace_bytes, stream)
+    if rc:
+        _check(rc)
 
 
 def attention_mass(shape: CacheShape, batch: Batch, q: int, q_stride: int, k_cache: int, scale: float, lse: int,
                    score_in: int, score_out: int, score_stride: int, *, window: int = 0, last: int = 0, stream: int = 0):
     """kv_attention_mass: the attention weight that each cached token collects, added to its score."""
-    _check(_lib.kv_attention_mass(shape._p, batch._p, q, q_stride, k_cache, scale, window, lse, last, score_in, score_out,
-                                  score_stride, stream))
+    if (window | last | score_stride) >> 32 or q_stride >> 64:
+        _out_of_range("attention_mass")
+    rc = _cdll.kv_attention_mass(shape._p, batch._p, q, q_stride, k_cache, scale, window, lse, last, score_in, score_out,
+                                 score_stride, stream)
+    if rc:
+        _check(rc)
 
 
 def evict_workspace(shape: CacheShape, batch: Batch) -> int:
@@ -379,8 +398,12 @@ def evict(shape: CacheShape, batch: Batch, keep: int, score_in: int, score_out: 
           v_cache: int, len_out: int, workspace: int, workspace_bytes: int, *, protect: int = 0, pos_in: int = 0,
           pos_out: int = 0, pos_stride: int = 0, stream: int = 0):
     """kv_evict: keeps the tokens of largest score and compacts the cache in place."""
-    _check(_lib.kv_evict(shape._p, batch._p, keep, protect, score_in, score_out, score_stride, pos_in, pos_out, pos_stride,
-                         k_cache, v_cache, len_out, workspace, workspace_bytes, stream))
+    if (score_stride | pos_stride) >> 32 or workspace_bytes >> 64:
+        _out_of_range("evict")
+    rc = _cdll.kv_evict(shape._p, batch._p, keep, protect, score_in, score_out, score_stride, pos_in, pos_out, pos_stride,
+                        k_cache, v_cache, len_out, workspace, workspace_bytes, stream)
+    if rc:
+        _check(rc)
 
 
 class KVPool:

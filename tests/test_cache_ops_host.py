@@ -44,7 +44,7 @@ def _refused(f, *a, **kw):
 SHAPES = [dict(heads=7), dict(heads=0), dict(kv_heads=0), dict(head_dim=0), dict(head_dim=12), dict(head_dim=264),
           dict(block=0), dict(slots=0), dict(slots=1 << 31), dict(heads=1 << 17), dict(block=1 << 17)]
 BATCHES = [dict(max_kv=641), dict(max_q=5), dict(kv_len=0), dict(kv_len=P + 2), dict(table=0), dict(table=P + 1),
-           dict(max_kv=1 << 31, stride=1 << 30), dict(n_seq=1 << 22)]
+           dict(max_kv=(1 << 30) + 1, stride=1 << 30), dict(n_seq=1 << 22), dict(n_seq=(1 << 17) + 1)]
 
 
 @pytest.mark.parametrize("call", [_attention, _mass, _evict, _rope])
@@ -123,11 +123,23 @@ def test_python_side_refusals():
         _mass(last=-1)
     with pytest.raises(ValueError):
         K.rope_table(P, 10, 64, kind="other")
+    for bad in (dict(q_stride=-8), dict(out_stride=1 << 64), dict(workspace_bytes=-1), dict(window=1 << 32)):
+        with pytest.raises(ValueError):
+            _attention(**bad)
+    for bad in (dict(q_stride=1 << 64), dict(last=1 << 32), dict(stride=-1)):
+        with pytest.raises(ValueError):
+            _mass(**bad)
+    for bad in (dict(stride=-1), dict(pos_stride=1 << 32), dict(n=-1)):
+        with pytest.raises(ValueError):
+            _evict(**bad)
+    for bad in (dict(n=-1), dict(rot=1 << 32), dict(pos_stride=-1), dict(k_stride=-8), dict(v_stride=1 << 64),
+                dict(q_stride=-8), dict(q_out_stride=1 << 65)):
+        with pytest.raises(ValueError):
+            _rope(**bad)
 
 
 def test_null_structures_and_reserved_fields():
-    lib, ok = K._lib, 0
-    shape, batch = _shape(), _batch()
+    lib, shape, batch = K._lib, _shape(), _batch()
     for f in (lib.kv_attention_workspace, lib.kv_evict_workspace):
         assert f(None, batch._p, P) == -1 and f(shape._p, None, P) == -1 and f(shape._p, batch._p, None) == -1
     assert lib.kv_rope_table(P, 10, 64, None, None) == -1
@@ -136,7 +148,6 @@ def test_null_structures_and_reserved_fields():
         _refused(K.attention_workspace, s, batch)
     batch._c.reserved = 1
     _refused(K.evict_workspace, shape, batch)
-    assert ok == 0
 
 
 def test_workspaces():
