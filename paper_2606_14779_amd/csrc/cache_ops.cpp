@@ -135,6 +135,8 @@ Cut cut_of(const CacheView &c, uint32_t window)
         }
         keys = (span + best - 1) / best;
     }
+    // no more parts than without a window: the workspace is asked for without one
+    if (window) keys = std::max(keys, (span + cut_of(c, 0).splits - 1) / cut_of(c, 0).splits);
     const uint64_t unit = few ? 128 : kTileKeys;
     keys = std::max(unit, (keys + unit - 1) / unit * unit);
     p.splits = (uint32_t)std::max<uint64_t>(1, (span + keys - 1) / keys);
@@ -143,7 +145,6 @@ Cut cut_of(const CacheView &c, uint32_t window)
     return p;
 }
 
-// Largest workspace over all windows: a window only shortens the span, and with it the number of parts.
 uint64_t attention_bytes(const CacheView &c) { return cut_of(c, 0).bytes; }
 
 // Words of workspace to a list: four of counts, two per token (candidates, then moves), a bit per token, and for

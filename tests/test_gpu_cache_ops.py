@@ -92,6 +92,12 @@ def test_attention_window(window, lens):
     check_attention(R.Case(lens, head_dim=128, seed=6), window=window, with_sinks=window == 64)
 
 
+@pytest.mark.parametrize("lens,window", [([(1, 17000)], 16400), ([(2, 5100)], 4000), ([(100, 3300)], 2500), ([(1, 300)], 200)])
+def test_attention_window_needs_no_more_workspace(lens, window):
+    """Lengths at which the keys without the window would be cut into fewer parts than those within it."""
+    check_attention(R.Case(lens, heads=16, kv_heads=8, seed=15), window=window)
+
+
 @pytest.mark.parametrize("lens", [FEW["ragged"], FEW["empty row"], ROWS["empty rows"], ROWS["ragged"], [(1, 9000)]])
 def test_attention_sinks(lens):
     check_attention(R.Case(lens, heads=16, kv_heads=2, seed=7), with_sinks=True)
