@@ -327,20 +327,28 @@ __global__ __launch_bounds__(kSelectThreads) void evict_finish(const EvictArgs a
     uint32_t ends[PER], total = 0;
 #pragma unroll
     for (int q = 0; q < PER; ++q) ends[q] = total += lists.found[wave * PER + q];
-    // f(candidate, whether there is one) in order, a few loads ahead
+    constexpr int U = 8;
+    auto load = [&](uint32_t i0, w2 (&k)[U]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t i = min(i0 + 64 * u + lane, total - 1);
+            uint32_t q = 0, begin = 0;
+#pragma unroll
+            for (int e = 0; e + 1 < PER; ++e)
+                if (i >= ends[e]) q = e + 1, begin = ends[e];
+            k[u] = lists.candidates[(uint64_t)(wave * PER + q) * size + (i - begin)];
+        }
+    };
+    // f(candidate, whether there is one) in order; the first ones stay in registers, as a rule all of them
+    w2 first[U];
+    if (total) load(0, first);
     auto over_candidates = [&](auto f) __attribute__((always_inline)) {
-        constexpr int U = 4;
-        for (uint32_t i0 = 0; i0 < total; i0 += 64 * U) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (64u * u < total) f(first[u], 64 * u + lane < total);
+        for (uint32_t i0 = 64 * U; i0 < total; i0 += 64 * U) {
             w2 k[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const uint32_t i = min(i0 + 64 * u + lane, total - 1);
-                uint32_t q = 0, begin = 0;
-#pragma unroll
-                for (int e = 0; e + 1 < PER; ++e)
-                    if (i >= ends[e]) q = e + 1, begin = ends[e];
-                k[u] = lists.candidates[(uint64_t)(wave * PER + q) * size + (i - begin)];
-            }
+            load(i0, k);
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (i0 + 64 * u < total) f(k[u], i0 + 64 * u + lane < total);
