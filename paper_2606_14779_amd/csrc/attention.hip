@@ -791,6 +791,12 @@ __global__ __launch_bounds__(kMassWaves * 64, DP > 128 ? 1 : 2) void attention_m
         last = (int32_t)min((int64_t)last, (int64_t)group_k0 + kMassWaves * TK - 1 + (int64_t)a.window - 1 - shift);
     const uint32_t row_begin = (uint32_t)max(first, 0) * c.group;
     const uint32_t row_end = last < first ? row_begin : (uint32_t)(last + 1) * c.group;
+    if (row_begin == row_end) {                      // none: under a window, most of a long context
+        const int32_t key = k0 + lane;
+        const uint64_t to = ((uint64_t)seq * c.kv_heads + kv_head) * a.score_stride + key;
+        if (key < s.kv) a.score_out[to] = a.score_in ? a.score_in[to] : 0.0f;
+        return;
+    }
 
     const int load_piece = tid % CH, load_row = tid / CH;
     const bool piece_live = (uint32_t)load_piece * 8 < c.head_dim;
@@ -855,7 +861,7 @@ __global__ __launch_bounds__(kMassWaves * 64, DP > 128 ? 1 : 2) void attention_m
             from = from == kNoRow ? 0 : from;
             rk[i] = load16g(a.k + (uint64_t)from * c.head_dim + (live ? piece * 8 : 0));
         }
-        if (row_begin < row_end) load_rows(row_begin);
+        load_rows(row_begin);
 #pragma unroll
         for (int i = 0; i < TK / KPASS; ++i) {
             const int at = load_key + i * KPASS;
@@ -877,7 +883,7 @@ __global__ __launch_bounds__(kMassWaves * 64, DP > 128 ? 1 : 2) void attention_m
     float acc[32];
 #pragma unroll
     for (int r = 0; r < 32; ++r) acc[r] = 0.0f;
-    if (row_begin < row_end) store_rows(0, row_begin);
+    store_rows(0, row_begin);
     loads_arrived();
     int buf = 0;
     for (uint32_t r0 = row_begin; r0 < row_end; r0 += TR, buf ^= 1) {
@@ -995,11 +1001,17 @@ __global__ __launch_bounds__(kMassWaves * 64, 2) void attention_mass_few(const M
 #pragma unroll
         for (int i = 0; i < KS; ++i) q[i] = w4{0, 0, 0, 0};
     }
+    // the first key that any of the asked rows sees: in place of keys before it one row is read, again and again (a
+    // branch around the loads would have every step wait for the next one's)
+    const int64_t lowest = !rows ? s.kv
+                           : a.window ? (int64_t)s.kv - (int64_t)min((uint32_t)s.n_q, a.last ? a.last : ~0u) + 1 - (int64_t)a.window
+                                      : 0;
     uint32_t seen[S];
     w4 k[2][2][KS];
     auto load = [&](int t, w4 (&to)[2][KS]) __attribute__((always_inline)) {
         const uint32_t key = first_key + t * NW * 32 + (lane & 31);
-        const uint32_t r = row_of(c, key < (uint32_t)s.kv ? slot[t] : -1, kv_head, key);
+        const bool asked = key < (uint32_t)s.kv && (int64_t)first_key + t * NW * 32 + 31 >= lowest;
+        const uint32_t r = row_of(c, asked ? slot[t] : -1, kv_head, key);
         seen[t] = (uint32_t)__ballot(r != kNoRow);
 #pragma unroll
         for (int b = 0; b < 2; ++b) {

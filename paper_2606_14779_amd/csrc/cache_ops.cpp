@@ -107,12 +107,15 @@ Cut cut_of(const CacheView &c, uint32_t window)
     const uint64_t rows = (uint64_t)c.total_q * c.group;
     const uint32_t tile_rows = row_waves(c.head_dim) * 32;
     const bool few = p.few = (uint64_t)c.max_q * c.group <= kFewRows;
+    if (!rows) return p.splits = 1, p.split_keys = kTileKeys, p;
     p.tiles = few ? c.n_seq : (uint32_t)(rows / tile_rows + c.n_seq);
     const uint64_t tile_tokens = few ? c.max_q : std::min<uint64_t>(c.max_q, tile_rows / c.group + 2);
     uint64_t span = c.max_kv;
     if (window) span = std::min<uint64_t>(span, (uint64_t)window + tile_tokens + kTileKeys);
-    // workgroups that have work if all sequences are alike
-    const uint64_t units = std::max<uint64_t>(1, (few ? c.n_seq : (rows + tile_rows - 1) / tile_rows) * c.kv_heads);
+    // workgroups that have work: a sequence's last tile is half full, if it has another one
+    const uint64_t units = (few              ? c.n_seq
+                            : c.n_seq == 1 ? (rows + tile_rows - 1) / tile_rows
+                                           : std::max<uint64_t>(c.n_seq, rows / tile_rows + c.n_seq / 2)) * c.kv_heads;
     uint64_t keys = span;                            // of a part
     if (few) {
         // about 1024 parts, which read the cache at its full rate, and not above 1024 keys where lengths may differ, so

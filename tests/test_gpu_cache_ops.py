@@ -193,7 +193,8 @@ def run_mass(c, q, scale, lse, last=0, window=0, score_in=None, score_out=None):
     (dict(lens=[(37, 190)], heads=15, kv_heads=5, head_dim=80, block=5, dtype="f16"), {}),
     (dict(lens=[(37, 190)], heads=7, kv_heads=1, head_dim=256, block=32), dict(last=0xFFFFFFFF, window=0xFFFFFFFF)),
     (dict(lens=[(40, 300), (20, 40)], absent=[(0, 0), (0, 7), (0, 18), (1, 0), (1, 1), (1, 2)]), {}),
-    (dict(lens=[(1, 20000)], heads=64, kv_heads=8), {})])
+    (dict(lens=[(1, 20000)], heads=64, kv_heads=8), {}), (dict(lens=[(2, 3000), (1, 5)]), dict(window=100, last=1)),
+    (dict(lens=[(90, 3000), (40, 700)]), dict(window=100, last=3)), (dict(lens=[(2, 900), (0, 70)]), dict(window=33))])
 def test_mass(case, kw):
     c = R.Case(seed=20, **case)
     q = c.normal(c.total, c.heads, c.head_dim, std=2.0)
