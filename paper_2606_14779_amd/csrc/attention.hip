@@ -449,6 +449,7 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
 
 // ---- up to 16 rows, the waves split the keys
 
+constexpr int kFewWaves = 4;
 constexpr int kFewKeys = 32;    // to a wave at a time
 
 // Bound by reading the cache: 16 KB in flight to a wave (head_dim 128), each loaded as soon as its registers are free.
@@ -456,10 +457,11 @@ constexpr int kFewKeys = 32;    // to a wave at a time
 // 128): 188 us, 5.1 TB/s, where a copy moves 6.1.
 // Short contexts are bound by what has to be known before the first key can be asked for, so the block table's
 // entries are asked for together with the sequence's length wherever they do not depend on it.
-template <class T, int DP, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void attention_few(const AttentionArgs a)
+// Two waves to a SIMD: three would have 168 registers, and what does not fit them costs more (276 us for those 32 tokens).
+template <class T, int DP>
+__global__ __launch_bounds__(kFewWaves * 64, 2) void attention_few(const AttentionArgs a)
 {
-    constexpr int TK = kFewKeys;
+    constexpr int NW = kFewWaves, TK = kFewKeys;
     constexpr int CH = DP / 8;
     constexpr int PASS = 64 / CH;                    // rows that a wave loads at once
     constexpr int N = TK / PASS;
@@ -1101,13 +1103,7 @@ struct Few {
     static hipError_t go(const AttentionArgs &a, hipStream_t stream)
     {
         const uint32_t grid = a.tiles * a.splits * a.c.kv_heads;
-        if constexpr (DP <= 128) {
-            if (a.splits == 1) {
-                attention_few<T, DP, 8><<<grid, 8 * 64, 0, stream>>>(a);
-                return hipGetLastError();
-            }
-        }
-        attention_few<T, DP, 4><<<grid, 4 * 64, 0, stream>>>(a);
+        attention_few<T, DP><<<grid, kFewWaves * 64, 0, stream>>>(a);
         return hipGetLastError();
     }
 };
