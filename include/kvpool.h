@@ -676,7 +676,8 @@ int kv_rope_append(const kvp_cache_shape *shape, const kvp_batch *batch, const f
  * sees the cached tokens j <= c (and, with a window, j > c - window).
  *   q[total_q][num_q_heads][head_dim], q_stride as above.
  *   scale        positive; logits are scale * q . k.
- *   window       0: none.
+ *   window       0: none.  It counts cache indexes, which are in the order of positions only until kv_evict has
+ *                worked on the cache: no window after it.
  *   sinks[num_q_heads]  NULL, or a logit per head that takes part in the softmax without a value.
  *   out          as q; a token that sees nothing gets 0.
  *   lse[num_q_heads][total_q]  NULL, or the logarithm of each row's sum of exponentials, sink included
@@ -711,7 +712,10 @@ int kv_attention_mass(const kvp_cache_shape *shape, const kvp_batch *batch, cons
  * tokens (position >= protect[s]), then by score (a NaN below every number),
  * then by lower index.  Kept tokens at index >= keep[s] move, in ascending
  * order, into the indexes below keep[s] that fell free; the others stay where
- * they are.  A sequence with at most keep[s] tokens stays as it is.
+ * they are.  So the tokens left are in no order of positions: attention over
+ * them is what it was over these tokens without a window, and a window, which
+ * counts cache indexes, would hide the wrong ones.  A sequence with at most
+ * keep[s] tokens stays as it is.
  *   keep[n_seq], protect[n_seq]   protect may be NULL: none is protected.
  *   score_in, score_out[n_seq][num_kv_heads][score_stride]   scores move with their tokens; those from the new
  *                length to the old one become 0.  May be the same array.

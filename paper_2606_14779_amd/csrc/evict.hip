@@ -4,7 +4,8 @@
 // tokens first, then by score, then by lower index; a NaN score counts below every number.  Kept tokens at
 // index >= keep move into the places below keep that fell free, both in ascending order.  No source is a
 // destination, so the moves need no order among themselves and the cache is compacted in place; and since
-// attention does not depend on the order of the keys before the new ones, nothing else has to move.
+// attention without a window does not depend on the order of the keys before the new ones, nothing else has to move.
+// (A window counts cache indexes, and these no longer follow the positions.)
 //
 // Bound by what has to wait for what: digits counted, picked, counted again, then the moves listed and made.  64 of
 // 2112 tokens of 16 sequences and 8 KV heads: 11 us to select in one workgroup a list, 5 to move.  128K tokens to 8K, 8

@@ -136,7 +136,10 @@ class ServeRun:
         return out
 
     def evict(self, keep: int, recent: int) -> None:
-        """Keeps `keep` tokens of every sequence, layer and KV head, the `recent` last ones among them."""
+        """Keeps `keep` tokens of every sequence, layer and KV head, the `recent` last ones among them.  Not with a
+        window: attention counts it in cache indexes, which eviction leaves in no order of positions."""
+        if self.window:
+            raise ValueError("a windowed cache cannot be evicted from: a window counts cache indexes")
         batch = K.Batch(self.n, 0, 0, int(self.lens.max()), 0, (kv_len := self._dev(self.lens)).data_ptr(),
                         self.table.data_ptr(), self.stride)
         keeps, protect = self._dev(np.full(self.n, keep)), self._dev(self.seen - recent)

@@ -1,0 +1,51 @@
+"""What a run of requests refuses, and where it has to go on: windows, room, evictions, decoding past the first table."""
+import types
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2606_14779_amd.serve import ServeRun   # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+SHAPE = types.SimpleNamespace(layers=1, kv_heads=2, head_dim=64, block_size=16)
+HEADS = 8
+
+
+@pytest.fixture(autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+@pytest.fixture
+def make():
+    runs = []
+
+    def new_run(contexts, room, **kw):
+        runs.append(ServeRun(SHAPE, HEADS, contexts, room, **kw))
+        g = torch.Generator(device="cuda").manual_seed(3)
+        runs[-1].cache.copy_(torch.randn(runs[-1].cache.shape, generator=g, device="cuda"))
+        return runs[-1]
+    yield new_run
+    for r in runs:
+        r.close()
+
+
+def _step(run, new, seed=0):
+    run.begin(new)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return run.layer(0, torch.randn(run.total, HEADS + 4, 64, generator=g, device="cuda").to(torch.bfloat16))
+
+
+def test_no_eviction_under_a_window(make):
+    """A window counts cache indexes: an eviction would leave recent tokens outside it and old ones inside."""
+    run = make([300, 77], 64, window=32)
+    _step(run, [3, 1])
+    before, lens = run.cache.clone(), run.lens.copy()
+    with pytest.raises(ValueError, match="window"):
+        run.evict(64, recent=8)
+    assert torch.equal(run.cache, before) and np.array_equal(run.lens, lens)
+    assert torch.isfinite(_step(run, [1, 1])).all()
