@@ -43,6 +43,7 @@ class ServeRun:
             table[i, :b] = order[at:at + b]
             at += b
         self.slots = slots
+        self.most = np.array(contexts, np.int64) + room   # cached tokens that a sequence has room for
         self.table = torch.from_numpy(table).to(self.device)
         self.cache = torch.zeros((shape.layers, 2, slots, shape.kv_heads, bs, shape.head_dim), dtype=self.dtype,
                                  device=self.device)
@@ -98,7 +99,7 @@ class ServeRun:
     def begin(self, new) -> None:
         """A step of new[i] tokens of sequence i: its lengths and positions, for all layers."""
         new = np.asarray(new, np.int64)
-        if len(new) != self.n or (new < 0).any() or (self.lens + new > self.max_kv).any() \
+        if len(new) != self.n or (new < 0).any() or (self.lens + new > self.most).any() \
                 or (self.seen + new > self.n_positions).any():
             raise ValueError("new tokens do not fit the sequences")
         self.lens = (self.lens + new).astype(np.int32)

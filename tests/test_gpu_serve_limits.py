@@ -49,3 +49,19 @@ def test_no_eviction_under_a_window(make):
         run.evict(64, recent=8)
     assert torch.equal(run.cache, before) and np.array_equal(run.lens, lens)
     assert torch.isfinite(_step(run, [1, 1])).all()
+
+
+def test_every_sequence_has_its_own_room(make):
+    """200 more tokens are fewer than the longest sequence may have in all, and more than the short one's slots hold."""
+    run = make([300, 77], 64)
+    for new in ([0, 200], [0, 65], [65, 0]):
+        with pytest.raises(ValueError):
+            run.begin(new)
+        assert run.lens.tolist() == [300, 77] and run.seen.tolist() == [300, 77]
+    slot, off = int(run.tables[1][140 // 16]), 140 % 16
+    run.cache[0, :, slot, :, off] = 0
+    _step(run, [0, 64])
+    assert run.lens.tolist() == [300, 141]
+    assert run.pos[0, 1, 0, 140].item() == 140 and (run.cache[0, :, slot, :, off] != 0).any(-1).all()   # written
+    run.offload()
+    run.fetch()
