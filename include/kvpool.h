@@ -709,8 +709,10 @@ int kv_attention_mass(const kvp_cache_shape *shape, const kvp_batch *batch, cons
 /*
  * Evicts from every sequence and KV head all but keep[s] tokens and compacts
  * the cache in place.  The kept ones are the first by this order: protected
- * tokens (position >= protect[s]), then by score (a NaN below every number),
- * then by lower index.  Kept tokens at index >= keep[s] move, in ascending
+ * tokens (position >= protect[s]) by lower index, whatever their scores, then
+ * the others by score (a NaN below every number) and lower index.  Where more
+ * than keep[s] are protected, those of the highest indexes go, and no other
+ * token is kept.  Kept tokens at index >= keep[s] move, in ascending
  * order, into the indexes below keep[s] that fell free; the others stay where
  * they are.  So the tokens left are in no order of positions: attention over
  * them is what it was over these tokens without a window, and a window, which

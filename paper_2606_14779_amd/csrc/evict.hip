@@ -1,7 +1,7 @@
 // Eviction from the paged cache by score, for gfx950 (MI355X).
 //
 // A sequence of n tokens keeps, for every KV head by itself, the `keep` tokens of largest key: protected
-// tokens first, then by score, then by lower index; a NaN score counts below every number.  Kept tokens at
+// tokens first, by lower index, then the others by score and lower index; a NaN score counts below every number.  Kept tokens at
 // index >= keep move into the places below keep that fell free, both in ascending order.  No source is a
 // destination, so the moves need no order among themselves and the cache is compacted in place; and since
 // attention without a window does not depend on the order of the keys before the new ones, nothing else has to move.

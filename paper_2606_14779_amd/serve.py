@@ -139,6 +139,8 @@ class ServeRun:
     def evict(self, keep: int, recent: int) -> None:
         """Keeps `keep` tokens of every sequence, layer and KV head, the `recent` last ones among them.  Not with a
         window: attention counts it in cache indexes, which eviction leaves in no order of positions."""
+        if not 0 <= recent <= keep:
+            raise ValueError("%d tokens cannot hold the last %d" % (keep, recent))
         if self.window:
             raise ValueError("a windowed cache cannot be evicted from: a window counts cache indexes")
         batch = K.Batch(self.n, 0, 0, int(self.lens.max()), 0, (kv_len := self._dev(self.lens)).data_ptr(),

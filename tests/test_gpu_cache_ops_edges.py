@@ -1,0 +1,56 @@
+"""The operators on the paged cache at the edges of what their header says: more protected tokens than are kept,
+statistics that are not finite, weights far below a row's largest, cost and results beside non-finite values, lists of
+2^28 tokens, long ragged batches and long lists of every kind of scores."""
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import cache_ops_ref as R   # noqa: E402
+from paper_2606_14779_amd import kvpool as K   # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def _stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _dev(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _evict(c, keep, score, protect=None, pos=None, score_out=None, pos_out=None):
+    """Scores, positions and lengths after kv_evict; in place where no outputs are given."""
+    keep, protect = _dev(keep), _dev(protect) if protect is not None else None
+    score_out, pos_out = score if score_out is None else score_out, pos if pos_out is None else pos_out
+    left = torch.full_like(c.kv_len, 7)
+    w, n = c.workspace(K.evict_workspace)
+    K.evict(c.shape, c.batch, keep.data_ptr(), score.data_ptr(), score_out.data_ptr(), score.shape[2], c.k_cache.data_ptr(),
+            c.v_cache.data_ptr(), left.data_ptr(), w.data_ptr(), n, protect=protect.data_ptr() if protect is not None else 0,
+            pos_in=pos.data_ptr() if pos is not None else 0, pos_out=pos_out.data_ptr() if pos_out is not None else 0,
+            pos_stride=score.shape[2], stream=_stream())
+    return score_out, pos_out, left.tolist()
+
+
+# ---- eviction
+
+@pytest.mark.parametrize("n", [300, 9000])
+def test_evict_more_protected_tokens_than_are_kept(n):
+    """Protected tokens go by index, not by their scores (which rise with the index here), before any other token."""
+    keep = n // 6
+    c = R.Case([(0, n)], kv_heads=2, heads=2, head_dim=8, seed=70)
+    score = torch.arange(n, dtype=torch.float32, device="cuda").repeat(1, 2, 1)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda").repeat(1, 2, 1)
+    _, pos, left = _evict(c, [keep], score, protect=[n // 2], pos=pos)
+    assert left == [keep]
+    for h in range(2):
+        assert sorted(pos[0, h, :keep].tolist()) == list(range(n // 2, n // 2 + keep))

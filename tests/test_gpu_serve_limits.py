@@ -65,3 +65,17 @@ def test_every_sequence_has_its_own_room(make):
     assert run.pos[0, 1, 0, 140].item() == 140 and (run.cache[0, :, slot, :, off] != 0).any(-1).all()   # written
     run.offload()
     run.fetch()
+
+
+def test_recent_tokens_fit_what_is_kept(make):
+    run = make([300, 77], 64)
+    _step(run, [3, 1])
+    before = run.cache.clone()
+    for keep, recent in ((8, 9), (0, 1), (-1, 0), (64, -1)):
+        with pytest.raises(ValueError):
+            run.evict(keep, recent)
+    assert torch.equal(run.cache, before) and run.lens.tolist() == [303, 78]
+    run.evict(9, 9)                                    # the last ones and no others
+    for s, n in enumerate((303, 78)):
+        for h in range(2):
+            assert sorted(run.pos[0, s, h, :9].tolist()) == list(range(n - 9, n))
