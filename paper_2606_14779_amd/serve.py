@@ -63,6 +63,7 @@ class ServeRun:
         self.pool = K.KVPool([K.Region("host", held * spec.block_bytes), K.Region("staging", held * spec.block_bytes)],
                              [1, 1], spec, device)
         self.requests, self._next_request = [None] * n, 1
+        self.held = np.zeros(n, bool)                   # whether a sequence's request has its cached tokens as they are
         self._work = None
 
     def _stream(self) -> int:
@@ -87,9 +88,12 @@ class ServeRun:
                 self.pool.release(self.requests[i])
             self.requests[i] = self._next_request
             self._next_request += 1
+            self.held[i] = True
 
     def fetch(self) -> None:
-        """Brings every sequence's cached tokens back from the pool."""
+        """Brings every sequence's cached tokens back from the pool, where they have not changed since ``offload``."""
+        if not self.held.all():
+            raise ValueError("sequences %s have changed since they were offloaded" % np.flatnonzero(~self.held).tolist())
         for i in range(self.n):
             blocks = -(-int(self.lens[i]) // self.shape.block_size)
             self.pool.retrieve_request(self.requests[i], self.tables[i][:blocks], self.slots, self.k_ptrs, self.v_ptrs,
@@ -107,6 +111,7 @@ class ServeRun:
         self.total, self.cu, self.kv_len = int(cu[-1]), self._dev(cu), self._dev(self.lens)
         self.positions = self._dev(np.concatenate([np.arange(s, s + k) for s, k in zip(self.seen, new)]))
         self.seen = self.seen + new
+        self.held[new > 0] = False
         self.batch = K.Batch(self.n, self.total, int(new.max()), int(self.lens.max()), self.cu.data_ptr(),
                              self.kv_len.data_ptr(), self.table.data_ptr(), self.stride)
         dims = (self.total, self.q_heads, self.shape.head_dim)
@@ -153,6 +158,7 @@ class ServeRun:
             K.evict(self.cache_shape, batch, keeps.data_ptr(), score, score, self.max_kv, self.k_ptrs[i], self.v_ptrs[i],
                     left.data_ptr(), self._workspace(need), need, protect=protect.data_ptr(), pos_in=pos, pos_out=pos,
                     pos_stride=self.max_kv, stream=self._stream())
+        self.held[self.lens > keep] = False
         self.lens = np.minimum(self.lens, keep)
 
     def close(self) -> None:

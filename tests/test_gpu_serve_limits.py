@@ -79,3 +79,28 @@ def test_recent_tokens_fit_what_is_kept(make):
     for s, n in enumerate((303, 78)):
         for h in range(2):
             assert sorted(run.pos[0, s, h, :9].tolist()) == list(range(n - 9, n))
+
+
+def test_only_what_the_pool_has_is_fetched(make):
+    """A request of fewer tokens in as many blocks would overwrite the newer ones."""
+    run = make([300, 77], 64)
+    with pytest.raises(ValueError):
+        run.fetch()                                    # nothing is in the pool yet
+    run.offload()
+    run.fetch()
+    _step(run, [0, 2])                                 # 79 tokens lie in as many blocks as 77
+    before = run.cache.clone()
+    with pytest.raises(ValueError, match="1"):
+        run.fetch()
+    assert torch.equal(run.cache, before)
+    run.offload()
+    run.cache.zero_()
+    run.fetch()
+    slot = torch.from_numpy(np.repeat(run.tables[1], 16)[:79].astype(np.int64)).cuda()
+    off = torch.arange(79, device="cuda") % 16
+    assert torch.equal(run.cache[0][:, slot, :, off], before[0][:, slot, :, off])
+    run.evict(300, recent=4)                           # nothing to evict
+    run.fetch()
+    run.evict(299, recent=4)
+    with pytest.raises(ValueError, match="0"):
+        run.fetch()
