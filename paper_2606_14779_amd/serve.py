@@ -79,16 +79,18 @@ class ServeRun:
 
     # ---- the pool's side
     def offload(self) -> None:
-        """Stores every sequence's cached tokens as a request of their own; a request from before is released."""
+        """Stores every sequence's cached tokens as a request of their own; a request from before is released.  A
+        sequence without tokens has none."""
         for i in range(self.n):
+            request = None
             blocks = -(-int(self.lens[i]) // self.shape.block_size)
-            loc_map = self.pool.place(self._next_request, blocks)
-            self.pool.store(loc_map, self.tables[i][:blocks], self.slots, self.k_ptrs, self.v_ptrs, self._stream())
+            if blocks:
+                request, self._next_request = self._next_request, self._next_request + 1
+                loc_map = self.pool.place(request, blocks)
+                self.pool.store(loc_map, self.tables[i][:blocks], self.slots, self.k_ptrs, self.v_ptrs, self._stream())
             if self.requests[i] is not None:
                 self.pool.release(self.requests[i])
-            self.requests[i] = self._next_request
-            self._next_request += 1
-            self.held[i] = True
+            self.requests[i], self.held[i] = request, True
 
     def fetch(self) -> None:
         """Brings every sequence's cached tokens back from the pool, where they have not changed since ``offload``."""
@@ -96,8 +98,9 @@ class ServeRun:
             raise ValueError("sequences %s have changed since they were offloaded" % np.flatnonzero(~self.held).tolist())
         for i in range(self.n):
             blocks = -(-int(self.lens[i]) // self.shape.block_size)
-            self.pool.retrieve_request(self.requests[i], self.tables[i][:blocks], self.slots, self.k_ptrs, self.v_ptrs,
-                                       self._stream())
+            if blocks:
+                self.pool.retrieve_request(self.requests[i], self.tables[i][:blocks], self.slots, self.k_ptrs, self.v_ptrs,
+                                           self._stream())
 
     # ---- the operators' side
     def begin(self, new) -> None:

@@ -104,3 +104,19 @@ def test_only_what_the_pool_has_is_fetched(make):
     run.evict(299, recent=4)
     with pytest.raises(ValueError, match="0"):
         run.fetch()
+
+
+def test_sequences_without_tokens(make):
+    """A request that has just begun, and one of which eviction left nothing."""
+    run = make([0, 77], 64)
+    run.offload()
+    run.fetch()
+    _step(run, [5, 0])
+    run.evict(0, recent=0)
+    assert run.lens.tolist() == [0, 0]
+    run.offload()                                      # the request of 77 tokens is released
+    assert run.requests == [None, None]
+    run.fetch()
+    assert torch.isfinite(_step(run, [1, 2])).all() and run.positions.tolist() == [5, 77, 78]
+    run.offload()
+    run.fetch()
