@@ -54,9 +54,8 @@ class ServeRun:
         per_head = (shape.layers, n, shape.kv_heads, self.max_kv)
         self.score = torch.zeros(per_head, dtype=torch.float32, device=self.device)
         self.pos = torch.arange(self.max_kv, dtype=torch.int32, device=self.device).expand(per_head).contiguous()
-        self.n_positions, self.rot = self.max_kv + room, shape.head_dim
-        self.angles = torch.empty((self.n_positions, self.rot // 2, 2), dtype=torch.float32, device=self.device)
-        K.rope_table(self.angles.data_ptr(), self.n_positions, self.rot, stream=self._stream(), **(rope or {}))
+        self.rot, self.rope = shape.head_dim, dict(rope or {})
+        self._positions_up_to(self.max_kv + room)
         self.cache_shape = K.CacheShape(dtype, q_heads, shape.kv_heads, shape.head_dim, bs, slots)
         spec = K.KVSpec(shape.layers, shape.kv_heads, shape.head_dim, bs, 2)
         held = sum(blocks) * 2 + 2 * n + 2              # twice over, so that a request can be replaced
@@ -71,6 +70,12 @@ class ServeRun:
 
     def _dev(self, a, dtype=None):
         return self.torch.as_tensor(np.ascontiguousarray(a, dtype=dtype or np.int32)).to(self.device)
+
+    def _positions_up_to(self, n: int) -> None:
+        """A table of the angles of positions below n."""
+        self.n_positions = n
+        self.angles = self.torch.empty((n, self.rot // 2, 2), dtype=self.torch.float32, device=self.device)
+        K.rope_table(self.angles.data_ptr(), n, self.rot, stream=self._stream(), **self.rope)
 
     def _workspace(self, need: int) -> int:
         if self._work is None or self._work.numel() < need:
@@ -106,9 +111,10 @@ class ServeRun:
     def begin(self, new) -> None:
         """A step of new[i] tokens of sequence i: its lengths and positions, for all layers."""
         new = np.asarray(new, np.int64)
-        if len(new) != self.n or (new < 0).any() or (self.lens + new > self.most).any() \
-                or (self.seen + new > self.n_positions).any():
+        if len(new) != self.n or (new < 0).any() or (self.lens + new > self.most).any():
             raise ValueError("new tokens do not fit the sequences")
+        if (need := int((self.seen + new).max())) > self.n_positions:   # evicted from, a sequence goes on and on
+            self._positions_up_to(max(need, 2 * self.n_positions))
         self.lens = (self.lens + new).astype(np.int32)
         cu = np.concatenate([[0], np.cumsum(new)])
         self.total, self.cu, self.kv_len = int(cu[-1]), self._dev(cu), self._dev(self.lens)

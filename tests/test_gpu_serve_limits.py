@@ -120,3 +120,23 @@ def test_sequences_without_tokens(make):
     assert torch.isfinite(_step(run, [1, 2])).all() and run.positions.tolist() == [5, 77, 78]
     run.offload()
     run.fetch()
+
+
+def test_decoding_goes_on_after_evictions(make):
+    """Far past the positions that the first lengths and their room make: each new token is rotated by its own."""
+    run = make([300, 77], 32)
+    for i in range(12):                                # 300 + 12 * 32 positions
+        _step(run, [32, 32 if i % 2 else 0], seed=i)
+        run.evict(77, recent=8)
+    assert run.seen.tolist() == [684, 269]
+    g = torch.Generator(device="cuda").manual_seed(99)
+    qkv = torch.randn(2, HEADS + 4, 64, generator=g, device="cuda").to(torch.bfloat16)
+    run.begin([1, 1])
+    run.layer(0, qkv)
+    f = 10000.0 ** (-torch.arange(0, 64, 2, dtype=torch.float64, device="cuda") / 64)
+    a = torch.tensor([684.0, 269.0], dtype=torch.float64, device="cuda")[:, None, None] * f
+    lo, hi = qkv.double()[:, :HEADS, :32], qkv.double()[:, :HEADS, 32:]
+    want = torch.cat([lo * a.cos() - hi * a.sin(), hi * a.cos() + lo * a.sin()], -1)
+    # one rounding to bf16, and cosines and sines in 32 bits
+    size = torch.cat([lo.abs() + hi.abs()] * 2, -1)
+    assert ((run.q.double() - want).abs() <= 2.0 ** -8 * want.abs() * 1.001 + 2.0 ** -22 * size).all()
