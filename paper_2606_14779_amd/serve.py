@@ -75,7 +75,8 @@ class ServeRun:
         """A table of the angles of positions below n."""
         self.n_positions = n
         self.angles = self.torch.empty((n, self.rot // 2, 2), dtype=self.torch.float32, device=self.device)
-        K.rope_table(self.angles.data_ptr(), n, self.rot, stream=self._stream(), **self.rope)
+        with self.torch.cuda.device(self.device):       # the operators launch on the current device
+            K.rope_table(self.angles.data_ptr(), n, self.rot, stream=self._stream(), **self.rope)
 
     def _workspace(self, need: int) -> int:
         if self._work is None or self._work.numel() < need:
@@ -133,6 +134,11 @@ class ServeRun:
         h, hk, d = self.q_heads, self.shape.kv_heads, self.shape.head_dim
         if tuple(qkv.shape) != (self.total, h + 2 * hk, d) or qkv.dtype != self.dtype or not qkv.is_contiguous():
             raise ValueError("qkv is not [total][q_heads + 2 kv_heads][head_dim] of the cache's type")
+        with self.torch.cuda.device(self.device):
+            return self._layer(index, qkv, mass_from)
+
+    def _layer(self, index: int, qkv, mass_from: int):
+        h, hk, d = self.q_heads, self.shape.kv_heads, self.shape.head_dim
         stream, row = self._stream(), (h + 2 * hk) * d
         k_cache, v_cache, scale = self.k_ptrs[index], self.v_ptrs[index], d ** -0.5
         at = qkv.data_ptr()
@@ -164,9 +170,10 @@ class ServeRun:
         need = K.evict_workspace(self.cache_shape, batch)
         for i in range(self.shape.layers):
             score, pos = self.score[i].data_ptr(), self.pos[i].data_ptr()
-            K.evict(self.cache_shape, batch, keeps.data_ptr(), score, score, self.max_kv, self.k_ptrs[i], self.v_ptrs[i],
-                    left.data_ptr(), self._workspace(need), need, protect=protect.data_ptr(), pos_in=pos, pos_out=pos,
-                    pos_stride=self.max_kv, stream=self._stream())
+            with self.torch.cuda.device(self.device):
+                K.evict(self.cache_shape, batch, keeps.data_ptr(), score, score, self.max_kv, self.k_ptrs[i],
+                        self.v_ptrs[i], left.data_ptr(), self._workspace(need), need, protect=protect.data_ptr(),
+                        pos_in=pos, pos_out=pos, pos_stride=self.max_kv, stream=self._stream())
         self.held[self.lens > keep] = False
         self.lens = np.minimum(self.lens, keep)
 
