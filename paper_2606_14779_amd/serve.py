@@ -134,6 +134,8 @@ class ServeRun:
         h, hk, d = self.q_heads, self.shape.kv_heads, self.shape.head_dim
         if tuple(qkv.shape) != (self.total, h + 2 * hk, d) or qkv.dtype != self.dtype or not qkv.is_contiguous():
             raise ValueError("qkv is not [total][q_heads + 2 kv_heads][head_dim] of the cache's type")
+        if qkv.device != self.device:
+            raise ValueError("qkv is on %s, the cache on %s" % (qkv.device, self.device))
         with self.torch.cuda.device(self.device):
             return self._layer(index, qkv, mass_from)
 

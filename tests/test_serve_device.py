@@ -26,7 +26,8 @@ class _Cuda:
         return types.SimpleNamespace(cuda_stream=0)
 
 
-def test_operators_run_on_the_run_s_device(monkeypatch):
+@pytest.fixture
+def run(monkeypatch):
     cuda, called = _Cuda(), []
     for name in ("rope_table", "rope_append", "attention", "attention_mass", "evict"):
         monkeypatch.setattr(serve.K, name, lambda *a, _n=name, **kw: called.append((_n, cuda.current)), raising=False)
@@ -44,9 +45,24 @@ def test_operators_run_on_the_run_s_device(monkeypatch):
     run.held, run._work, run.n_positions = np.ones(1, bool), None, 8
     run.table, run.cache_shape, run.k_ptrs, run.v_ptrs = torch.zeros(1, 4, dtype=torch.int32), None, [0], [0]
     run.score, run.pos = torch.zeros(1, 1, 2, 64), torch.zeros(1, 1, 2, 64, dtype=torch.int32)
+    return run, called, cuda
+
+
+def test_operators_run_on_the_run_s_device(run):
+    run, called, cuda = run
     run.begin([2])                                     # past the 8 positions: a new table
     run.layer(0, types.SimpleNamespace(shape=(2, 12, 64), dtype=run.dtype, device=run.device, is_contiguous=lambda: True,
                                        data_ptr=lambda: 0x10000))
     run.evict(16, recent=4)
     assert called == [(n, 1) for n in ("rope_table", "rope_append", "attention", "attention_mass", "evict")]
     assert cuda.current == 0
+
+
+def test_projections_elsewhere_are_refused(run):
+    """Their address would be followed by kernels on the run's device."""
+    run, called, _ = run
+    run.begin([2])
+    del called[:]
+    with pytest.raises(ValueError, match="cpu"):
+        run.layer(0, torch.zeros(2, 12, 64, dtype=torch.bfloat16))
+    assert not called
