@@ -992,10 +992,9 @@ __global__ __launch_bounds__(kMassWaves * 64, 2) void attention_mass_few(const M
     const uint32_t rows = (uint32_t)s.n_q * c.group;                       // at most 16
     const uint32_t row = rows ? min((uint32_t)col, rows - 1) : 0, token = token_of(c, row);
     const uint32_t head = kv_head * c.group + row - token * c.group;
-    const int32_t limit = s.kv - s.n_q + (int32_t)token;
-    const int64_t floor_key = a.window ? (int64_t)limit + 1 - (int64_t)a.window : 0;
+    int32_t limit = -1;                              // a row past the end, not asked for or without keys: no weight,
+    float lse = 0.0f;                                // whatever its query holds
     w4 q[KS];
-    float lse = INFINITY;                            // a row past the end, or without keys, gives no weight: exp2(-inf)
     if (rows) {
         const uint16_t *p = a.q + (uint64_t)(s.q_begin + token) * a.q_stride + (uint64_t)head * c.head_dim;
 #pragma unroll
@@ -1006,11 +1005,15 @@ __global__ __launch_bounds__(kMassWaves * 64, 2) void attention_mass_few(const M
         }
         const float x = a.lse[(uint64_t)head * c.total_q + s.q_begin + token];
         const bool asked = a.last == 0 || (uint32_t)s.n_q - token <= a.last;
-        if ((uint32_t)col < rows && asked && x > -INFINITY) lse = x * kLog2e;
+        if ((uint32_t)col < rows && asked && x > -INFINITY) {
+            limit = s.kv - s.n_q + (int32_t)token;
+            lse = x * kLog2e;
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < KS; ++i) q[i] = w4{0, 0, 0, 0};
     }
+    const int64_t floor_key = a.window ? (int64_t)limit + 1 - (int64_t)a.window : 0;
     // the first key that any of the asked rows sees: in place of keys before it one row is read, again and again (a
     // branch around the loads would have every step wait for the next one's)
     const int64_t lowest = !rows ? s.kv

@@ -54,3 +54,42 @@ def test_evict_more_protected_tokens_than_are_kept(n):
     assert left == [keep]
     for h in range(2):
         assert sorted(pos[0, h, :keep].tolist()) == list(range(n // 2, n // 2 + keep))
+
+
+# ---- attention mass
+
+def _mass(c, q, lse, scale=0.125, **kw):
+    out = torch.full((len(c.lens), c.kv_heads, c.max_kv), 7.0, dtype=torch.float32, device="cuda")
+    K.attention_mass(c.shape, c.batch, q.data_ptr(), q.stride(0), c.k_cache.data_ptr(), scale, lse.data_ptr(), 0,
+                     out.data_ptr(), c.max_kv, stream=_stream(), **kw)
+    return out
+
+
+def _attend(c, q, scale=0.125, sinks=None, window=0):
+    out = torch.full((c.total, c.heads, c.head_dim), 7.0, dtype=R.DTYPE[c.dtype], device="cuda")
+    lse = torch.full((c.heads, c.total), 7.0, dtype=torch.float32, device="cuda")
+    w, n = c.workspace(K.attention_workspace)
+    K.attention(c.shape, c.batch, q.data_ptr(), q.stride(0), c.k_cache.data_ptr(), c.v_cache.data_ptr(), scale,
+                out.data_ptr(), out.stride(0), window=window, sinks=sinks.data_ptr() if sinks is not None else 0,
+                lse=lse.data_ptr(), workspace=w.data_ptr(), workspace_bytes=n, stream=_stream())
+    return out, lse
+
+
+MASS = {"few": [(4, 200), (3, 70), (1, 9)], "many": [(40, 300), (150, 170), (9, 20)]}
+
+
+@pytest.mark.parametrize("window", [0, 33])
+@pytest.mark.parametrize("lens", list(MASS))
+def test_mass_of_the_asked_queries_alone(lens, window):
+    """What the other queries hold, NaN and infinities among it, is of no concern."""
+    c = R.Case(MASS[lens], heads=8, kv_heads=2, seed=80)
+    q = c.normal(c.total, 8, 64, std=2.0)
+    _, lse = _attend(c, q, window=window)
+    want = _mass(c, q, lse, last=2, window=window)
+    for value in (math.nan, math.inf):
+        other, other_lse = q.clone(), lse.clone()
+        for s, (new, _) in enumerate(c.lens):
+            unasked = slice(int(c.cu_host[s]), int(c.cu_host[s]) + max(0, new - 2))
+            other[unasked, :, 7] = value
+            other_lse[:, unasked] = value
+        assert torch.equal(_mass(c, other, other_lse, last=2, window=window), want)
