@@ -697,7 +697,9 @@ int kv_attention_workspace(const kvp_cache_shape *shape, const kvp_batch *batch,
  * head:
  *   score_out[s][h][j] = score_in[s][h][j] + sum over queries of exp(logit - lse)
  * for j < kv_len[s]; entries from kv_len[s] on are not written.  q, scale and
- * window as in the kv_attention call that made lse.
+ * window as in the kv_attention call that made lse.  A query whose lse is -inf
+ * (it sees nothing) adds nothing; one whose lse is NaN makes the scores of the
+ * tokens that it sees NaN.
  *   score_in     NULL for 0; may be score_out.
  *   score_*[n_seq][num_kv_heads][score_stride]
  * Sums run in a fixed order: the same inputs give the same bits.

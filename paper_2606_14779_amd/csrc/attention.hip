@@ -849,7 +849,7 @@ __global__ __launch_bounds__(kMassWaves * 64, DP > 128 ? 1 : 2) void attention_m
             *(w4 *)&lds[(buf * TR + r) * DP + qp * 8] = rq[i];
         }
         // a row past the end, or without keys, gives no weight: exp2(-inf)
-        if (tid < TR) lds_lse[buf][tid] = r0 + tid < row_end && r_lse > -INFINITY ? r_lse * kLog2e : INFINITY;
+        if (tid < TR) lds_lse[buf][tid] = r0 + tid < row_end && r_lse != -INFINITY ? r_lse * kLog2e : INFINITY;
     };
 
     uint64_t seen = 0;
@@ -1005,7 +1005,7 @@ __global__ __launch_bounds__(kMassWaves * 64, 2) void attention_mass_few(const M
         }
         const float x = a.lse[(uint64_t)head * c.total_q + s.q_begin + token];
         const bool asked = a.last == 0 || (uint32_t)s.n_q - token <= a.last;
-        if ((uint32_t)col < rows && asked && x > -INFINITY) {
+        if ((uint32_t)col < rows && asked && x != -INFINITY) {
             limit = s.kv - s.n_q + (int32_t)token;
             lse = x * kLog2e;
         }

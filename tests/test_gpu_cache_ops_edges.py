@@ -93,3 +93,23 @@ def test_mass_of_the_asked_queries_alone(lens, window):
             other[unasked, :, 7] = value
             other_lse[:, unasked] = value
         assert torch.equal(_mass(c, other, other_lse, last=2, window=window), want)
+
+
+@pytest.mark.parametrize("window", [0, 33])
+@pytest.mark.parametrize("lens", list(MASS))
+def test_mass_of_a_row_that_is_not_a_number(lens, window):
+    """exp(logit - NaN): the tokens that the row sees show it, and no others."""
+    c = R.Case(MASS[lens], heads=8, kv_heads=2, seed=81)
+    q = c.normal(c.total, 8, 64, std=2.0)
+    _, lse = _attend(c, q, window=window)
+    want = _mass(c, q, lse, window=window)
+    new, kv = c.lens[0]
+    row = new - 2
+    lse[5, row] = math.nan                            # a head of the second KV head
+    got = _mass(c, q, lse, window=window)
+    index = kv - new + row
+    sees = torch.zeros_like(got, dtype=torch.bool)
+    sees[0, 1, max(0, index - window + 1) if window else 0:index + 1] = True
+    assert torch.isnan(got[sees]).all() and torch.equal(got[~sees], want[~sees])
+    lse[5, row] = -math.inf                           # as a row that sees nothing
+    assert torch.isfinite(_mass(c, q, lse, window=window)).all()
