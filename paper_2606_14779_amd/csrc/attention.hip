@@ -330,10 +330,12 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
 #pragma unroll
         for (int r = 0; r < 16; ++r) top = fmaxf(top, z[1][r]);
         top = fmaxf(top, other_half(top)) * a.scale_log2;
-        // The maximum moves only when it is passed by 2^8: weights up to 2^8 lose nothing in 32 bits, nor when
-        // rounded to 16 (their sum and the output keep the same factor), and rescaling becomes rare.
-        if (__builtin_expect(__any(top > m + 8.0f), 0)) {
-            const float to = fmaxf(m, top);
+        // m moves only when the maximum has passed it by 2^8, and then to the maximum: weights up to 2^8 lose nothing in
+        // 32 bits, nor when rounded to 16 (their sum and the output keep the same factor), and rescaling becomes rare.
+        // A 16-bit float ends at 2^-25, where weights would still be in the sum and no longer in the output, and has
+        // room up to 2^16: m stays 2^7 below the maximum, so that weights run from 2^-32 of the largest to 2^15.
+        if (__builtin_expect(__any(top > m + (8.0f + T::kLift)), 0)) {
+            const float to = fmaxf(m, top - T::kLift);
             const float f = exp2_fast(m - to);
             m = to;
             l *= f;
@@ -608,8 +610,8 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attention_few(const Attenti
         for (int r = 0; r < 4; ++r) top = fmaxf(top, z[1][r]);
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, other_half(top)) * a.scale_log2;
-        if (__any(top > m + 8.0f)) {
-            const float to = fmaxf(m, top);
+        if (__any(top > m + (8.0f + T::kLift))) {    // as in attention_rows
+            const float to = fmaxf(m, top - T::kLift);
             const float f = exp2_fast(m - to);
             m = to;
             l *= f;

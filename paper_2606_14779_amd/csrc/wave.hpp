@@ -36,7 +36,9 @@ __device__ __forceinline__ bool finite_to(w4 x, uint32_t exponent)
     return all;
 }
 
+// kLift: what the reference point of a row's weights lies below their maximum, in powers of two (see the softmax).
 struct BF16 {
+    static constexpr float kLift = 0.0f;
     typedef __bf16 x8 __attribute__((ext_vector_type(8)));
     typedef __bf16 x2 __attribute__((ext_vector_type(2)));
     static __device__ __forceinline__ v16f mma32(w4 a, w4 b, v16f c)
@@ -60,6 +62,7 @@ struct BF16 {
 };
 
 struct F16 {
+    static constexpr float kLift = 7.0f;
     typedef _Float16 x8 __attribute__((ext_vector_type(8)));
     typedef _Float16 x2 __attribute__((ext_vector_type(2)));
     static __device__ __forceinline__ v16f mma32(w4 a, w4 b, v16f c)

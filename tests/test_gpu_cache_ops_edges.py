@@ -113,3 +113,34 @@ def test_mass_of_a_row_that_is_not_a_number(lens, window):
     assert torch.isnan(got[sees]).all() and torch.equal(got[~sees], want[~sees])
     lse[5, row] = -math.inf                           # as a row that sees nothing
     assert torch.isfinite(_mass(c, q, lse, window=window)).all()
+
+
+# ---- attention
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("new", [1, 17])
+def test_attention_of_many_weights_far_below_the_largest(new, dtype):
+    """One key of weight 1 and 131071 of about 2^-25.5, the values of which lie in other elements than its own.
+
+    So many heads that a workgroup has 65536 keys or all of them.  What those elements hold is off by the rounding of the
+    small weights, all alike, which 16-bit floats hold to 2^-32 of the largest: 2^-6.5 relative; by up to 2^17 roundings
+    of a sum in 32 bits, 2^-24 each; and, as the element of the large weight, by what the sum of weights loses of the
+    small ones beside it, 2^17 of 2^-25.5 at most; by the rounding of the output and of the large weight, eps each."""
+    n, heads = 131072, 512
+    c = R.Case([(new, n)], heads=heads, kv_heads=heads, head_dim=8, dtype=dtype, seed=90)
+    c.k_cache.zero_()
+    c.v_cache.fill_(1.0)
+    c.v_cache[..., 0] = 0.0
+    slot = int(c.true_table[0, 0])
+    c.k_cache[slot, :, 0, 0] = 8.84
+    c.v_cache[slot, :, 0] = 0.0
+    c.v_cache[slot, :, 0, 0] = 1.0
+    q = torch.zeros(new, heads, 8, dtype=R.DTYPE[dtype], device="cuda")
+    q[..., 0] = 16.0
+    out, _ = _attend(c, q)
+    weight = math.exp(-16.0 * c.k_cache[slot, 0, 0, 0].item() * 0.125)
+    small = torch.arange(n - new, n, dtype=torch.float64, device="cuda")[:, None, None] * weight    # together, for each row
+    lost = n * weight + 2 * R.EPS[dtype]
+    assert ((out[..., :1].double() * (1 + small) - 1).abs() <= lost).all()
+    off = (out[..., 1:].double() * (1 + small) / small - 1).abs().max().item()
+    assert off <= 2.0 ** -6.5 + 2.0 ** -7 + lost, off
