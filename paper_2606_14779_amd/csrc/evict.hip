@@ -431,8 +431,15 @@ __global__ __launch_bounds__(256) void evict_move(const EvictArgs a, const uint3
     const int32_t *table = c.table + (uint64_t)seq * c.table_stride;
     if (group == 0 && head == 0 && threadIdx.x == 0) a.len_out[seq] = (int32_t)left;
     const uint64_t sl = (uint64_t)list * a.score_stride, pl = (uint64_t)list * a.pos_stride;
-    for (uint32_t u = group * 256 + threadIdx.x; u < count * pieces; u += groups * 256) {
-        const uint32_t i = u / pieces, piece = u - i * pieces;
+    // move i, piece of it: their product may pass 32 bits
+    const uint32_t begin = group * 256 + threadIdx.x, step = groups * 256;
+    const uint32_t step_i = step / pieces, step_piece = step % pieces;
+    uint32_t i = begin / pieces, piece = begin % pieces;
+    for (; i < count; i += step_i, piece += step_piece) {
+        if (piece >= pieces) {
+            piece -= pieces;
+            if (++i >= count) break;
+        }
         const uint32_t hole = lists.pairs[2 * (uint64_t)i], mover = lists.pairs[2 * (uint64_t)i + 1];
         if (piece == 0) {
             const float x = a.score_in[sl + mover];
@@ -450,7 +457,7 @@ __global__ __launch_bounds__(256) void evict_move(const EvictArgs a, const uint3
         *(w4 *)(a.v_cache + d) = v;
     }
     const bool copies = a.score_out != a.score_in || (a.pos_out && a.pos_out != a.pos_in);
-    for (uint32_t i = group * 256 + threadIdx.x; i < n; i += groups * 256) {
+    for (i = begin; i < n; i += step) {
         if (i < left && !copies) continue;
         const bool kept = n <= keep || (lists.kept[i >> 6] >> (i & 63) & 1);
         if (i >= left && !kept) a.score_out[sl + i] = 0.0f;

@@ -56,6 +56,18 @@ def test_evict_more_protected_tokens_than_are_kept(n):
         assert sorted(pos[0, h, :keep].tolist()) == list(range(n // 2, n // 2 + keep))
 
 
+def test_evict_a_list_of_2_28_tokens():
+    """2^27 moves of 32 pieces each: as many as 32 bits count. The slots are absent, so that only scores move."""
+    n, keep = 1 << 28, 1 << 27
+    c = R.Case([(0, 0)], kv_heads=1, heads=1, head_dim=256, block=1 << 15, spare=1, max_kv=n, seed=71)
+    c.kv_len.fill_(n)
+    score = torch.zeros(1, 1, n, dtype=torch.float32, device="cuda")
+    score[..., keep:] = 1.0
+    _, _, left = _evict(c, [keep], score)
+    assert left == [keep]
+    assert (score[..., :keep] == 1.0).all() and (score[..., keep:] == 0.0).all()
+
+
 # ---- attention mass
 
 def _mass(c, q, lse, scale=0.125, **kw):
