@@ -36,6 +36,18 @@ __device__ __forceinline__ bool finite_to(w4 x, uint32_t exponent)
     return all;
 }
 
+// Puts 0 in the place of those that are not; whether there were none.
+__device__ __forceinline__ bool bound_to(w4 &x, uint32_t exponent)
+{
+    const bool all = finite_to(x, exponent);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if ((x[i] & exponent) == exponent) x[i] &= 0xFFFF0000u;
+        if ((x[i] >> 16 & exponent) == exponent) x[i] &= 0xFFFFu;
+    }
+    return all;
+}
+
 // kLift: what the reference point of a row's weights lies below their maximum, in powers of two (see the softmax).
 struct BF16 {
     static constexpr float kLift = 0.0f;
@@ -59,6 +71,7 @@ struct BF16 {
         return __builtin_bit_cast(float, i ? (w & 0xFFFF0000u) : (w << 16));
     }
     static __device__ __forceinline__ bool finite(w4 x) { return finite_to(x, 0x7F80u); }
+    static __device__ __forceinline__ bool bound(w4 &x) { return bound_to(x, 0x7F80u); }
 };
 
 struct F16 {
@@ -83,9 +96,11 @@ struct F16 {
         return (float)__builtin_bit_cast(x2, w)[i];
     }
     static __device__ __forceinline__ bool finite(w4 x) { return finite_to(x, 0x7C00u); }
+    static __device__ __forceinline__ bool bound(w4 &x) { return bound_to(x, 0x7C00u); }
 };
 
 __device__ __forceinline__ w4 load16g(const uint16_t *p) { return *(gw4 *)p; }
+__device__ __forceinline__ w2 load8g(const uint16_t *p) { return *(__attribute__((address_space(1))) const w2 *)p; }
 __device__ __forceinline__ int32_t load4g(const int32_t *p) { return *(gi32 *)p; }
 
 // Orders a wave's own accesses of LDS, which the hardware keeps in order, for the compiler.

@@ -156,3 +156,65 @@ def test_attention_of_many_weights_far_below_the_largest(new, dtype):
     assert ((out[..., :1].double() * (1 + small) - 1).abs() <= lost).all()
     off = (out[..., 1:].double() * (1 + small) / small - 1).abs().max().item()
     assert off <= 2.0 ** -6.5 + 2.0 ** -7 + lost, off
+
+
+BESIDE = {"single token": [(1, 9001)], "few": [(3, 700), (2, 65), (1, 1)], "many": [(100, 3000), (40, 41), (300, 300)]}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("window", [0, 50])
+@pytest.mark.parametrize("head_dim", [64, 72, 128, 200])
+@pytest.mark.parametrize("lens", list(BESIDE))
+def test_attention_beside_values_that_are_not_finite(lens, head_dim, window, dtype):
+    """The rows that see such a value have it in its element, infinities with their signs, and every other result has
+    the bits that it has with any finite value there.
+
+    Logits are below 2^3, so that every weight is far from 0 in both types."""
+    c = R.Case(BESIDE[lens], heads=8, kv_heads=2, head_dim=head_dim, dtype=dtype, seed=91)
+    q, scale = c.normal(c.total, 8, head_dim, std=0.5), head_dim ** -0.5
+    want, want_lse = _attend(c, q, scale, window=window)
+    expected = want.float()
+    for s, (new, kv) in enumerate(c.lens):
+        slot, off = c.places(s, kv)
+        first = int(c.cu_host[s])
+        index = torch.arange(kv - new, kv, device="cuda")
+        for back, d, value in ((1, 3, math.inf), (2, 3, math.inf), (1, head_dim - 1, math.nan), (3, 0, -math.inf),
+                               (new, 11, -math.inf), (new + 1, 12, math.inf), (new + 1, 13, -math.inf)):
+            at = kv - back
+            if at < 0:
+                continue
+            c.v_cache[slot[at], 1, off[at], d] = value
+            sees = (index >= at) & ((index - at < window) if window else True)
+            rows = expected[first:first + new, 4:, d]
+            rows[sees] = torch.where(torch.isinf(rows[sees]) & (rows[sees] != value), math.nan,
+                                     torch.where(torch.isnan(rows[sees]), math.nan, value))
+    out, lse = _attend(c, q, scale, window=window)
+    assert torch.equal(lse, want_lse)
+    assert torch.equal(torch.isnan(out), torch.isnan(expected))
+    assert torch.equal(out.float().nan_to_num(7.0, math.inf, -math.inf), expected.nan_to_num(7.0, math.inf, -math.inf))
+
+
+@pytest.mark.parametrize("lens", [[(1, 65537)], [(256, 65536)], [(4, 65536), (1, 30)]], ids=str)
+def test_attention_costs_no_more_beside_a_value_that_is_not_finite(lens):
+    """One infinity among the newest token's values: a call of up to three times the other's time, where going over all
+    keys of its rows once more would take 30 and more."""
+    c = R.Case(lens, heads=32, kv_heads=8, head_dim=128, seed=92)
+    q = c.normal(c.total, 32, 128)
+
+    def took():
+        times = []
+        for _ in range(5):
+            begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            begin.record()
+            _attend(c, q)
+            end.record()
+            end.synchronize()
+            times.append(begin.elapsed_time(end))
+        return min(times)
+
+    took()
+    without = took()
+    slot, off = c.places(0, lens[0][1])
+    c.v_cache[slot[-1], 3, off[-1], 5] = math.inf
+    beside = took()
+    assert beside <= 3 * without + 0.05, "%.3f ms, %.3f without" % (beside, without)
