@@ -688,7 +688,8 @@ int kv_attention(const kvp_cache_shape *shape, const kvp_batch *batch, const voi
                  const void *k_cache, const void *v_cache, float scale, uint32_t window, const float *sinks,
                  void *out, uint64_t out_stride, float *lse, void *workspace, uint64_t workspace_bytes, void *stream);
 
-/* Bytes of workspace that kv_attention needs for this shape and batch (only its four sizes count); may be 0. */
+/* Bytes of workspace that kv_attention needs for this shape and batch; may be 0.  Of the batch only n_seq, total_q,
+ * max_q and max_kv are looked at: its arrays need not be there yet. */
 int kv_attention_workspace(const kvp_cache_shape *shape, const kvp_batch *batch, uint64_t *bytes);
 
 /*
@@ -735,7 +736,7 @@ int kv_evict(const kvp_cache_shape *shape, const kvp_batch *batch, const int32_t
              uint32_t pos_stride, void *k_cache, void *v_cache, int32_t *len_out, void *workspace,
              uint64_t workspace_bytes, void *stream);
 
-/* Bytes of workspace that kv_evict needs for this shape and batch. */
+/* Bytes of workspace that kv_evict needs for this shape and batch, of which only n_seq and max_kv are looked at. */
 int kv_evict_workspace(const kvp_cache_shape *shape, const kvp_batch *batch, uint64_t *bytes);
 
 #ifdef __cplusplus

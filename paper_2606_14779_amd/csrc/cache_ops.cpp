@@ -37,8 +37,9 @@ void divide_by(uint32_t d, uint32_t *magic, uint32_t *shift)
 // What a launch's grid can count, with room: new tokens times query heads, sequences times KV heads, parts of a call.
 constexpr uint64_t kMostRows = 1ull << 29, kMostLists = 1ull << 18, kMostParts = 1ull << 22;
 
-// Checks the shape and the batch; queries says whether cu_q is used.
-CacheView view_of(const kvp_cache_shape *s, const kvp_batch *b, bool queries)
+// Checks the shape and the batch; queries says whether cu_q is used, arrays whether the batch's arrays are (a workspace
+// is asked for by sizes alone).
+CacheView view_of(const kvp_cache_shape *s, const kvp_batch *b, bool queries, bool arrays = true)
 {
     need(s && b, "null argument");
     need(s->dtype == KVP_BF16 || s->dtype == KVP_F16, "dtype is neither KVP_BF16 nor KVP_F16");
@@ -51,14 +52,16 @@ CacheView view_of(const kvp_cache_shape *s, const kvp_batch *b, bool queries)
     need((uint64_t)s->num_slots * s->num_kv_heads <= 0xFFFFFFFEull / s->block_size, "a cache of 2^32 rows or more");
     need(s->reserved == 0 && b->reserved == 0, "reserved fields are not 0");
     need(b->max_kv <= 1u << 30 && b->max_q <= 1u << 30 && b->total_q <= 1u << 30, "a length of more than 2^30");
-    need((uint64_t)b->table_stride * s->block_size >= b->max_kv, "table_stride * block_size is less than max_kv");
+    need(!arrays || (uint64_t)b->table_stride * s->block_size >= b->max_kv, "table_stride * block_size is less than max_kv");
     need((uint64_t)b->n_seq * s->num_kv_heads <= kMostLists, "more than 2^18 sequences times KV heads");
     CacheView c{};
     if (b->n_seq) {
-        need_pointer(b->kv_len, 4, "kv_len");
-        if (b->max_kv) need_pointer(b->block_table, 4, "block_table");
+        if (arrays) {
+            need_pointer(b->kv_len, 4, "kv_len");
+            if (b->max_kv) need_pointer(b->block_table, 4, "block_table");
+            if (queries) need_pointer(b->cu_q, 4, "cu_q");
+        }
         if (queries) {
-            need_pointer(b->cu_q, 4, "cu_q");
             need(b->max_q <= b->total_q, "max_q is more than total_q");
             need((uint64_t)b->total_q * s->num_q_heads <= kMostRows, "more than 2^29 new tokens times query heads");
         }
@@ -167,7 +170,7 @@ void need_scale(float scale) { need(std::isfinite(scale) && scale > 0, "scale is
 void op_attention_workspace(const kvp_cache_shape *s, const kvp_batch *b, uint64_t *bytes)
 {
     need(bytes, "bytes is null");
-    *bytes = attention_bytes(view_of(s, b, true));
+    *bytes = attention_bytes(view_of(s, b, true, false));
 }
 
 void op_attention(const kvp_cache_shape *s, const kvp_batch *b, const void *q, uint64_t q_stride, const void *k,
@@ -338,7 +341,7 @@ void op_rope_table(float *angles, uint32_t n_positions, uint32_t rot, const kvp_
 void op_evict_workspace(const kvp_cache_shape *s, const kvp_batch *b, uint64_t *bytes)
 {
     need(bytes, "bytes is null");
-    *bytes = evict_bytes(view_of(s, b, false));
+    *bytes = evict_bytes(view_of(s, b, false, false));
 }
 
 void op_evict(const kvp_cache_shape *s, const kvp_batch *b, const int32_t *keep, const int32_t *protect,
