@@ -617,7 +617,9 @@ typedef struct {
  * block_table[s * table_stride + j / block_size]; an entry outside
  * [0, num_slots) is absent: no query sees its tokens and nothing is written
  * there.  A sequence may have no new token, or no cached one.  At most 2^18
- * sequences times KV heads and 2^29 new tokens times query heads in a call.
+ * sequences times KV heads and 2^29 new tokens times query heads in a call;
+ * kv_rope_append takes less than 2^24 new tokens, and kv_attention_mass less
+ * than 2^24 of n_seq * num_kv_heads * ceil(max_kv / 128).
  */
 typedef struct {
     uint32_t n_seq;
@@ -631,12 +633,14 @@ typedef struct {
     const int32_t *block_table; /* [n_seq][table_stride] */
 } kvp_batch;
 
-/* How rotary frequencies f_j = base^(-2j / rot_dim) are scaled for contexts longer than the trained one. */
+/* How rotary frequencies f_j = base^(-2j / rot_dim) are scaled for contexts longer than the trained one.  Another
+ * scaling, such as one whose indexes of alpha and beta are rounded to whole numbers, is a table that the caller fills. */
 #define KVP_ROPE_PLAIN          0u  /* not at all */
 #define KVP_ROPE_LINEAR         1u  /* all: f / factor */
 #define KVP_ROPE_BY_PARTS       2u  /* f (g + (1 - g) / factor); with r the turns that f makes over original_length,
                                        g = (r - alpha) / (beta - alpha), limited to [0, 1] */
-#define KVP_ROPE_BY_PARTS_INDEX 3u  /* the same with g linear in j instead: 1 where f_j makes beta turns, 0 where alpha */
+#define KVP_ROPE_BY_PARTS_INDEX 3u  /* the same with g linear in j instead: 1 where f_j makes beta turns, 0 where alpha;
+                                       these two j are neither rounded nor limited to the indexes that there are */
 typedef struct {
     uint32_t kind;            /* KVP_ROPE_* above */
     uint32_t reserved;        /* 0 */
