@@ -144,15 +144,16 @@ __global__ __launch_bounds__(256) void rope_append(const RopeArgs a)
 // cos and sin of position * frequency: revolutions in 64 bits, reduced before the functions are taken.
 __global__ __launch_bounds__(256) void rope_table(const RopeTableArgs a)
 {
-    const uint64_t idx = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-    const uint64_t position = idx / a.half;
-    if (position >= a.n_positions) return;
-    const uint32_t j = (uint32_t)(idx - position * a.half);
-    double t = (double)position * a.turns[j];
-    t -= rint(t);
-    double s, c;
-    sincospi(2.0 * t, &s, &c);
-    *(v2f *)(a.angles + 2 * idx) = v2f{(float)(c * a.magnitude), (float)(s * a.magnitude)};
+    const uint64_t pairs = (uint64_t)a.n_positions * a.half;
+    for (uint64_t idx = (uint64_t)blockIdx.x * 256 + threadIdx.x; idx < pairs; idx += (uint64_t)gridDim.x * 256) {
+        const uint64_t position = idx / a.half;
+        const uint32_t j = (uint32_t)(idx - position * a.half);
+        double t = (double)position * a.turns[j];
+        t -= rint(t);
+        double s, c;
+        sincospi(2.0 * t, &s, &c);
+        *(v2f *)(a.angles + 2 * idx) = v2f{(float)(c * a.magnitude), (float)(s * a.magnitude)};
+    }
 }
 
 }  // namespace
@@ -179,8 +180,9 @@ hipError_t launch_rope(const RopeArgs &a, uint32_t dtype, hipStream_t stream)
 
 hipError_t launch_rope_table(const RopeTableArgs &a, hipStream_t stream)
 {
-    const uint32_t grid = (uint32_t)(((uint64_t)a.n_positions * a.half + 255) / 256);
-    rope_table<<<grid, 256, 0, stream>>>(a);
+    // a pair to a thread; a launch has less than 2^32 threads, larger tables are gone over in steps
+    const uint64_t groups = ((uint64_t)a.n_positions * a.half + 255) / 256;
+    rope_table<<<(uint32_t)(groups < 1u << 22 ? groups : 1u << 22), 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 

@@ -218,3 +218,22 @@ def test_attention_costs_no_more_beside_a_value_that_is_not_finite(lens):
     c.v_cache[slot[-1], 3, off[-1], 5] = math.inf
     beside = took()
     assert beside <= 3 * without + 0.05, "%.3f ms, %.3f without" % (beside, without)
+
+
+# ---- rotary positions
+
+def test_rope_table_of_more_than_2_32_pairs():
+    """34 GB, more pairs than a launch has threads."""
+    n, rot, base = (1 << 26) + 3, 128, 500000.0
+    table = torch.full((n, rot // 2, 2), 7.0, dtype=torch.float32, device="cuda")
+    K.rope_table(table.data_ptr(), n, rot, base=base, stream=_stream())
+    at = torch.tensor([0, 1, 12345, (1 << 24) + 1, (1 << 26) - 1, n - 2, n - 1], device="cuda")
+    f = base ** (-2.0 * torch.arange(rot // 2, dtype=torch.float64, device="cuda") / rot)
+    angle = at.double()[:, None] * f
+    want = torch.stack([angle.cos(), angle.sin()], -1)
+    # rounding to 32 bits, and 2^-51 relative in angles of up to 2^26
+    assert (table[at].double() - want).abs().max().item() <= 2.0 ** -24 + 2.0 ** -25
+    for part in table.split(1 << 24):
+        assert (part != 7.0).all()
+    del table
+    torch.cuda.empty_cache()
