@@ -48,7 +48,9 @@ __device__ __forceinline__ w4 turn_anyhow(const uint16_t *x, uint32_t at, uint32
     return out;
 }
 
-__device__ __forceinline__ v4f load4f(const float *p) { return *(__attribute__((address_space(1))) const v4f *)p; }
+// Four floats of a table, which is 8-byte aligned.
+typedef float v4f_at8 __attribute__((ext_vector_type(4), aligned(8)));
+__device__ __forceinline__ v4f load4f(const float *p) { return *(__attribute__((address_space(1))) const v4f_at8 *)p; }
 
 // A token to a workgroup.  What it loads and stores of its heads does not wait for its place in the cache: that
 // takes a search among the sequences, their lengths and the block table, one after the other.

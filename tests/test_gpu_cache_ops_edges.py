@@ -237,3 +237,22 @@ def test_rope_table_of_more_than_2_32_pairs():
         assert (part != 7.0).all()
     del table
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rope_append_from_a_table_aligned_to_8_bytes(interleaved):
+    c = R.Case([(5, 90), (1, 1)], heads=8, kv_heads=2, seed=100)
+    q, k, v = c.normal(6, 8, 64), c.normal(6, 2, 64), c.normal(6, 2, 64)
+    angle = torch.rand(100, 32, generator=c.g, device="cuda") * 6.28
+    table = torch.stack([angle.cos(), angle.sin()], -1).contiguous()
+    room, positions = torch.zeros(table.numel() + 4, device="cuda"), _dev([99, 3, 50, 7, 0, 64])
+    results = []
+    for at in (0, 2):                                  # floats past an aligned address
+        room[at:at + table.numel()] = table.flatten()
+        out = torch.zeros_like(q)
+        k_cache, v_cache = torch.zeros_like(c.k_cache), torch.zeros_like(c.v_cache)
+        K.rope_append(c.shape, c.batch, room.data_ptr() + 4 * at, 100, 64, positions.data_ptr(), k.data_ptr(), 128, v.data_ptr(),
+                      128, k_cache.data_ptr(), v_cache.data_ptr(), q=q.data_ptr(), q_stride=512, q_out=out.data_ptr(), q_out_stride=512,
+                      interleaved=interleaved, stream=_stream())
+        results.append((out, k_cache, v_cache))
+    assert all(torch.equal(a, b) for a, b in zip(*results)) and results[0][0].abs().sum().item() > 0
