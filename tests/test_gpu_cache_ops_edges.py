@@ -9,6 +9,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 import cache_ops_ref as R   # noqa: E402
+import test_gpu_cache_ops as T   # noqa: E402
 from paper_2606_14779_amd import kvpool as K   # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -256,3 +257,69 @@ def test_rope_append_from_a_table_aligned_to_8_bytes(interleaved):
                       interleaved=interleaved, stream=_stream())
         results.append((out, k_cache, v_cache))
     assert all(torch.equal(a, b) for a, b in zip(*results)) and results[0][0].abs().sum().item() > 0
+
+
+@pytest.mark.parametrize("n_seq", [64, 65, 5000])
+def test_rope_append_to_many_sequences(n_seq):
+    """Each token finds its own sequence among others with none, one or several."""
+    rng = np.random.default_rng(101)
+    new = rng.choice([0, 0, 1, 1, 2, 9], n_seq)
+    new[[0, -1]] = 0, 3                                # the first and the last but one have none
+    new[-2] = 0
+    cached = new + rng.integers(0, 20, n_seq)
+    c = R.Case([(int(a), int(b)) for a, b in zip(new, cached)], heads=2, kv_heads=2, head_dim=8, block=4, seed=101)
+    k, v = c.normal(c.total, 2, 8), c.normal(c.total, 2, 8)
+    seq = np.repeat(np.arange(n_seq), new)
+    at = np.arange(c.total) - c.cu_host[seq] + cached[seq] - new[seq]
+    slot, off = (torch.from_numpy(x.astype(np.int64)).cuda() for x in (c.true_table[seq, at // 4], at % 4))
+    want_k, want_v = c.k_cache.clone(), c.v_cache.clone()
+    want_k[slot, :, off], want_v[slot, :, off] = k, v
+    positions = torch.from_numpy(at.astype(np.int32)).cuda()
+    pos = torch.full((n_seq, 2, c.max_kv), -5, dtype=torch.int32, device="cuda")
+    want_pos = pos.clone()
+    want_pos[torch.from_numpy(seq).cuda(), :, positions.long()] = positions[:, None].expand(-1, 2)
+    K.rope_append(c.shape, c.batch, 0, 100, 0, positions.data_ptr(), k.data_ptr(), 16, v.data_ptr(), 16, c.k_cache.data_ptr(),
+                  c.v_cache.data_ptr(), pos=pos.data_ptr(), pos_stride=c.max_kv, stream=_stream())
+    assert torch.equal(c.k_cache.view(torch.int16), want_k.view(torch.int16))
+    assert torch.equal(c.v_cache.view(torch.int16), want_v.view(torch.int16))
+    assert torch.equal(pos, want_pos)
+
+
+# ---- batches and lists larger than those of the other tests
+
+def _ragged(n_seq, rng):
+    """More than 16 rows in some sequences and none in others, one long; in no order."""
+    new = rng.choice([0, 1, 3, 17, 40, 70], n_seq)
+    cached = np.maximum(0, new + rng.integers(-5, 150, n_seq))     # some new tokens see nothing
+    lens = [(int(a), int(b)) for a, b in zip(new, cached)]
+    lens[n_seq // 2] = (300, 1500)
+    return lens
+
+
+@pytest.mark.parametrize("window", [0, 65])
+@pytest.mark.parametrize("n_seq", [64, 65, 150])
+def test_attention_and_mass_of_many_ragged_sequences(n_seq, window):
+    """Row tiles found by their lengths (up to 64 sequences), and one sequence after the other."""
+    c = R.Case(_ragged(n_seq, np.random.default_rng(110)), heads=4, kv_heads=2, head_dim=64, seed=110)
+    q, lse = T.check_attention(c, window=window)[::2]
+    want, tol = R.mass(c, q, 0.125, lse, last=20, window=window)
+    got = _mass(c, q, lse, last=20, window=window)
+    for s, (_, kv) in enumerate(c.lens):
+        assert ((got[s, :, :kv].double() - want[s, :, :kv]).abs() <= tol[s, :, :kv]).all()
+        assert (got[s, :, kv:] == 7.0).all()
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("kind", ["normal", "ties", "zeros", "special", "rising"])
+def test_evict_long_lists(kind, in_place):
+    """More than 8192 tokens in some of the sequences, every kind of scores, positions, protected tokens, in place."""
+    rng = np.random.default_rng(111)
+    lens = [(0, 8193), (0, 0), (1, 20000), (0, 65), (3, 40001), (0, 9000), (0, 8192)]
+    keep = [8192, 4, 1, 64, 20000, 9000, 0]
+    c = R.Case(lens, seed=111, head_dim=8)
+    T.check_evict(c, keep, T._scores(c, kind, rng), in_place=in_place)
+    c = R.Case(lens, seed=112, block=5, head_dim=40, kv_heads=3, heads=3, dtype="f16")
+    shape = (len(lens), 3, c.max_kv + 3)
+    pos = torch.from_numpy(rng.permutation(10 ** 6)[:np.prod(shape)].reshape(shape).astype(np.int32)).cuda()
+    protect = [900000, 0, 999900, 10 ** 6, 700000, 0, 3]
+    T.check_evict(c, [5000, 4, 333, 64, 7000, 8999, 100], T._scores(c, kind, rng), protect=protect, pos=pos, in_place=in_place)
