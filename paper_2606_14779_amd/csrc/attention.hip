@@ -113,7 +113,7 @@ __device__ __forceinline__ bool unbounded_row(const uint16_t *v, uint32_t head_d
 // stage later.  What the products of stage 2t read, K(t) and V(t - 1), is stored by the first half in stage 2t - 1
 // and by the second in 2t - 2; the buffers' last readers are done at the end of stage 2t - 3.
 //
-// 512 new tokens over 128K (32 heads, 8 KV heads, 128): 1050 us, 1040 TFLOP/s, where a bf16 matrix product of 16384^3
+// 512 new tokens over 128K (32 heads, 8 KV heads, 128): 1074 us, 1022 TFLOP/s, where a bf16 matrix product of 16384^3
 // reaches 1370.  Matrix cores busy for 51 % of the cycles, no LDS bank conflicts, 87 % of the L2 reads hit; the clock
 // falls to about 2.0 GHz of 2.4 under it.  Without turns (four waves, two such workgroups to a CU) 1218 us.
 template <class T, int DP, class Offset>
@@ -442,8 +442,9 @@ constexpr int kFewWaves = 4;
 constexpr int kFewKeys = 32;    // to a wave at a time
 
 // Bound by reading the cache: 16 KB in flight to a wave (head_dim 128), each loaded as soon as its registers are free.
-// One token over 128K (64 heads, 8 KV heads, 64): 43 us, 6.2 TB/s; 32 tokens over ragged contexts of up to 16K (32, 8,
-// 128): 188 us, 5.1 TB/s, where a copy moves 6.1.
+// One token over 128K (64 heads, 8 KV heads, 64): 55 us with its join, 4.8 TB/s, where inputs change from call to call
+// (41 and 5 on the same 268 MB again and again, part of which the cache behind L2 still holds); 32 tokens over ragged
+// contexts of up to 16K (32, 8, 128): 190 us, 5.1 TB/s, where a copy moves 6.1.
 // Short contexts are bound by what has to be known before the first key can be asked for, so the block table's
 // entries are asked for together with the sequence's length wherever they do not depend on it.
 // Two waves to a SIMD: three would have 168 registers, and what does not fit them costs more (276 us for those 32 tokens).
@@ -781,7 +782,7 @@ __device__ __forceinline__ void halve(float (&acc)[32], int lane)
 // A wave holds 64 keys as the A operand and goes over the rows, which come through LDS for all waves: S^T again,
 // so every lane adds up the weights of its own 32 keys, for one row of each 32, in a fixed order; the lanes are
 // added at the end.  Bound by the vector unit: a difference, an exponential and a sum to a weight.  256 tokens over 128K
-// (32 heads, 4 KV heads, 128): 320 us, 860 TFLOP/s.
+// (32 heads, 4 KV heads, 128): 321 us, 854 TFLOP/s.
 template <class T, int DP>
 __global__ __launch_bounds__(kMassWaves * 64, DP > 128 ? 1 : 2) void attention_mass(const MassArgs a)
 {
@@ -979,7 +980,8 @@ __global__ __launch_bounds__(kMassWaves * 64, DP > 128 ? 1 : 2) void attention_m
 }
 
 // Up to 16 rows: bound by reading the keys, which go from memory to the registers that the product takes them from.
-// 8 tokens over 16K (32 heads, 8 KV heads, 128): 27 us, 4.9 TB/s; by way of LDS 31 to 34.
+// 8 tokens over 16K (32 heads, 8 KV heads, 128): 31 us, 4.2 TB/s where inputs change from call to call; 27 us on the
+// same ones again, by way of LDS 31 to 34.
 constexpr int kMassSteps = 4;                        // of 32 keys a wave
 
 template <class T, int DP>

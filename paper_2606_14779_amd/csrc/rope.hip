@@ -8,8 +8,10 @@
 // be reduced with more than 32 bits, and a table row of 4 * rot bytes serves all heads of a token.
 // Products are in 32 bits, rounded once to the cache's type.
 //
-// Bound by memory: packed prompts of 12.7K tokens (64 heads, 8 KV heads, 64) take 45 us, 263 MB at 5.8 TB/s, where a
-// copy moves 6.1; a decoding step of 32 tokens takes 3.7 us on the GPU, a chain of four dependent loads.
+// Bound by memory: packed prompts of 12.7K tokens (64 heads, 8 KV heads, 64; pairs interleaved) take 51 us, 263 MB at 5.1
+// TB/s, where inputs change from call to call (44 us on the same ones again); of 12.3K (32, 8, 128; pairs in halves) 53 us
+// on the same ones, 302 MB at 5.7 TB/s, where a copy moves 6.1.  A table of 128K positions of 64 pairs takes 32 us, for 64-bit
+// sines and cosines of 67 MB that a copy would write in 11.  A decoding step of 32 tokens takes 3.7 us on the GPU, a chain of four dependent loads.
 
 #include "wave.hpp"
 

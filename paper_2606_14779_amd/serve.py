@@ -7,7 +7,8 @@ that each cached token collected).  ``evict`` keeps a budget of tokens per head 
 stores what is left as a new, smaller request.  ``python -m paper_2606_14779_amd.serve`` runs that round trip and
 prints what each part took.
 
-There is no model here: the caller hands over each layer's projected queries, keys and values.
+There is no model here: the caller hands over each layer's projected queries, keys and values.  All layers have the
+same window or none, and no attention sinks, which a caller who needs them passes to ``kvpool.attention`` itself.
 """
 from __future__ import annotations
 
