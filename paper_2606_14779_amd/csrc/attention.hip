@@ -68,8 +68,9 @@ __device__ __forceinline__ Split keys_of(const AttentionArgs &a, const Seq &s, i
 // over once more before a row ends, key by key: what each row that sees such a key lacks of its output is added here.
 // 256 new tokens over 64K (32 heads, 8 KV heads, 128) take 0.34 ms with an infinity among the newest values or without;
 // going over all keys of the rows once more took 140 ms.
-//   q: this lane's pieces of its row, 16 bytes each, of elements from + i * step on; add: sums over the lanes of a row
-//   o: this lane's output, four elements each, from + i * step on
+
+// The weight of key k in this lane's row: q[i] are the row's elements from + i * QSTEP to + 7, and add sums a value over the
+// lanes that have the others.
 template <class T, int Q, int QSTEP, class Add>
 __device__ __forceinline__ float weight_of(const w4 (&q)[Q], uint32_t from, const uint16_t *k, uint32_t head_dim,
                                            float scale_log2, float m, Add add)
@@ -84,6 +85,7 @@ __device__ __forceinline__ float weight_of(const w4 (&q)[Q], uint32_t from, cons
     }
     return exp2_fast(__builtin_fmaf(add(x), scale_log2, -m));
 }
+// What a row lacks of element e of four: the products left out.
 template <class T>
 __device__ __forceinline__ float unbounded_part(w2 v, int e, float weight)
 {
