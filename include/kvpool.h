@@ -743,6 +743,123 @@ int kv_evict(const kvp_cache_shape *shape, const kvp_batch *batch, const int32_t
 /* Bytes of workspace that kv_evict needs for this shape and batch, of which only n_seq and max_kv are looked at. */
 int kv_evict_workspace(const kvp_cache_shape *shape, const kvp_batch *batch, uint64_t *bytes);
 
+/* ---- 8-bit pages, and drafted tokens over the paged cache ----
+ *
+ * Pages of either kind hold a layer's cache; batches, block tables and errors
+ * are those above.  Elements of 8-bit pages are e4m3 (4 bits of exponent, 3 of
+ * mantissa, largest 448, no infinities) times a power of two that 32
+ * neighbouring elements of a head share.  A slot of the K or V buffer is one
+ * piece of memory,
+ *   [num_kv_heads][block_size][head_dim]  elements, one byte each, then
+ *   [num_kv_heads][block_size][4 * ceil(head_dim / 128)]  exponents: byte b is
+ *       that of elements 32 b to 32 b + 31, which are 2^(byte - 127) times
+ *       what they hold; bytes past the last such b are written as 0,
+ * rounded up to a multiple of 16 bytes (kv_page_bytes).  Where nothing has to
+ * be rounded up, a pool moves such slots as those of a kvp_kv_spec with
+ * elem_bytes 1 and head_dim + 4 * ceil(head_dim / 128) in place of head_dim.
+ *
+ * A row x of 32 elements (fewer at the end of a head) is written with the
+ * least exponent e that has max |x| <= 448 * 2^e, within -117 to 120 for
+ * KVP_BF16 and -15 to 8 for KVP_F16, and elements x / 2^e rounded to nearest
+ * even; at the largest e they stop at 240.  So every element that a call here
+ * writes is exact and finite in the shape's dtype, in which it is read.
+ * Infinities and NaN become NaN and do not count for max |x|.
+ */
+#define KVP_PAGES_16BIT 0u    /* elements of the shape's dtype: [num_slots][num_kv_heads][block_size][head_dim] */
+#define KVP_PAGES_E4M3  1u    /* 8 bits, as above */
+
+typedef struct {
+    uint32_t kind;            /* KVP_PAGES_* */
+    uint32_t reserved;        /* 0 */
+    void *k, *v;              /* num_slots slots each, 16-byte aligned */
+} kvp_pages;
+
+/* Bytes of a slot of the K or of the V buffer of pages of this kind. */
+int kv_page_bytes(const kvp_cache_shape *shape, uint32_t kind, uint64_t *bytes);
+
+/* Norm of every head of the queries and keys, before they turn: x / sqrt(mean(x^2) + eps) * weight. */
+typedef struct {
+    const void *q_weight, *k_weight;   /* [head_dim] of the shape's dtype, 16-byte aligned; NULL: ones */
+    float eps;                /* not negative */
+    uint32_t reserved;        /* 0 */
+} kvp_head_norm;
+
+/* Positions on several axes, such as time, height and width. */
+typedef struct {
+    uint32_t num_axes;        /* 1 to 4 */
+    uint32_t reserved;        /* 0 */
+    uint8_t axis_of[128];     /* of every pair j < rot_dim / 2 the axis, by whose position it turns */
+} kvp_rope_axes;
+
+/*
+ * kv_rope_append with a norm before the rotation, positions on several axes,
+ * and pages of either kind, in one pass and with one rounding.
+ *   norm         NULL: none.  Values are never normed.
+ *   axes         NULL: one axis.
+ *   positions[num_axes][total_q]  pair j of a token turns by table[positions[axis_of[j]][token]][j]; a token with a
+ *                position outside [0, n_positions) on any axis gets a NaN query and key.
+ *   pos          NULL, or receives the positions on axis 0.
+ * table, rot_dim, flags, q, q_out, k and v as there; q_out must not overlap q.
+ */
+int kv_norm_rope_append(const kvp_cache_shape *shape, const kvp_batch *batch, const kvp_pages *pages,
+                        const kvp_head_norm *norm, const kvp_rope_axes *axes, const float *table, uint32_t n_positions,
+                        uint32_t rot_dim, uint32_t flags, const int32_t *positions, const void *q, uint64_t q_stride,
+                        void *q_out, uint64_t q_out_stride, const void *k, uint64_t k_stride, const void *v,
+                        uint64_t v_stride, int32_t *pos, uint32_t pos_stride, void *stream);
+
+/*
+ * Writes the cached tokens first[s] <= j < kv_len[s] of every sequence from
+ * pages of one kind to pages of the other: a context that the pool holds in 8
+ * bits comes back for the operators that take 16-bit pages, or one is made
+ * smaller before it is offloaded.
+ *   from         the batch's slots (num_slots of the shape).
+ *   to           of the other kind, to_slots slots; token j goes to slot to_table[s * to_stride + j / block_size].
+ *                Nothing is written where either slot is absent, nor to other tokens of a slot.  The buffers
+ *                must not overlap those of from, and no slot may be written for two sequences.
+ *   first[n_seq] NULL: 0.
+ * Of the batch cu_q, total_q and max_q are not used.  n_seq * num_kv_heads *
+ * ceil(max_kv / 64) must be less than 2^24, to_slots as num_slots.
+ */
+int kv_convert_pages(const kvp_cache_shape *shape, const kvp_batch *batch, const kvp_pages *from, const kvp_pages *to,
+                     const int32_t *to_table, uint32_t to_stride, uint32_t to_slots, const int32_t *first, void *stream);
+
+/*
+ * kv_attention over pages of either kind, with a mask among the new tokens for
+ * drafts that form a tree.  Logits, sinks, out, lse and workspace as there;
+ * 8-bit elements are read as the values that they stand for.
+ *   tree[total_q][tree_words]  NULL: causal.  Else bit j % 64 of word j / 64 of a new token's row says whether it
+ *                sees new token j of its own sequence (cache index kv_len - n_q + j), itself included; bits from n_q on
+ *                are not looked at.  It sees all tokens cached before the new ones.  8-byte aligned.
+ *   tree_words   at least ceil(max_q / 64), at most 2^20; 0 without a tree.
+ *   window       with a tree, a token that sees d new tokens stands d - 1 places behind the first: it sees the tokens
+ *                cached before the new ones at j > kv_len - n_q + d - 1 - window, and new ones by its mask alone.
+ * A token that sees nothing gets 0 and an lse of -inf (or that of its sink).
+ */
+int kv_attention_pages(const kvp_cache_shape *shape, const kvp_batch *batch, const kvp_pages *pages, const uint64_t *tree,
+                       uint32_t tree_words, const void *q, uint64_t q_stride, float scale, uint32_t window,
+                       const float *sinks, void *out, uint64_t out_stride, float *lse, void *workspace,
+                       uint64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace that kv_attention_pages needs for this shape and batch, whatever the pages, tree and window; of
+ * the batch only n_seq, total_q, max_q and max_kv are looked at. */
+int kv_attention_pages_workspace(const kvp_cache_shape *shape, const kvp_batch *batch, uint64_t *bytes);
+
+/*
+ * After drafted tokens were checked: the accepted ones of every sequence move
+ * together.  The K and V rows at cache index kv_len[s] - n_q + path[cu_q[s] + i]
+ * go to index kv_len[s] - n_q + i, for i < accepted[s], in place.
+ *   accepted[n_seq]  from 0 to n_q.
+ *   path[total_q]    a sequence's first accepted[s] entries: the accepted new tokens, strictly ascending from 0 to
+ *                n_q - 1 (as a path down a tree is).  Other entries are not looked at.
+ *   pos[n_seq][num_kv_heads][pos_stride]  NULL, or a list of positions whose entries move with their tokens.
+ *   len_out[n_seq]   kv_len[s] - n_q + accepted[s]; may be batch->kv_len.
+ * Slots of the new tokens are of no other sequence.  A row whose source or
+ * destination is absent does not move (its entry of pos does).  The tokens past the new length are
+ * left as they are.
+ */
+int kv_tree_commit(const kvp_cache_shape *shape, const kvp_batch *batch, const kvp_pages *pages, const int32_t *path,
+                   const int32_t *accepted, int32_t *pos, uint32_t pos_stride, int32_t *len_out, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

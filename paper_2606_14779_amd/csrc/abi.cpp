@@ -40,6 +40,19 @@ void op_attention_mass(const kvp_cache_shape *, const kvp_batch *, const void *,
 void op_evict(const kvp_cache_shape *, const kvp_batch *, const int32_t *, const int32_t *, const float *, float *,
               uint32_t, const int32_t *, int32_t *, uint32_t, void *, void *, int32_t *, void *, uint64_t, void *);
 void op_evict_workspace(const kvp_cache_shape *, const kvp_batch *, uint64_t *);
+void op_page_bytes(const kvp_cache_shape *, uint32_t, uint64_t *);
+void op_norm_rope_append(const kvp_cache_shape *, const kvp_batch *, const kvp_pages *, const kvp_head_norm *,
+                         const kvp_rope_axes *, const float *, uint32_t, uint32_t, uint32_t, const int32_t *, const void *,
+                         uint64_t, void *, uint64_t, const void *, uint64_t, const void *, uint64_t, int32_t *, uint32_t,
+                         void *);
+void op_convert_pages(const kvp_cache_shape *, const kvp_batch *, const kvp_pages *, const kvp_pages *, const int32_t *,
+                      uint32_t, uint32_t, const int32_t *, void *);
+void op_attention_pages(const kvp_cache_shape *, const kvp_batch *, const kvp_pages *, const uint64_t *, uint32_t,
+                        const void *, uint64_t, float, uint32_t, const float *, void *, uint64_t, float *, void *, uint64_t,
+                        void *);
+void op_attention_pages_workspace(const kvp_cache_shape *, const kvp_batch *, uint64_t *);
+void op_tree_commit(const kvp_cache_shape *, const kvp_batch *, const kvp_pages *, const int32_t *, const int32_t *, int32_t *,
+                    uint32_t, int32_t *, void *);
 }  // namespace kvp
 
 struct kvp_pool {
@@ -360,6 +373,51 @@ int kv_evict(const kvp_cache_shape *shape, const kvp_batch *batch, const int32_t
 int kv_evict_workspace(const kvp_cache_shape *shape, const kvp_batch *batch, uint64_t *bytes)
 {
     return guarded([&] { kvp::op_evict_workspace(shape, batch, bytes); });
+}
+
+int kv_page_bytes(const kvp_cache_shape *shape, uint32_t kind, uint64_t *bytes)
+{
+    return guarded([&] { kvp::op_page_bytes(shape, kind, bytes); });
+}
+
+int kv_norm_rope_append(const kvp_cache_shape *shape, const kvp_batch *batch, const kvp_pages *pages,
+                        const kvp_head_norm *norm, const kvp_rope_axes *axes, const float *table, uint32_t n_positions,
+                        uint32_t rot_dim, uint32_t flags, const int32_t *positions, const void *q, uint64_t q_stride,
+                        void *q_out, uint64_t q_out_stride, const void *k, uint64_t k_stride, const void *v,
+                        uint64_t v_stride, int32_t *pos, uint32_t pos_stride, void *stream)
+{
+    return guarded([&] {
+        kvp::op_norm_rope_append(shape, batch, pages, norm, axes, table, n_positions, rot_dim, flags, positions, q, q_stride,
+                                 q_out, q_out_stride, k, k_stride, v, v_stride, pos, pos_stride, stream);
+    });
+}
+
+int kv_convert_pages(const kvp_cache_shape *shape, const kvp_batch *batch, const kvp_pages *from, const kvp_pages *to,
+                     const int32_t *to_table, uint32_t to_stride, uint32_t to_slots, const int32_t *first, void *stream)
+{
+    return guarded([&] { kvp::op_convert_pages(shape, batch, from, to, to_table, to_stride, to_slots, first, stream); });
+}
+
+int kv_attention_pages(const kvp_cache_shape *shape, const kvp_batch *batch, const kvp_pages *pages, const uint64_t *tree,
+                       uint32_t tree_words, const void *q, uint64_t q_stride, float scale, uint32_t window,
+                       const float *sinks, void *out, uint64_t out_stride, float *lse, void *workspace,
+                       uint64_t workspace_bytes, void *stream)
+{
+    return guarded([&] {
+        kvp::op_attention_pages(shape, batch, pages, tree, tree_words, q, q_stride, scale, window, sinks, out, out_stride, lse,
+                                workspace, workspace_bytes, stream);
+    });
+}
+
+int kv_attention_pages_workspace(const kvp_cache_shape *shape, const kvp_batch *batch, uint64_t *bytes)
+{
+    return guarded([&] { kvp::op_attention_pages_workspace(shape, batch, bytes); });
+}
+
+int kv_tree_commit(const kvp_cache_shape *shape, const kvp_batch *batch, const kvp_pages *pages, const int32_t *path,
+                   const int32_t *accepted, int32_t *pos, uint32_t pos_stride, int32_t *len_out, void *stream)
+{
+    return guarded([&] { kvp::op_tree_commit(shape, batch, pages, path, accepted, pos, pos_stride, len_out, stream); });
 }
 
 }  // extern "C"

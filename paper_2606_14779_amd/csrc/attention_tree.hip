@@ -1,0 +1,12 @@
+// Attention over 16-bit pages with a mask among the new tokens, for gfx950 (MI355X): instances of attention_kernels.hpp.
+
+#include "attention_kernels.hpp"
+
+namespace kvp {
+
+hipError_t launch_attention_tree(const AttentionArgs &a, uint32_t dtype, hipStream_t stream)
+{
+    return dtype == KVP_BF16 ? by_head_dim<BF16, kTree16>(a, stream) : by_head_dim<F16, kTree16>(a, stream);
+}
+
+}  // namespace kvp

@@ -104,11 +104,11 @@ struct Cut {
 // How an attention call is cut.  A KV head's rows (new tokens x group) go to attention_few if no sequence has more
 // than a 16-row product holds, else to tiles of 256 (128 at a head_dim of more than 128).  Where the tiles do not
 // fill the chip, the keys are split, as far as a part holds enough keys to be worth its output's way through memory.
-Cut cut_of(const CacheView &c, uint32_t window)
+Cut cut_of(const CacheView &c, uint32_t window, uint32_t waves)
 {
     Cut p{};
     const uint64_t rows = (uint64_t)c.total_q * c.group;
-    const uint32_t tile_rows = row_waves(c.head_dim) * 32;
+    const uint32_t tile_rows = waves * 32;
     const bool few = p.few = (uint64_t)c.max_q * c.group <= kFewRows;
     if (!rows) return p.splits = 1, p.split_keys = kTileKeys, p;
     p.tiles = few ? c.n_seq : (uint32_t)(rows / tile_rows + c.n_seq);
@@ -143,7 +143,7 @@ Cut cut_of(const CacheView &c, uint32_t window)
         keys = (span + best - 1) / best;
     }
     // no more parts than without a window: the workspace is asked for without one
-    if (window) keys = std::max(keys, (span + cut_of(c, 0).splits - 1) / cut_of(c, 0).splits);
+    if (window) keys = std::max(keys, (span + cut_of(c, 0, waves).splits - 1) / cut_of(c, 0, waves).splits);
     const uint64_t unit = few ? 128 : kTileKeys;
     keys = std::max(unit, (keys + unit - 1) / unit * unit);
     p.splits = (uint32_t)std::max<uint64_t>(1, (span + keys - 1) / keys);
@@ -152,7 +152,63 @@ Cut cut_of(const CacheView &c, uint32_t window)
     return p;
 }
 
-uint64_t attention_bytes(const CacheView &c) { return cut_of(c, 0).bytes; }
+uint64_t attention_bytes(const CacheView &c) { return cut_of(c, 0, row_waves(c.head_dim)).bytes; }
+
+// Waves of 32 rows to a row tile of attention over pages.
+uint32_t page_waves(const CacheView &c)
+{
+    const uint64_t rows = (uint64_t)c.max_q * c.group;
+    const uint32_t most = row_waves(c.head_dim);
+    return rows <= 64 ? 2 : rows <= 128 ? std::min(4u, most) : most;
+}
+uint64_t attention_pages_bytes(const CacheView &c)
+{
+    return std::max(attention_bytes(c), cut_of(c, 0, page_waves(c)).bytes);
+}
+
+uint32_t row_exponents(uint32_t head_dim) { return (head_dim + 127) / 128 * 4; }
+
+// A slot's bytes; a cache of less than 2^32 rows has less than 2^43.
+uint64_t slot_bytes(const CacheView &c, uint32_t kind)
+{
+    const uint64_t rows = (uint64_t)c.kv_heads * c.block;
+    if (kind == KVP_PAGES_16BIT) return rows * c.head_dim * 2;
+    return (rows * (c.head_dim + row_exponents(c.head_dim)) + 15) / 16 * 16;
+}
+
+void need_kind(uint32_t kind) { need(kind == KVP_PAGES_16BIT || kind == KVP_PAGES_E4M3, "unknown kind of pages"); }
+
+// Checks the pages; buffers says whether they are looked at.
+PageView pages_of(const CacheView &c, const kvp_pages *p, uint32_t num_slots, bool buffers)
+{
+    need(p, "pages is null");
+    need_kind(p->kind);
+    need(p->reserved == 0, "reserved fields are not 0");
+    if (buffers) {
+        need_pointer(p->k, 16, "k pages");
+        need_pointer(p->v, 16, "v pages");
+    }
+    PageView v{};
+    v.k = static_cast<uint8_t *>(p->k);
+    v.v = static_cast<uint8_t *>(p->v);
+    v.slot_bytes = slot_bytes(c, p->kind);
+    if (p->kind == KVP_PAGES_E4M3) {
+        const uint64_t elements = (uint64_t)c.kv_heads * c.block * c.head_dim;
+        need(elements <= 0x7FFFFFFFull, "a slot of 2^31 elements or more");
+        v.exponents = (uint32_t)elements;
+        v.row_exponents = row_exponents(c.head_dim);
+    }
+    v.num_slots = num_slots;
+    return v;
+}
+
+// Lanes of 8 elements to a head, a power of two of them.
+uint32_t lanes_log2(uint32_t head_dim)
+{
+    uint32_t n = 0;
+    while ((8u << n) < head_dim) ++n;
+    return n;
+}
 
 // Words of workspace to a list: four of counts, two per token (candidates, then moves), a bit per token, and for
 // long lists the counts of 2^11 digits per part and of four waves' candidates.
@@ -167,31 +223,24 @@ void need_scale(float scale) { need(std::isfinite(scale) && scale > 0, "scale is
 
 }  // namespace
 
-void op_attention_workspace(const kvp_cache_shape *s, const kvp_batch *b, uint64_t *bytes)
-{
-    need(bytes, "bytes is null");
-    *bytes = attention_bytes(view_of(s, b, true, false));
-}
+namespace {
 
-void op_attention(const kvp_cache_shape *s, const kvp_batch *b, const void *q, uint64_t q_stride, const void *k,
-                  const void *v, float scale, uint32_t window, const float *sinks, void *out, uint64_t out_stride,
-                  float *lse, void *workspace, uint64_t workspace_bytes, void *stream)
+// What every attention call checks and says to its kernels, but for the tensors that the cut makes launches of.
+void fill_attention(AttentionArgs &a, const void *q, uint64_t q_stride, const void *k, const void *v, float scale,
+                    uint32_t window, const float *sinks, void *out, uint64_t out_stride, float *lse, uint32_t waves,
+                    void *workspace, uint64_t workspace_bytes, const char *too_small)
 {
-    AttentionArgs a{};
-    a.c = view_of(s, b, true);
-    need_scale(scale);
     const uint64_t row = (uint64_t)a.c.heads * a.c.head_dim;
-    if (a.c.total_q == 0) return;
     need_rows(q, q_stride, 0, "q");
     need_rows(out, out_stride, row, "out");
     need_pointer(k, 16, "k_cache");
     need_pointer(v, 16, "v_cache");
     need(aligned(sinks, 4), "sinks is not aligned to 4 bytes");
     need(aligned(lse, 4), "lse is not aligned to 4 bytes");
-    const Cut p = cut_of(a.c, window);
+    const Cut p = cut_of(a.c, window, waves);
     if (p.bytes) {
         need_pointer(workspace, 16, "workspace");
-        need(workspace_bytes >= p.bytes, "workspace is smaller than kv_attention_workspace says");
+        need(workspace_bytes >= p.bytes, too_small);
     }
     a.q = static_cast<const uint16_t *>(q);
     a.k = static_cast<const uint16_t *>(k);
@@ -210,9 +259,194 @@ void op_attention(const kvp_cache_shape *s, const kvp_batch *b, const void *q, u
     const uint64_t parts = (uint64_t)p.splits * a.c.total_q * a.c.heads;
     a.part_o = static_cast<float *>(workspace);
     a.part_ml = a.part_o ? a.part_o + parts * a.c.head_dim : nullptr;
+    a.waves = waves;
+}
+
+}  // namespace
+
+void op_attention_workspace(const kvp_cache_shape *s, const kvp_batch *b, uint64_t *bytes)
+{
+    need(bytes, "bytes is null");
+    *bytes = attention_bytes(view_of(s, b, true, false));
+}
+
+void op_attention(const kvp_cache_shape *s, const kvp_batch *b, const void *q, uint64_t q_stride, const void *k,
+                  const void *v, float scale, uint32_t window, const float *sinks, void *out, uint64_t out_stride,
+                  float *lse, void *workspace, uint64_t workspace_bytes, void *stream)
+{
+    AttentionArgs a{};
+    a.c = view_of(s, b, true);
+    need_scale(scale);
+    if (a.c.total_q == 0) return;
+    fill_attention(a, q, q_stride, k, v, scale, window, sinks, out, out_stride, lse, row_waves(a.c.head_dim), workspace,
+                   workspace_bytes, "workspace is smaller than kv_attention_workspace says");
     const hipStream_t st = static_cast<hipStream_t>(stream);
     check_hip(launch_attention(a, s->dtype, st), "attention launch");
-    if (p.splits > 1) check_hip(launch_attention_join(a, s->dtype, st), "attention join launch");
+    if (a.splits > 1) check_hip(launch_attention_join(a, s->dtype, st), "attention join launch");
+}
+
+void op_attention_pages_workspace(const kvp_cache_shape *s, const kvp_batch *b, uint64_t *bytes)
+{
+    need(bytes, "bytes is null");
+    *bytes = attention_pages_bytes(view_of(s, b, true, false));
+}
+
+void op_attention_pages(const kvp_cache_shape *s, const kvp_batch *b, const kvp_pages *pages, const uint64_t *tree,
+                        uint32_t tree_words, const void *q, uint64_t q_stride, float scale, uint32_t window,
+                        const float *sinks, void *out, uint64_t out_stride, float *lse, void *workspace,
+                        uint64_t workspace_bytes, void *stream)
+{
+    AttentionArgs a{};
+    a.c = view_of(s, b, true);
+    need_scale(scale);
+    const PageView p = pages_of(a.c, pages, a.c.num_slots, a.c.total_q != 0);
+    need(aligned(tree, 8), "tree is not aligned to 8 bytes");
+    need(tree ? (uint64_t)tree_words * 64 >= a.c.max_q && tree_words <= 1u << 20 : tree_words == 0,
+         "tree_words is not from ceil(max_q / 64) to 2^20, or not 0 without a tree");
+    if (a.c.total_q == 0) return;
+    const bool eight = pages->kind == KVP_PAGES_E4M3;
+    // 16-bit pages under a causal mask are kv_attention's
+    const uint32_t waves = eight || tree ? page_waves(a.c) : row_waves(a.c.head_dim);
+    fill_attention(a, q, q_stride, p.k, p.v, scale, window, sinks, out, out_stride, lse, waves, workspace, workspace_bytes,
+                   "workspace is smaller than kv_attention_pages_workspace says");
+    a.exponents = p.exponents;
+    a.row_exponents = p.row_exponents;
+    a.slot_bytes = p.slot_bytes;
+    a.tree = tree;
+    a.tree_words = tree_words;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    check_hip(eight  ? launch_attention_e4m3(a, s->dtype, st)
+              : tree ? launch_attention_tree(a, s->dtype, st)
+                     : launch_attention(a, s->dtype, st),
+              "attention launch");
+    if (a.splits > 1) check_hip(launch_attention_join(a, s->dtype, st), "attention join launch");
+}
+
+void op_page_bytes(const kvp_cache_shape *s, uint32_t kind, uint64_t *bytes)
+{
+    need(bytes, "bytes is null");
+    const kvp_batch none{};
+    const CacheView c = view_of(s, &none, false, false);
+    need_kind(kind);
+    *bytes = slot_bytes(c, kind);
+}
+
+void op_norm_rope_append(const kvp_cache_shape *s, const kvp_batch *b, const kvp_pages *pages, const kvp_head_norm *norm,
+                         const kvp_rope_axes *axes, const float *angles, uint32_t n_positions, uint32_t rot, uint32_t flags,
+                         const int32_t *positions, const void *q, uint64_t q_stride, void *q_out, uint64_t q_out_stride,
+                         const void *k, uint64_t k_stride, const void *v, uint64_t v_stride, int32_t *pos,
+                         uint32_t pos_stride, void *stream)
+{
+    AppendArgs a{};
+    a.c = view_of(s, b, true);
+    a.pages = pages_of(a.c, pages, a.c.num_slots, a.c.total_q != 0);
+    need(!(flags & ~KVP_ROPE_INTERLEAVED), "unknown flags");
+    need(rot % 2 == 0 && rot <= a.c.head_dim, "rot_dim is odd or more than head_dim");
+    need(!q == !q_out, "one of q and q_out is null");
+    a.axes = 1;
+    if (axes) {
+        need(axes->num_axes >= 1 && axes->num_axes <= kMostAxes, "num_axes is not from 1 to 4");
+        need(axes->reserved == 0, "reserved fields are not 0");
+        a.axes = axes->num_axes;
+        for (uint32_t j = 0; j < rot / 2; ++j) {
+            need(axes->axis_of[j] < a.axes, "a pair's axis is not below num_axes");
+            a.axis_of[j] = axes->axis_of[j];
+        }
+    }
+    if (norm) {
+        need(norm->reserved == 0, "reserved fields are not 0");
+        need(std::isfinite(norm->eps) && norm->eps >= 0, "eps is negative or no number");
+        need(aligned(norm->q_weight, 16) && aligned(norm->k_weight, 16), "q_weight or k_weight is not aligned to 16 bytes");
+        a.norm = 1;
+        a.eps = norm->eps;
+        a.q_weight = static_cast<const uint16_t *>(norm->q_weight);
+        a.k_weight = static_cast<const uint16_t *>(norm->k_weight);
+    }
+    if (a.c.total_q == 0) return;
+    need(n_positions > 0, "an empty table of angles");
+    if (rot) need_pointer(angles, 8, "angles");
+    need_pointer(positions, 4, "positions");
+    const uint64_t row = (uint64_t)a.c.heads * a.c.head_dim;
+    if (q) {
+        need_rows(q, q_stride, 0, "q");
+        need_rows(q_out, q_out_stride, row, "q_out");
+        need(q != q_out, "q_out is q");
+    }
+    need_rows(k, k_stride, 0, "k");
+    need_rows(v, v_stride, 0, "v");
+    if (pos) {
+        need_pointer(pos, 4, "pos");
+        need(pos_stride >= a.c.max_kv, "pos_stride is less than max_kv");
+    }
+    need(a.c.total_q < 1u << 24, "2^24 new tokens or more in one call");
+    a.angles = angles;
+    a.positions = positions;
+    a.n_positions = n_positions;
+    a.rot = rot;
+    a.interleaved = flags & KVP_ROPE_INTERLEAVED ? 1 : 0;
+    a.lanes_log2 = lanes_log2(a.c.head_dim);
+    a.per_dim = 1.0f / (float)a.c.head_dim;
+    a.q = static_cast<const uint16_t *>(q);
+    a.k = static_cast<const uint16_t *>(k);
+    a.v = static_cast<const uint16_t *>(v);
+    a.q_out = static_cast<uint16_t *>(q_out);
+    a.q_stride = q_stride;
+    a.q_out_stride = q_out_stride;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.pos = pos;
+    a.pos_stride = pos_stride;
+    check_hip(launch_append(a, s->dtype, static_cast<hipStream_t>(stream)), "append launch");
+}
+
+void op_convert_pages(const kvp_cache_shape *s, const kvp_batch *b, const kvp_pages *from, const kvp_pages *to,
+                      const int32_t *to_table, uint32_t to_stride, uint32_t to_slots, const int32_t *first, void *stream)
+{
+    ConvertArgs a{};
+    a.c = view_of(s, b, false);
+    const bool any = a.c.n_seq && a.c.max_kv;
+    a.from = pages_of(a.c, from, a.c.num_slots, any);
+    a.to = pages_of(a.c, to, to_slots, any);
+    need(from->kind != to->kind, "pages of the same kind");
+    need(to_slots > 0, "to_slots is 0");
+    need((uint64_t)to_slots * a.c.kv_heads <= 0xFFFFFFFEull / a.c.block, "a cache of 2^32 rows or more");
+    need((uint64_t)to_stride * a.c.block >= a.c.max_kv, "to_stride * block_size is less than max_kv");
+    need(aligned(first, 4), "first is not aligned to 4 bytes");
+    need(((uint64_t)a.c.max_kv + kConvertTokens - 1) / kConvertTokens * a.c.n_seq * a.c.kv_heads < 1u << 24,
+         "too many tokens for one call");
+    if (!any) return;
+    need_pointer(to_table, 4, "to_table");
+    a.to_table = to_table;
+    a.to_stride = to_stride;
+    a.first = first;
+    a.lanes_log2 = lanes_log2(a.c.head_dim);
+    check_hip(launch_convert(a, s->dtype, static_cast<hipStream_t>(stream)), "page conversion launch");
+}
+
+void op_tree_commit(const kvp_cache_shape *s, const kvp_batch *b, const kvp_pages *pages, const int32_t *path,
+                    const int32_t *accepted, int32_t *pos, uint32_t pos_stride, int32_t *len_out, void *stream)
+{
+    CommitArgs a{};
+    a.c = view_of(s, b, true);
+    a.pages = pages_of(a.c, pages, a.c.num_slots, a.c.n_seq != 0);
+    if (a.c.n_seq == 0) return;
+    need_pointer(accepted, 4, "accepted");
+    need_pointer(len_out, 4, "len_out");
+    if (a.c.total_q) need_pointer(path, 4, "path");
+    if (pos) {
+        need_pointer(pos, 4, "pos");
+        need(pos_stride >= a.c.max_kv, "pos_stride is less than max_kv");
+    }
+    a.path = path;
+    a.accepted = accepted;
+    a.pos = pos;
+    a.pos_stride = pos_stride;
+    a.lanes_log2 = lanes_log2(a.c.head_dim);
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const bool in_place = len_out == b->kv_len;   // the move still reads the old lengths
+    a.len_out = in_place ? nullptr : len_out;
+    check_hip(launch_commit(a, st), "commit launch");
+    if (in_place) check_hip(launch_commit_lengths(a, len_out, st), "commit lengths launch");
 }
 
 void op_attention_mass(const kvp_cache_shape *s, const kvp_batch *b, const void *q, uint64_t q_stride, const void *k,

@@ -1,5 +1,5 @@
 // Operators on the engine's paged cache: what their host side (cache_ops.cpp)
-// and their kernels (attention.hip, rope.hip, evict.hip) share.
+// and their kernels (attention.hip, rope.hip, evict.hip, attention_tree.hip, attention_e4m3.hip, pages.hip) share.
 #ifndef KVP_CACHE_OPS_HPP
 #define KVP_CACHE_OPS_HPP
 
@@ -21,9 +21,18 @@ struct CacheView {
 };
 constexpr uint32_t kNoRow = 0xFFFFFFFFu;
 
+// Pages of either kind: slots of 16-bit elements, or of bytes with a power of two to 32 of them.
+struct PageView {
+    uint8_t *k, *v;
+    uint64_t slot_bytes;
+    uint32_t exponents;              // where a slot's exponents begin; 0: 16-bit elements
+    uint32_t row_exponents;          // bytes of exponents to a row
+    uint32_t num_slots;
+};
+
 struct AttentionArgs {
     CacheView c;
-    const uint16_t *q, *k, *v;
+    const uint16_t *q, *k, *v;       // k, v: of 8-bit pages too, by bytes
     uint64_t q_stride, out_stride;   // elements between tokens
     uint16_t *out;
     float *lse;                      // [heads][total_q] or null
@@ -34,6 +43,12 @@ struct AttentionArgs {
     uint32_t tiles, splits, split_keys;
     float *part_o;                   // [splits][total_q * heads][head_dim]
     float *part_ml;                  // [splits][total_q * heads][2]
+    // of attention over pages alone
+    uint32_t waves;                  // of attention_rows
+    uint32_t exponents, row_exponents;   // of 8-bit pages; 0: 16-bit elements
+    uint64_t slot_bytes;
+    const uint64_t *tree;            // [total_q][tree_words] or null
+    uint32_t tree_words;
 };
 
 struct MassArgs {
@@ -60,6 +75,39 @@ struct RopeArgs {
 };
 
 constexpr uint32_t kMostRotary = 256;   // rotated elements of a head
+constexpr uint32_t kMostAxes = 4;
+struct AppendArgs {
+    CacheView c;
+    PageView pages;
+    const float *angles;             // [n_positions][rot / 2][2]
+    const int32_t *positions;        // [axes][total_q]
+    uint32_t n_positions, rot, interleaved, axes;
+    uint32_t lanes_log2;             // lanes to a head: 8 elements each
+    uint32_t norm;                   // whether queries and keys are normed
+    float eps, per_dim;              // 1 / head_dim
+    const uint16_t *q_weight, *k_weight;   // null: ones
+    const uint16_t *q, *k, *v;
+    uint16_t *q_out;
+    uint64_t q_stride, q_out_stride, k_stride, v_stride;
+    int32_t *pos;
+    uint32_t pos_stride;
+    uint8_t axis_of[kMostRotary / 2];
+};
+
+struct ConvertArgs {
+    CacheView c;
+    PageView from, to;
+    const int32_t *to_table, *first; // first: null = 0
+    uint32_t to_stride, lanes_log2;
+};
+
+struct CommitArgs {
+    CacheView c;
+    PageView pages;
+    const int32_t *path, *accepted;
+    int32_t *pos, *len_out;          // len_out: null = by a launch of its own
+    uint32_t pos_stride, lanes_log2;
+};
 struct RopeTableArgs {
     float *angles;
     uint32_t n_positions, half;
@@ -88,12 +136,20 @@ hipError_t launch_mass(const MassArgs &a, uint32_t dtype, hipStream_t stream);
 hipError_t launch_rope(const RopeArgs &a, uint32_t dtype, hipStream_t stream);
 hipError_t launch_rope_table(const RopeTableArgs &a, hipStream_t stream);
 hipError_t launch_evict(const EvictArgs &a, hipStream_t stream);
+hipError_t launch_attention_e4m3(const AttentionArgs &a, uint32_t dtype, hipStream_t stream);
+hipError_t launch_attention_tree(const AttentionArgs &a, uint32_t dtype, hipStream_t stream);
+hipError_t launch_append(const AppendArgs &a, uint32_t dtype, hipStream_t stream);
+hipError_t launch_convert(const ConvertArgs &a, uint32_t dtype, hipStream_t stream);
+hipError_t launch_commit(const CommitArgs &a, hipStream_t stream);
+hipError_t launch_commit_lengths(const CommitArgs &a, int32_t *len_out, hipStream_t stream);
 
 // Rows (new tokens times the heads of a KV head) and keys of the attention kernels' tiles.
 constexpr uint32_t kFewRows = 16;
 // 32 rows to a wave, two waves to a SIMD; at a head_dim of more than 128 the registers hold one.
 constexpr int row_waves(uint32_t head_dim) { return head_dim > 128 ? 4 : 8; }
 constexpr uint32_t kTileKeys = 64;
+
+constexpr uint32_t kConvertTokens = 64;    // to a workgroup
 
 // Eviction: tokens that one workgroup holds in registers, and the workgroups that a longer list is spread over.
 constexpr uint32_t kEvictShort = 8192;

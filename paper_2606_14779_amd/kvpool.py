@@ -40,6 +40,7 @@ MEASURE_FILES_TOGETHER = 2   # file regions read all at once, as a retrieve read
 DTYPES = {"bf16": 0, "f16": 1}
 ROPE_KINDS = {"plain": 0, "linear": 1, "by_parts": 2, "by_parts_index": 3}
 ROPE_INTERLEAVED = 1
+PAGES = {"16": 0, "e4m3": 1}
 
 LOC_DTYPE = np.dtype([("region", "<u4"), ("gen", "<u4"), ("offset", "<u8")])
 
@@ -94,6 +95,20 @@ class _RopeScaling(ctypes.Structure):
                 ("beta", ctypes.c_double), ("magnitude", ctypes.c_double)]
 
 
+class _Pages(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_uint32), ("reserved", ctypes.c_uint32), ("k", ctypes.c_uint64), ("v", ctypes.c_uint64)]
+
+
+class _HeadNorm(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_uint64), ("k_weight", ctypes.c_uint64), ("eps", ctypes.c_float),
+                ("reserved", ctypes.c_uint32)]
+
+
+class _RopeAxes(ctypes.Structure):
+    _fields_ = [("num_axes", ctypes.c_uint32), ("reserved", ctypes.c_uint32), ("axis_of", ctypes.c_uint8 * 128)]
+
+
+assert ctypes.sizeof(_Pages) == 24 and ctypes.sizeof(_HeadNorm) == 24 and ctypes.sizeof(_RopeAxes) == 136
 assert ctypes.sizeof(_CacheShape) == 28 and ctypes.sizeof(_Batch) == 48 and ctypes.sizeof(_RopeScaling) == 56
 assert ctypes.sizeof(_RegionDesc) == 24 and ctypes.sizeof(_KVSpec) == 24
 assert LOC_DTYPE.itemsize == 16
@@ -164,6 +179,13 @@ _SIGS = {
     "kv_rope_table": (_i32, [_vp, _u32, _u32, _vp, _vp]),
     "kv_rope_append": (_i32, [_vp, _vp, _vp, _u32, _u32, _u32, _vp, _vp, _u64, _vp, _u64, _vp, _u64, _vp, _u64, _vp,
                               _vp, _vp, _u32, _vp]),
+    "kv_page_bytes": (_i32, [_vp, _u32, _vp]),
+    "kv_norm_rope_append": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _u32, _u32, _u32, _vp, _vp, _u64, _vp, _u64, _vp, _u64, _vp,
+                                   _u64, _vp, _u32, _vp]),
+    "kv_convert_pages": (_i32, [_vp, _vp, _vp, _vp, _vp, _u32, _u32, _vp, _vp]),
+    "kv_attention_pages": (_i32, [_vp, _vp, _vp, _vp, _u32, _vp, _u64, _f32, _u32, _vp, _vp, _u64, _vp, _vp, _u64, _vp]),
+    "kv_attention_pages_workspace": (_i32, [_vp, _vp, _vp]),
+    "kv_tree_commit": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _u32, _vp, _vp]),
     "kv_attention": (_i32, [_vp, _vp, _vp, _u64, _vp, _vp, _f32, _u32, _vp, _vp, _u64, _vp, _vp, _u64, _vp]),
     "kv_attention_workspace": (_i32, [_vp, _vp, _vp]),
     "kv_attention_mass": (_i32, [_vp, _vp, _vp, _u64, _vp, _f32, _u32, _vp, _u32, _vp, _vp, _u32, _vp]),
@@ -402,6 +424,103 @@ def evict(shape: CacheShape, batch: Batch, keep: int, score_in: int, score_out: 
         _out_of_range("evict")
     rc = _cdll.kv_evict(shape._p, batch._p, keep, protect, score_in, score_out, score_stride, pos_in, pos_out, pos_stride,
                         k_cache, v_cache, len_out, workspace, workspace_bytes, stream)
+    if rc:
+        _check(rc)
+
+
+class Pages:
+    """A layer's cache of either kind (kvp_pages): "16", elements of the shape's dtype, or "e4m3", 8 bits."""
+
+    def __init__(self, kind: str, k: int, v: int):
+        if kind not in PAGES:
+            raise ValueError("kind %r is none of %s" % (kind, ", ".join(PAGES)))
+        self._c = _struct(_Pages, PAGES[kind], 0, k, v)
+        self._p = ctypes.addressof(self._c)
+
+
+class HeadNorm:
+    """Norm of every head of queries and keys (kvp_head_norm); a weight of 0: ones."""
+
+    def __init__(self, q_weight: int, k_weight: int, eps: float):
+        self._c = _HeadNorm(operator.index(q_weight), operator.index(k_weight), eps, 0)
+        self._p = ctypes.addressof(self._c)
+        if self._c.q_weight != q_weight or self._c.k_weight != k_weight:
+            _out_of_range("HeadNorm")
+
+
+class RopeAxes:
+    """Positions on several axes (kvp_rope_axes): axis_of has the axis of every pair of rotated elements."""
+
+    def __init__(self, num_axes: int, axis_of):
+        axis_of = [operator.index(x) for x in axis_of]
+        if not 0 <= num_axes < 1 << 32 or len(axis_of) > 128 or any(not 0 <= x < 256 for x in axis_of):
+            raise ValueError("num_axes or axis_of is outside its range")
+        self._c = _RopeAxes(num_axes, 0, (ctypes.c_uint8 * 128)(*axis_of))
+        self._p = ctypes.addressof(self._c)
+        self.pairs = len(axis_of)
+
+
+def page_bytes(shape: CacheShape, kind: str) -> int:
+    """Bytes of a slot of the K or of the V buffer of pages of this kind."""
+    if kind not in PAGES:
+        raise ValueError("kind %r is none of %s" % (kind, ", ".join(PAGES)))
+    n = ctypes.c_uint64()
+    _check(_lib.kv_page_bytes(shape._p, PAGES[kind], ctypes.addressof(n)))
+    return n.value
+
+
+def norm_rope_append(shape: CacheShape, batch: Batch, pages: Pages, table: int, n_positions: int, rot_dim: int,
+                     positions: int, k: int, k_stride: int, v: int, v_stride: int, *, norm: HeadNorm | None = None,
+                     axes: RopeAxes | None = None, q: int = 0, q_stride: int = 0, q_out: int = 0, q_out_stride: int = 0,
+                     pos: int = 0, pos_stride: int = 0, interleaved: bool = False, stream: int = 0):
+    """kv_norm_rope_append: queries and keys normed and turned; keys, values and positions to pages of either kind."""
+    if (n_positions | rot_dim | pos_stride) >> 32 or (q_stride | q_out_stride | k_stride | v_stride) >> 64:
+        _out_of_range("norm_rope_append")
+    if axes is not None and axes.pairs < rot_dim // 2:
+        raise ValueError("axis_of has %d pairs, rot_dim %d" % (axes.pairs, rot_dim // 2))
+    rc = _cdll.kv_norm_rope_append(shape._p, batch._p, pages._p, norm._p if norm is not None else None,
+                                   axes._p if axes is not None else None, table, n_positions, rot_dim,
+                                   ROPE_INTERLEAVED if interleaved else 0, positions, q, q_stride, q_out, q_out_stride, k,
+                                   k_stride, v, v_stride, pos, pos_stride, stream)
+    if rc:
+        _check(rc)
+
+
+def convert_pages(shape: CacheShape, batch: Batch, source: Pages, to: Pages, to_table: int, to_stride: int, to_slots: int,
+                  *, first: int = 0, stream: int = 0):
+    """kv_convert_pages: cached tokens from pages of one kind to pages of the other."""
+    if (to_stride | to_slots) >> 32:
+        _out_of_range("convert_pages")
+    rc = _cdll.kv_convert_pages(shape._p, batch._p, source._p, to._p, to_table, to_stride, to_slots, first, stream)
+    if rc:
+        _check(rc)
+
+
+def attention_pages_workspace(shape: CacheShape, batch: Batch) -> int:
+    """Bytes of workspace that attention_pages needs for this shape and batch."""
+    n = ctypes.c_uint64()
+    _check(_lib.kv_attention_pages_workspace(shape._p, batch._p, ctypes.addressof(n)))
+    return n.value
+
+
+def attention_pages(shape: CacheShape, batch: Batch, pages: Pages, q: int, q_stride: int, scale: float, out: int,
+                    out_stride: int, *, tree: int = 0, tree_words: int = 0, window: int = 0, sinks: int = 0, lse: int = 0,
+                    workspace: int = 0, workspace_bytes: int = 0, stream: int = 0):
+    """kv_attention_pages: attention over pages of either kind, causal or with a tree's mask among the new tokens."""
+    if (window | tree_words) >> 32 or (q_stride | out_stride | workspace_bytes) >> 64:
+        _out_of_range("attention_pages")
+    rc = _cdll.kv_attention_pages(shape._p, batch._p, pages._p, tree, tree_words, q, q_stride, scale, window, sinks, out,
+                                  out_stride, lse, workspace, workspace_bytes, stream)
+    if rc:
+        _check(rc)
+
+
+def tree_commit(shape: CacheShape, batch: Batch, pages: Pages, path: int, accepted: int, len_out: int, *, pos: int = 0,
+                pos_stride: int = 0, stream: int = 0):
+    """kv_tree_commit: the accepted ones of the drafted tokens move together in the cache."""
+    if pos_stride >> 32:
+        _out_of_range("tree_commit")
+    rc = _cdll.kv_tree_commit(shape._p, batch._p, pages._p, path, accepted, pos, pos_stride, len_out, stream)
     if rc:
         _check(rc)
 
