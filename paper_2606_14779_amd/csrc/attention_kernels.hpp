@@ -154,13 +154,12 @@ __device__ __forceinline__ bool unbounded_row(const AttentionArgs &a, uint32_t r
 // 512 new tokens over 128K (32 heads, 8 KV heads, 128): 1074 us, 1022 TFLOP/s, where a bf16 matrix product of 16384^3
 // reaches 1370.  Matrix cores busy for 51 % of the cycles, no LDS bank conflicts, 87 % of the L2 reads hit; the clock
 // falls to about 2.0 GHz of 2.4 under it.  Without turns (four waves, two such workgroups to a CU) 1218 us.
-constexpr int row_occupancy(int head_dim, int waves) { return head_dim > 128 || waves == 2 ? 1 : 2; }
-
-template <class T, int DP, class Offset, int KIND = kCausal16, int NW = row_waves(DP)>
-__global__ __launch_bounds__(NW * 64, row_occupancy(DP, NW)) void attention_rows(const AttentionArgs a)
+template <class T, int DP, class Offset, int KIND = kCausal16>
+__global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attention_rows(const AttentionArgs a)
 {
-    constexpr int TK = kTileKeys, TR = NW * 32;
+    constexpr int TK = kTileKeys, NW = row_waves(DP), TR = NW * 32;
     constexpr bool E8 = KIND == kEight;
+    constexpr int AHEAD = DP > 128 || KIND == kCausal16 ? 1 : 2;   // tiles that have been asked for and are not in LDS
     constexpr int XW = E8 ? (DP + 127) / 128 : 1;    // words of exponents to a row of 8-bit pages
     constexpr int CH = DP / 8;                       // 16-byte pieces of a row
     constexpr int PASS = NW * 64 / CH;               // rows that the workgroup loads at once
@@ -173,22 +172,24 @@ __global__ __launch_bounds__(NW * 64, row_occupancy(DP, NW)) void attention_rows
     const uint32_t rest = blockIdx.x / c.kv_heads;
     // the tiles of a part of the keys run side by side, so that its keys come from L2 for all but one of them;
     // under a causal mask later tiles have more keys
-    const uint32_t split = rest / a.tiles, rank = rest % a.tiles;
-    uint32_t seq, row0;
+    uint32_t split, seq, row0;
     Seq s;
     if (c.n_seq > 1 && c.n_seq <= 64) {
-        const Tile t = tile_by_length(c, rank, TR, TK);
+        const Tile t = tile_by_length(c, rest, a.splits, TR, TK);
         if (t.tile == kNoTile) return;
+        split = t.split;
         seq = t.seq;
         s = t.s;
         row0 = t.tile * TR;
     } else {
-        const uint32_t tile = a.tiles - 1 - rank;
+        split = rest / a.tiles;
+        const uint32_t tile = a.tiles - 1 - rest % a.tiles;
         seq = seq_of_tile(c, tile, TR);
         s = load_seq(c, seq);
         row0 = (tile - first_tile(c, seq, TR)) * TR;
     }
     // the same for all lanes, whichever way they came
+    split = __builtin_amdgcn_readfirstlane(split);
     seq = __builtin_amdgcn_readfirstlane(seq);
     row0 = __builtin_amdgcn_readfirstlane(row0);
     s = {__builtin_amdgcn_readfirstlane(s.q_begin), __builtin_amdgcn_readfirstlane(s.n_q), __builtin_amdgcn_readfirstlane(s.kv)};
@@ -250,8 +251,8 @@ __global__ __launch_bounds__(NW * 64, row_occupancy(DP, NW)) void attention_rows
     const bool piece_live = (uint32_t)load_piece * 8 < c.head_dim;
     const Offset piece_at = piece_live ? load_piece * (E8 ? 8 : 16) : 0;
     const int32_t *table = c.table + (uint64_t)seq * c.table_stride;
-    std::conditional_t<E8, w2, w4> rk[N], rv[N];     // 8 elements each
-    uint32_t xk[XW], xv[XW];                         // exponents of this lane's key in 8-bit pages
+    std::conditional_t<E8, w2, w4> rk[AHEAD][N], rv[AHEAD][N];   // 8 elements each
+    uint32_t xk[AHEAD][XW], xv[AHEAD][XW];                         // exponents of this lane's key in 8-bit pages
 
     auto slot_at = [&](int32_t t) __attribute__((always_inline)) {   // table entry of this lane's key of tile t
         return load4g(table + block_of(c, min(keys.begin + t * TK + lane, keys.end - 1)));
@@ -308,7 +309,7 @@ __global__ __launch_bounds__(NW * 64, row_occupancy(DP, NW)) void attention_rows
     // Rows of 64 elements lie two to 64 banks of LDS, longer ones fill them: the pieces of a row change places with
     // its number, so that 16 rows read at one place of K, and four at four places of V, meet different banks.  PASS
     // and the steps between the rows that a lane reads leave the number's low bits as they are: one place to a lane.
-    auto k_place = [&](int r) __attribute__((always_inline)) { return DP >= 128 ? r & (PASS >= 16 ? 15 : PASS >= 8 ? 7 : 3) : (r >> 1) & 7; };
+    auto k_place = [&](int r) __attribute__((always_inline)) { return DP >= 128 ? r & (PASS >= 16 ? 15 : 7) : (r >> 1) & 7; };
     auto v_place = [&](int r) __attribute__((always_inline)) { return DP >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2; };
     const uint32_t k_store = load_row * DP * 2 + (load_piece ^ k_place(load_row)) * 16;
     const uint32_t v_store = load_row * DP * 2 + (load_piece ^ v_place(load_row)) * 16;
@@ -343,22 +344,22 @@ __global__ __launch_bounds__(NW * 64, row_occupancy(DP, NW)) void attention_rows
 #pragma unroll
         for (int i = 0; i < N; ++i) *(w4 *)(lds + (v_store + buffer) + i * PASS * DP * 2) = x[i];
     };
-    auto store_k = [&](uint32_t buffer) __attribute__((always_inline)) {
+    auto store_k = [&](uint32_t buffer, int set) __attribute__((always_inline)) {
         if constexpr (E8) {
             w4 x[N];
-            wide(rk, xk, x);
+            wide(rk[set], xk[set], x);
             put_k(buffer, x);
         } else {
-            put_k(buffer, rk);
+            put_k(buffer, rk[set]);
         }
     };
-    auto store_v = [&](int32_t t, uint32_t buffer, uint64_t seen) __attribute__((always_inline)) {
+    auto store_v = [&](int32_t t, uint32_t buffer, uint64_t seen, int set) __attribute__((always_inline)) {
         if constexpr (E8) {
             w4 x[N];
-            wide(rv, xv, x);
+            wide(rv[set], xv[set], x);
             put_v(t, buffer, seen, x);
         } else {
-            put_v(t, buffer, seen, rv);
+            put_v(t, buffer, seen, rv[set]);
         }
     };
 
@@ -433,8 +434,8 @@ __global__ __launch_bounds__(NW * 64, row_occupancy(DP, NW)) void attention_rows
     };
 
     if (tiles_n) {
-        // which keys of tiles t to t + 2 are there; the first half of the waves does not use the last
-        uint64_t seen0, seen1, seen2 = 0;
+        // which keys of tiles t to t + AHEAD + 1 are there; the first half of the waves does not use the last
+        uint64_t seen0, seen1, seen2 = 0, seen3 = 0;
         const int32_t slot0 = slot_at(0), slot1 = slot_at(1);
         uint32_t r0 = row_at(0, slot0), r1 = row_at(1, slot1);
         int32_t slot = slot_at(2);
@@ -442,34 +443,63 @@ __global__ __launch_bounds__(NW * 64, row_occupancy(DP, NW)) void attention_rows
         seen1 = __ballot(r1 != kNoRow);
         Offset at_v = offset_of(r0, slot0), at_k = offset_of(r1, slot1);
         Offset exponents_v = exponents_of(r0, slot0), exponents_k = exponents_of(r1, slot1);
-        load(a.k, at_v, rk);
-        load(a.v, at_v, rv);
-        load_exponents(a.k, exponents_v, xk);
-        load_exponents(a.v, exponents_v, xv);
-        store_k(0);
+        load(a.k, at_v, rk[0]);
+        if (AHEAD == 1 || second) load(a.v, at_v, rv[0]);
+        load_exponents(a.k, exponents_v, xk[0]);
+        if (AHEAD == 1 || second) load_exponents(a.v, exponents_v, xv[0]);
+        store_k(0, 0);
 #pragma unroll
         for (int i = 0; i < N; ++i) *(w4 *)(lds + (v_store + 3 * BUF) + i * PASS * DP * 2) = w4{0, 0, 0, 0};   // "V(-1)"
-        load(a.k, at_k, rk);
-        load_exponents(a.k, exponents_k, xk);
+        if (AHEAD == 1 || second) {
+            load(a.k, at_k, rk[0]);
+            load_exponents(a.k, exponents_k, xk[0]);
+        }
         int32_t next = 2;                            // tile of the next K to load; slot is its table entry
-        // stores the pair that was loaded to the buffers of parity odd and starts the next one's loads
-        auto pass_on = [&](int32_t t, bool odd, uint64_t seen) __attribute__((always_inline)) {   // t: V's tile
-            const uint32_t r = row_at(next, slot);   // before the loads: so that it does not wait for them
+        // starts the loads of the next pair into a set of registers
+        auto ask = [&](int set) __attribute__((always_inline)) {
+            ++next;
+            if constexpr (AHEAD == 2) slot = slot_at(next);   // first: so that using it does not wait for the pair
+            load(a.v, at_v, rv[set]);                // past the last tile: some row
+            load(a.k, at_k, rk[set]);
+            load_exponents(a.v, exponents_v, xv[set]);
+            load_exponents(a.k, exponents_k, xk[set]);
+            if constexpr (AHEAD == 1) slot = slot_at(next);
+        };
+        auto move_on = [&](uint32_t r) __attribute__((always_inline)) {
             at_v = at_k;
             at_k = offset_of(r, slot);
             exponents_v = exponents_k;
             exponents_k = exponents_of(r, slot);
-            store_v(t, odd ? 3 * BUF : 2 * BUF, seen);
-            store_k(odd ? 0 : BUF);
-            load(a.v, at_v, rv);                     // past the last tile: some row
-            load(a.k, at_k, rk);
-            load_exponents(a.v, exponents_v, xv);
-            load_exponents(a.k, exponents_k, xk);
-            ++next;
-            slot = slot_at(next);
+        };
+        // stores the pair that was loaded to the buffers of parity odd and starts the loads of another
+        auto pass_on = [&](int32_t t, bool odd, uint64_t seen, int set) __attribute__((always_inline)) {   // t: V's tile
+            const uint32_t r = row_at(next, slot);   // before the loads: so that it does not wait for them
+            move_on(r);
+            store_v(t, odd ? 3 * BUF : 2 * BUF, seen, set);
+            store_k(odd ? 0 : BUF, set);
+            ask(set);
             return __ballot(r != kNoRow);
         };
-        if (second) seen2 = pass_on(0, false, seen0);
+        if constexpr (AHEAD == 2) {
+            // the sets take turns, the second half's a stage earlier: an iteration uses the same one in both
+            const uint32_t r = row_at(next, slot);
+            if (second) {
+                move_on(r);
+                ask(1);
+                seen2 = __ballot(r != kNoRow);
+                seen3 = pass_on(0, false, seen0, 0);
+            } else {
+                load(a.v, at_v, rv[AHEAD - 1]);
+                load(a.k, at_k, rk[AHEAD - 1]);
+                load_exponents(a.v, exponents_v, xv[AHEAD - 1]);
+                load_exponents(a.k, exponents_k, xk[AHEAD - 1]);
+                move_on(r);
+                ask(0);
+                seen2 = __ballot(r != kNoRow);
+            }
+        } else {
+            if (second) seen2 = pass_on(0, false, seen0, 0);
+        }
         __syncthreads();
         if (second) __syncthreads();
         auto iteration = [&](int32_t t, auto buffer) __attribute__((always_inline)) {
@@ -477,10 +507,17 @@ __global__ __launch_bounds__(NW * 64, row_occupancy(DP, NW)) void attention_rows
             products(buf * BUF, (3 - buf) * BUF);
             __syncthreads();
             softmax(t, seen0);
-            const uint64_t after = pass_on(second ? t + 1 : t, second != (buf == 1), second ? seen1 : seen0);
+            const uint64_t after = pass_on(second ? t + 1 : t, second != (buf == 1), second ? seen1 : seen0,
+                                           AHEAD == 2 ? 1 - buf : 0);
             seen0 = seen1;
-            seen1 = second ? seen2 : after;
-            seen2 = after;
+            if constexpr (AHEAD == 2) {
+                seen1 = seen2;
+                seen2 = second ? seen3 : after;
+                seen3 = after;
+            } else {
+                seen1 = second ? seen2 : after;
+                seen2 = after;
+            }
             __syncthreads();
         };
         for (int32_t t = 0;; t += 2) {
@@ -886,18 +923,351 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
     }
 }
 
-template <class T, int DP, int KIND, int NW>
+// ---- up to 32 or 64 rows, the waves split the keys
+
+// The rest-th part of the keys of a batch of up to 64 sequences: those that hold keys first, sequence by sequence, then the
+// empty ones.  Workgroups begin in this order on one place of the chip after the other, whether they have work or not.
+struct Part {
+    uint32_t seq, split;
+    Seq s;
+};
+__device__ __forceinline__ Part part_of(const AttentionArgs &a, uint32_t rest, bool tree)
+{
+    const uint32_t lane = threadIdx.x & 63;
+    Seq s = load_seq(a.c, min(lane, a.c.n_seq - 1));
+    if (lane >= a.c.n_seq) s.n_q = 0;
+    uint32_t parts = 0;                              // of this lane's sequence that hold keys
+    if (s.n_q) {
+        const Split first = keys_of(a, s, tree ? -1 : 0, s.n_q - 1, 0);
+        const uint32_t span = (uint32_t)max(s.kv - first.begin, 0);
+        parts = min((span + a.split_keys - 1) / a.split_keys, a.splits);
+    }
+    const uint32_t upto = sum_upto(parts), all = (uint32_t)__builtin_amdgcn_readlane(upto, 63);
+    const uint32_t empty = s.n_q ? a.splits - parts : 0, empty_upto = sum_upto(empty);
+    const bool held = rest < all;
+    const uint32_t at = held ? rest : rest - all;
+    const uint64_t found = __ballot((held ? upto : empty_upto) > at);
+    if (!found) return {kNoTile, 0, s};
+    const int who = __ffsll((unsigned long long)found) - 1;
+    auto from = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane(x, who); };
+    s = {(int32_t)from(s.q_begin), (int32_t)from(s.n_q), (int32_t)from(s.kv)};
+    const uint32_t split = held ? at - (from(upto) - from(parts)) : from(parts) + at - (from(empty_upto) - from(empty));
+    return {(uint32_t)who, split, s};
+}
+
+// Drafts of a few tokens, whose group's heads make 17 to 64 rows: attention_few with products of 32 rows.  A wave has 32
+// rows and 32 keys at a time, which its lanes take from memory as the products want them; values pass through the wave's
+// own part of LDS, to be read by columns.  With two groups of rows (RG) neighbouring waves load the same keys.
+template <class T, int DP, int KIND, int RG>
+__global__ __launch_bounds__(kFewWaves * RG * 64, DP > 128 ? 1 : 2) void attention_some(const AttentionArgs a)
+{
+    constexpr bool E8 = KIND == kEight;
+    constexpr int XW = E8 ? (DP + 127) / 128 : 1;    // words of exponents to a row of 8-bit pages
+    constexpr int NW = kFewWaves, TK = kFewKeys;
+    constexpr int EL = E8 ? 16 : 8;                  // elements of a load
+    constexpr int CH = DP / EL;
+    constexpr int PASS = 64 / CH;                    // rows that a wave loads at once
+    constexpr int N = TK / PASS;
+    constexpr int KS = DP / 16;                      // products of a step with K, 8 elements to a lane
+    constexpr int RS = DP + 4;                       // words of a row in the join: rows begin in different banks
+    // each wave's values, and at the end its part of the output: [wave][rows][DP] in 32 bits
+    constexpr int VB = NW * RG * TK * DP * 2, OB = NW * RG * 32 * RS * 4;
+    __shared__ __align__(16) char lds[VB > OB ? VB : OB];
+    __shared__ float lds_ml[NW][2][RG * 32];
+
+    const CacheView &c = a.c;
+    const uint32_t kv_head = blockIdx.x % c.kv_heads;
+    const uint32_t rest = blockIdx.x / c.kv_heads;
+    const int tid = threadIdx.x, lane = tid & 63, place = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wave = place / RG, row0 = place % RG * 32;   // among the keys and among the rows
+    const bool tree = a.tree;
+    uint32_t split = rest % a.splits, seq = rest / a.splits;
+    Seq s;
+    if (a.splits > 1 && c.n_seq > 1 && c.n_seq <= 64) {
+        const Part p = part_of(a, rest, tree);
+        split = __builtin_amdgcn_readfirstlane(p.split);
+        seq = __builtin_amdgcn_readfirstlane(p.seq);
+        if (seq == kNoTile) return;
+        s = {__builtin_amdgcn_readfirstlane(p.s.q_begin), __builtin_amdgcn_readfirstlane(p.s.n_q), __builtin_amdgcn_readfirstlane(p.s.kv)};
+    } else {
+        s = load_seq(c, seq);
+    }
+    const int32_t *table = c.table + (uint64_t)seq * c.table_stride;
+    const uint32_t rows = (uint32_t)s.n_q * c.group;   // at most 32 RG
+    if (!rows) return;
+    const Split keys = keys_of(a, s, tree ? -1 : 0, s.n_q - 1, split);
+    if (a.splits > 1 && keys.begin >= keys.end) {      // of no weight: its output is not looked at
+        for (uint32_t r = tid; r < rows; r += kFewWaves * RG * 64) {
+            const uint32_t t = token_of(c, r), h = kv_head * c.group + r - t * c.group;
+            *(v2f *)(a.part_ml + 2 * ((uint64_t)split * c.total_q * c.heads + ((uint64_t)s.q_begin + t) * c.heads + h)) = v2f{kLowest, 0.0f};
+        }
+        return;
+    }
+
+    const int col = lane & 31, half = lane >> 5;
+    // with a tree: what is said here of the keys that a row sees holds for those before the new tokens
+    const int32_t shift = s.kv - s.n_q;
+    const uint32_t row = min((uint32_t)(row0 + col), rows - 1);
+    const int32_t token = (int32_t)token_of(c, row);
+    const uint32_t head = kv_head * c.group + row - (uint32_t)token * c.group;
+    const int32_t limit = tree ? shift - 1 : min(shift + token, s.kv - 1);
+    const int64_t end = tree && a.window ? (int64_t)shift + tree_depth(a, s, token) : (int64_t)limit + 1;
+    const int32_t floor_key = a.window ? (int32_t)max(end - (int64_t)a.window, (int64_t)0) : 0;
+    // a product's 16 elements, 8 to a lane: neighbours, or for 8-bit pages those that two products' lanes load as 16
+    auto element_of = [&](int i) __attribute__((always_inline)) {
+        return E8 ? 32u * (i / 2) + 16 * half + 8 * (i & 1) : 16u * i + 8 * half;
+    };
+    w4 q[KS];
+    {
+        const uint16_t *p = a.q + (uint64_t)(s.q_begin + token) * a.q_stride + (uint64_t)head * c.head_dim;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            const uint32_t at = element_of(i);
+            q[i] = load16g(p + (at < c.head_dim ? at : 0));
+            if (c.head_dim != DP && at >= c.head_dim) q[i] = w4{0, 0, 0, 0};
+        }
+    }
+    const int32_t all_first = tree ? shift - 1 : shift;   // last key that every row sees
+    const int64_t all_full = a.window ? (int64_t)s.kv - (int64_t)a.window : 0;   // first key that every row sees
+
+    v16f o[DP / 32];
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i) o[i] = v16f{};
+    float m = kLowest, l = 0.0f;
+
+    const int load_piece = lane % CH, load_row = lane / CH;
+    const bool piece_live = (uint32_t)load_piece * EL < c.head_dim;
+    const uint32_t piece_at = piece_live ? load_piece * EL : 0;
+    const int32_t mine = keys.begin + wave * TK;     // this wave's first keys; then every NW * TK
+    const int32_t steps = keys.end > mine ? (keys.end - mine + NW * TK - 1) / (NW * TK) : 0;
+
+    bool bounded = true;                             // the values of tiles that not all rows see are finite
+    w4 rk[KS * 8 / EL], rv[N];
+    uint32_t exponents[XW];                          // lane i: of key i, and lane i + 32 of value i
+    uint32_t seen_next = 0;
+    auto slot_at = [&](int32_t t) __attribute__((always_inline)) {
+        const int32_t key = mine + t * (NW * TK) + col;
+        return load4g(table + block_of(c, min(key, keys.end - 1)));
+    };
+    auto load_tile = [&](int32_t t, int32_t slot) __attribute__((always_inline)) {
+        const int32_t key = mine + t * (NW * TK) + col;
+        const uint32_t r = row_of(c, key < keys.end ? slot : -1, kv_head, key);
+        seen_next = (uint32_t)__ballot(r != kNoRow);
+        uint64_t at_row;                             // bytes
+        if constexpr (E8) {
+            const uint64_t base = r == kNoRow ? 0 : (uint64_t)(uint32_t)slot * a.slot_bytes;
+            const uint64_t row = r == kNoRow ? 0 : r - (uint32_t)slot * (c.kv_heads * c.block);
+            at_row = base + row * c.head_dim;
+            const uint8_t *x = (const uint8_t *)(lane < 32 ? a.k : a.v) + base + a.exponents + row * a.row_exponents;
+#pragma unroll
+            for (int w = 0; w < XW; ++w) exponents[w] = (uint32_t)load4g((const int32_t *)x + w);
+        } else {
+            at_row = (uint64_t)(r == kNoRow ? 0 : r) * (c.head_dim * 2);
+        }
+        const uint8_t *p = (const uint8_t *)a.k + at_row;   // the lane's own key
+#pragma unroll
+        for (int i = 0; i < KS * 8 / EL; ++i) {
+            const uint32_t at = E8 ? 32u * i + 16 * half : 16u * i + 8 * half;
+            rk[i] = load16g((const uint16_t *)(p + (at < c.head_dim ? at : 0) * (E8 ? 1 : 2)));   // past the end: q is 0 there
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            rv[i] = load16g((const uint16_t *)((const uint8_t *)a.v + lane_value(at_row, load_row + i * PASS) +
+                                                  piece_at * (E8 ? 1 : 2)));
+    };
+    char *vs = lds + place * (TK * DP * 2);
+    auto v_place = [&](int r) __attribute__((always_inline)) { return DP >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2; };
+    uint32_t v_read[DP / 32];
+    {
+        const int ti = lane & 15, r = 4 * half + ti / 4;
+#pragma unroll
+        for (int i = 0; i < DP / 32; ++i)
+            v_read[i] = r * DP * 2 + ((4 * i + 2 * (lane >> 4 & 1) + (ti % 4) / 2) ^ v_place(r)) * 16 + (ti & 1) * 8;
+    }
+
+    int32_t slot_next = -1;
+    if (steps) {
+        const int32_t slot0 = slot_at(0);
+        slot_next = slot_at(1);
+        loads_arrived();
+        load_tile(0, slot0);
+    }
+    for (int32_t t = 0; t < steps; ++t) {
+        const uint32_t seen = seen_next;
+        const int32_t k0 = mine + t * (NW * TK);
+        const bool edge = !(k0 + TK - 1 <= all_first && (int64_t)k0 >= all_full);   // not all rows see these keys
+        v16f z{};
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            w4 k;
+            if constexpr (E8) {
+                const w4 x = rk[i / 2];
+                const uint32_t word = lane_value(exponents[i / 8], col);   // 32 elements: two products
+                k = widen<T>(i & 1 ? w2{x[2], x[3]} : w2{x[0], x[1]}, power_of(word, i / 2 % 4 * 8));
+            } else {
+                k = rk[i];
+            }
+            if (c.head_dim != DP && element_of(i) >= c.head_dim) k = w4{0, 0, 0, 0};
+            z = T::mma32(k, q[i], z);
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int r = load_row + i * PASS;
+            w4 v[EL / 8];
+            if constexpr (E8) {
+                uint32_t word = lane_value(exponents[0], 32 + r);
+                if constexpr (XW > 1) {
+                    const uint32_t other = lane_value(exponents[XW - 1], 32 + r);
+                    word = load_piece >= 8 ? other : word;
+                }
+                const float power = power_of(word, load_piece / 2 % 4 * 8);
+                v[0] = widen<T>(w2{rv[i][0], rv[i][1]}, power);
+                v[EL / 8 - 1] = widen<T>(w2{rv[i][2], rv[i][3]}, power);
+            } else {
+                v[0] = rv[i];
+            }
+#pragma unroll
+            for (int j = 0; j < EL / 8; ++j) {
+                const bool there = (uint32_t)(EL * load_piece + 8 * j) < c.head_dim && (seen >> r & 1);
+                if (!there) v[j] = w4{0, 0, 0, 0};
+                if (__builtin_expect(edge, 0)) bounded &= T::bound(v[j]);
+                *(w4 *)(vs + r * DP * 2 + (((EL / 8) * load_piece + j) ^ v_place(r)) * 16) = v[j];
+            }
+        }
+        if (t + 1 < steps) {
+            load_tile(t + 1, slot_next);
+            slot_next = slot_at(t + 2);
+        }
+        w4 p[2];
+        if (edge || seen != ~0u) {
+            const uint32_t here = seen >> (4 * half);
+            const uint32_t drafted = tree ? ((uint32_t)tree_bits(a, s, token, k0 - shift) & seen) >> (4 * half) : 0;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int at = 8 * (r / 4) + r % 4;
+                const int32_t key = k0 + at + 4 * half;
+                const bool sees = (key <= limit && key >= floor_key && (here >> at & 1)) || (drafted >> at & 1);
+                z[r] = sees ? z[r] : -INFINITY;
+            }
+        }
+        float top = z[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) top = fmaxf(top, z[r]);
+        top = fmaxf(top, other_half(top)) * a.scale_log2;
+        if (__any(top > m + (8.0f + T::kLift))) {   // as in attention_rows
+            const float to = fmaxf(m, top - T::kLift);
+            const float f = exp2_fast(m - to);
+            m = to;
+            l *= f;
+#pragma unroll
+            for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[i][r] *= f;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int r = 8 * i + 2 * j;
+                const float x = exp2_fast(__builtin_fmaf(z[r], a.scale_log2, -m));
+                const float y = exp2_fast(__builtin_fmaf(z[r + 1], a.scale_log2, -m));
+                l += x;
+                l += y;
+                p[i][j] = T::pack(x, y);
+            }
+        // the wave's own values: LDS keeps a wave's accesses in order
+        wave_lds_order();
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int db = 0; db < DP / 32; ++db) {
+                const char *v = vs + v_read[db] + i * 16 * DP * 2;
+                const w2 x = read_down((const uint16_t *)v), y = read_down((const uint16_t *)(v + 8 * DP * 2));
+                const w4 value = {x[0], x[1], y[0], y[1]};
+                o[db] = T::mma32(value, p[i], o[db]);
+            }
+        wave_lds_order();
+    }
+
+    if (__builtin_expect(__any(!bounded), 0)) {
+        for (int32_t t = 0; t < steps; ++t) {
+            const int32_t k0 = mine + t * (NW * TK), key = k0 + col;
+            if (k0 + TK - 1 <= all_first && (int64_t)k0 >= all_full) continue;
+            const uint32_t r = row_of(c, key < keys.end ? slot_at(t) : -1, kv_head, key);
+            const bool found = r != kNoRow && unbounded_row<T, KIND>(a, r);
+            for (uint32_t left = (uint32_t)__ballot(found); left; left &= left - 1) {
+                const int j = __ffs(left) - 1;
+                const uint32_t at = (uint32_t)__builtin_amdgcn_readlane(r, j);
+                const float weight = weight_of<T, KIND>(a, q, at, m, element_of,
+                                                        [](float x) { return x + other_half(x); });
+                const bool drafted = tree && (tree_bits(a, s, token, k0 + j - shift) & 1);
+                if ((k0 + j > limit || k0 + j < floor_key) && !drafted) continue;
+#pragma unroll
+                for (int i = 0; i < DP / 8; ++i) {
+                    const uint32_t d = 8 * i + 4 * half;
+                    if (d >= c.head_dim) continue;
+                    const w2 v = four_at<T, KIND>(a, at, d);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[i / 4][4 * (i % 4) + e] += unbounded_part<T>(v, e, weight);
+                }
+            }
+        }
+    }
+
+    // join the waves: scale each part to the common maximum, then add
+    l += other_half(l);
+    if (half == 0) {
+        lds_ml[wave][0][row0 + col] = m;
+        lds_ml[wave][1][row0 + col] = l;
+    }
+    __syncthreads();
+    float *parts = (float *)lds;
+    float top = lds_ml[0][0][row0 + col];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) top = fmaxf(top, lds_ml[w][0][row0 + col]);
+    const float f = exp2_fast(m - top);
+#pragma unroll
+    for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            *(v4f *)&parts[(wave * RG * 32 + row0 + col) * RS + db * 32 + 8 * j + 4 * half] =
+                v4f{o[db][4 * j] * f, o[db][4 * j + 1] * f, o[db][4 * j + 2] * f, o[db][4 * j + 3] * f};
+    __syncthreads();
+    for (uint32_t i = tid; i < rows * (DP / 4); i += NW * RG * 64) {
+        const uint32_t r = i / (DP / 4), at = i % (DP / 4) * 4;
+        if (at >= c.head_dim) continue;
+        v4f sum = *(v4f *)&parts[r * RS + at];
+        float mm = lds_ml[0][0][r], ll = 0.0f;
+#pragma unroll
+        for (int w = 1; w < NW; ++w) {
+            sum += *(v4f *)&parts[(w * RG * 32 + r) * RS + at];
+            mm = fmaxf(mm, lds_ml[w][0][r]);
+        }
+#pragma unroll
+        for (int w = 0; w < NW; ++w) ll += lds_ml[w][1][r] * exp2_fast(lds_ml[w][0][r] - mm);
+        const uint32_t t = token_of(c, r), h = kv_head * c.group + r - t * c.group;
+        const uint64_t out_row = (uint64_t)s.q_begin + t;
+        if (a.splits == 1) {
+            const RowEnd e = finish_row(mm, ll, a.sinks, h);
+            uint16_t *p = a.out + out_row * a.out_stride + (uint64_t)h * c.head_dim + at;
+            *(w2 *)p = w2{T::pack(sum[0] * e.scale_o, sum[1] * e.scale_o), T::pack(sum[2] * e.scale_o, sum[3] * e.scale_o)};
+            if (a.lse && at == 0) a.lse[(uint64_t)h * c.total_q + out_row] = e.lse;
+        } else {
+            const uint64_t part = (uint64_t)split * c.total_q * c.heads + out_row * c.heads + h;
+            *(v4f *)(a.part_o + part * c.head_dim + at) = sum;
+            if (at == 0) *(v2f *)(a.part_ml + 2 * part) = v2f{mm, ll};
+        }
+    }
+}
+
+template <class T, int DP, int KIND>
 hipError_t rows_as(const AttentionArgs &a, hipStream_t stream)
 {
     const uint32_t grid = a.tiles * a.splits * a.c.kv_heads;
-    // offsets of 32 bits are for the vector unit's sake, which small tiles do not fill
-    if constexpr (NW == row_waves(DP)) {
-        if ((uint64_t)a.c.num_slots * a.slot_bytes <= 0xFFFFFFFFull) {
-            attention_rows<T, DP, uint32_t, KIND, NW><<<grid, NW * 64, 0, stream>>>(a);
-            return hipGetLastError();
-        }
-    }
-    attention_rows<T, DP, uint64_t, KIND, NW><<<grid, NW * 64, 0, stream>>>(a);
+    if ((uint64_t)a.c.num_slots * a.slot_bytes <= 0xFFFFFFFFull)
+        attention_rows<T, DP, uint32_t, KIND><<<grid, row_waves(DP) * 64, 0, stream>>>(a);
+    else
+        attention_rows<T, DP, uint64_t, KIND><<<grid, row_waves(DP) * 64, 0, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -906,14 +1276,16 @@ template <class T, int DP, int KIND>
 hipError_t by_rows(const AttentionArgs &a, hipStream_t stream)
 {
     if (a.few_rows) {
-        attention_few<T, DP, KIND><<<a.tiles * a.splits * a.c.kv_heads, kFewWaves * 64, 0, stream>>>(a);
+        const uint32_t grid = a.tiles * a.splits * a.c.kv_heads;
+        if (a.few_rows <= 16)
+            attention_few<T, DP, KIND><<<grid, kFewWaves * 64, 0, stream>>>(a);
+        else if (a.few_rows <= 32)
+            attention_some<T, DP, KIND, 1><<<grid, kFewWaves * 64, 0, stream>>>(a);
+        else if constexpr (some_rows(DP) > 32)
+            attention_some<T, DP, KIND, 2><<<grid, kFewWaves * 128, 0, stream>>>(a);
         return hipGetLastError();
     }
-    if (a.waves == 2) return rows_as<T, DP, KIND, 2>(a, stream);
-    if constexpr (row_waves(DP) > 4) {
-        if (a.waves == 4) return rows_as<T, DP, KIND, 4>(a, stream);
-    }
-    return rows_as<T, DP, KIND, row_waves(DP)>(a, stream);
+    return rows_as<T, DP, KIND>(a, stream);
 }
 template <class T, int KIND>
 hipError_t by_head_dim(const AttentionArgs &a, hipStream_t stream)

@@ -95,8 +95,13 @@ void need_rows(const void *p, uint64_t stride, uint64_t least, const char *what)
     need(stride <= 1ull << 40, "a stride of more than 2^40 elements");
 }
 
+// Rows of a sequence up to which the waves split the keys, and the parts that such a call is cut into.
+struct CutRule {
+    uint32_t few_rows, parts;
+};
+
 struct Cut {
-    bool few;
+    uint32_t few;     // most rows of a sequence, or 0: tiles of rows
     uint32_t tiles, splits, split_keys;
     uint64_t bytes;   // of workspace
 };
@@ -104,14 +109,17 @@ struct Cut {
 // How an attention call is cut.  A KV head's rows (new tokens x group) go to attention_few if no sequence has more
 // than a 16-row product holds, else to tiles of 256 (128 at a head_dim of more than 128).  Where the tiles do not
 // fill the chip, the keys are split, as far as a part holds enough keys to be worth its output's way through memory.
-Cut cut_of(const CacheView &c, uint32_t window, uint32_t waves)
+Cut cut_of(const CacheView &c, uint32_t window, const CutRule &rule)
 {
     Cut p{};
     const uint64_t rows = (uint64_t)c.total_q * c.group;
-    const uint32_t tile_rows = waves * 32;
-    const bool few = p.few = (uint64_t)c.max_q * c.group <= kFewRows;
+    const uint32_t tile_rows = row_waves(c.head_dim) * 32;
+    const bool few = (uint64_t)c.max_q * c.group <= rule.few_rows;
+    p.few = few ? std::max(1u, c.max_q * c.group) : 0;
     if (!rows) return p.splits = 1, p.split_keys = kTileKeys, p;
-    p.tiles = few ? c.n_seq : (uint32_t)(rows / tile_rows + c.n_seq);
+    p.tiles = few            ? c.n_seq
+              : c.n_seq == 1 ? (uint32_t)((rows + tile_rows - 1) / tile_rows)
+                             : (uint32_t)(rows / tile_rows + c.n_seq);
     const uint64_t tile_tokens = few ? c.max_q : std::min<uint64_t>(c.max_q, tile_rows / c.group + 2);
     uint64_t span = c.max_kv;
     if (window) span = std::min<uint64_t>(span, (uint64_t)window + tile_tokens + kTileKeys);
@@ -121,12 +129,12 @@ Cut cut_of(const CacheView &c, uint32_t window, uint32_t waves)
                                            : std::max<uint64_t>(c.n_seq, rows / tile_rows + c.n_seq / 2)) * c.kv_heads;
     uint64_t keys = span;                            // of a part
     if (few) {
-        // about 1024 parts, which read the cache at its full rate, and not above 1024 keys where lengths may differ, so
+        // about 1024 parts (by the rule), which read the cache at its full rate, and not above 1024 keys where lengths may differ, so
         // that none is left alone at the end.  32 sequences of up to 16K: 191 us at 1024 keys, 210 at 512, 223 at 4096;
         // one of 128K: 47 us at 1024, 49 at 512, 67 at 128.  256 keys stay whole: 8.5 us, where two parts and their join
         // take 10.8.
         if (span > 256) {
-            keys = std::max<uint64_t>(128, units * span / 1024);
+            keys = std::max<uint64_t>(128, units * span / rule.parts);
             if (c.n_seq > 1) keys = std::min<uint64_t>(keys, 1024);
             keys = std::max(keys, units * span / kMostParts);
         }
@@ -143,7 +151,7 @@ Cut cut_of(const CacheView &c, uint32_t window, uint32_t waves)
         keys = (span + best - 1) / best;
     }
     // no more parts than without a window: the workspace is asked for without one
-    if (window) keys = std::max(keys, (span + cut_of(c, 0, waves).splits - 1) / cut_of(c, 0, waves).splits);
+    if (window) keys = std::max(keys, (span + cut_of(c, 0, rule).splits - 1) / cut_of(c, 0, rule).splits);
     const uint64_t unit = few ? 128 : kTileKeys;
     keys = std::max(unit, (keys + unit - 1) / unit * unit);
     p.splits = (uint32_t)std::max<uint64_t>(1, (span + keys - 1) / keys);
@@ -152,19 +160,11 @@ Cut cut_of(const CacheView &c, uint32_t window, uint32_t waves)
     return p;
 }
 
-uint64_t attention_bytes(const CacheView &c) { return cut_of(c, 0, row_waves(c.head_dim)).bytes; }
+Cut attention_cut(const CacheView &c, uint32_t window) { return cut_of(c, window, {kFewRows, 1024}); }
 
-// Waves of 32 rows to a row tile of attention over pages.
-uint32_t page_waves(const CacheView &c)
-{
-    const uint64_t rows = (uint64_t)c.max_q * c.group;
-    const uint32_t most = row_waves(c.head_dim);
-    return rows <= 64 ? 2 : rows <= 128 ? std::min(4u, most) : most;
-}
-uint64_t attention_pages_bytes(const CacheView &c)
-{
-    return std::max(attention_bytes(c), cut_of(c, 0, page_waves(c)).bytes);
-}
+// Half as many parts: they move half the bytes of 8-bit pages, or join the outputs of more rows.  One token over 128K in 8
+// bits (32 heads, 8 KV heads, 128) 58.0 us, 62.0 at 1024 parts; trees of 8 and of 16 tokens over 128K 63 and 92, 72 and 106.
+Cut pages_cut(const CacheView &c, uint32_t window) { return cut_of(c, window, {some_rows(c.head_dim), 512}); }
 
 uint32_t row_exponents(uint32_t head_dim) { return (head_dim + 127) / 128 * 4; }
 
@@ -227,7 +227,7 @@ namespace {
 
 // What every attention call checks and says to its kernels, but for the tensors that the cut makes launches of.
 void fill_attention(AttentionArgs &a, const void *q, uint64_t q_stride, const void *k, const void *v, float scale,
-                    uint32_t window, const float *sinks, void *out, uint64_t out_stride, float *lse, uint32_t waves,
+                    uint32_t window, const float *sinks, void *out, uint64_t out_stride, float *lse, const Cut &p,
                     void *workspace, uint64_t workspace_bytes, const char *too_small)
 {
     const uint64_t row = (uint64_t)a.c.heads * a.c.head_dim;
@@ -237,7 +237,6 @@ void fill_attention(AttentionArgs &a, const void *q, uint64_t q_stride, const vo
     need_pointer(v, 16, "v_cache");
     need(aligned(sinks, 4), "sinks is not aligned to 4 bytes");
     need(aligned(lse, 4), "lse is not aligned to 4 bytes");
-    const Cut p = cut_of(a.c, window, waves);
     if (p.bytes) {
         need_pointer(workspace, 16, "workspace");
         need(workspace_bytes >= p.bytes, too_small);
@@ -259,7 +258,6 @@ void fill_attention(AttentionArgs &a, const void *q, uint64_t q_stride, const vo
     const uint64_t parts = (uint64_t)p.splits * a.c.total_q * a.c.heads;
     a.part_o = static_cast<float *>(workspace);
     a.part_ml = a.part_o ? a.part_o + parts * a.c.head_dim : nullptr;
-    a.waves = waves;
 }
 
 }  // namespace
@@ -267,7 +265,7 @@ void fill_attention(AttentionArgs &a, const void *q, uint64_t q_stride, const vo
 void op_attention_workspace(const kvp_cache_shape *s, const kvp_batch *b, uint64_t *bytes)
 {
     need(bytes, "bytes is null");
-    *bytes = attention_bytes(view_of(s, b, true, false));
+    *bytes = attention_cut(view_of(s, b, true, false), 0).bytes;
 }
 
 void op_attention(const kvp_cache_shape *s, const kvp_batch *b, const void *q, uint64_t q_stride, const void *k,
@@ -278,7 +276,7 @@ void op_attention(const kvp_cache_shape *s, const kvp_batch *b, const void *q, u
     a.c = view_of(s, b, true);
     need_scale(scale);
     if (a.c.total_q == 0) return;
-    fill_attention(a, q, q_stride, k, v, scale, window, sinks, out, out_stride, lse, row_waves(a.c.head_dim), workspace,
+    fill_attention(a, q, q_stride, k, v, scale, window, sinks, out, out_stride, lse, attention_cut(a.c, window), workspace,
                    workspace_bytes, "workspace is smaller than kv_attention_workspace says");
     const hipStream_t st = static_cast<hipStream_t>(stream);
     check_hip(launch_attention(a, s->dtype, st), "attention launch");
@@ -288,7 +286,8 @@ void op_attention(const kvp_cache_shape *s, const kvp_batch *b, const void *q, u
 void op_attention_pages_workspace(const kvp_cache_shape *s, const kvp_batch *b, uint64_t *bytes)
 {
     need(bytes, "bytes is null");
-    *bytes = attention_pages_bytes(view_of(s, b, true, false));
+    const CacheView c = view_of(s, b, true, false);
+    *bytes = std::max(attention_cut(c, 0).bytes, pages_cut(c, 0).bytes);   // causal ones of 16 bits are kv_attention's
 }
 
 void op_attention_pages(const kvp_cache_shape *s, const kvp_batch *b, const kvp_pages *pages, const uint64_t *tree,
@@ -306,8 +305,8 @@ void op_attention_pages(const kvp_cache_shape *s, const kvp_batch *b, const kvp_
     if (a.c.total_q == 0) return;
     const bool eight = pages->kind == KVP_PAGES_E4M3;
     // 16-bit pages under a causal mask are kv_attention's
-    const uint32_t waves = eight || tree ? page_waves(a.c) : row_waves(a.c.head_dim);
-    fill_attention(a, q, q_stride, p.k, p.v, scale, window, sinks, out, out_stride, lse, waves, workspace, workspace_bytes,
+    const Cut cut = eight || tree ? pages_cut(a.c, window) : attention_cut(a.c, window);
+    fill_attention(a, q, q_stride, p.k, p.v, scale, window, sinks, out, out_stride, lse, cut, workspace, workspace_bytes,
                    "workspace is smaller than kv_attention_pages_workspace says");
     a.exponents = p.exponents;
     a.row_exponents = p.row_exponents;

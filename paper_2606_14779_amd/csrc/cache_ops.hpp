@@ -39,12 +39,11 @@ struct AttentionArgs {
     const float *sinks;              // [heads] or null
     float scale_log2;                // scale * log2(e)
     uint32_t window;                 // 0: none
-    uint32_t few_rows;               // attention_few, else attention_rows
+    uint32_t few_rows;               // most rows of a sequence where the waves split the keys; 0: attention_rows
     uint32_t tiles, splits, split_keys;
     float *part_o;                   // [splits][total_q * heads][head_dim]
     float *part_ml;                  // [splits][total_q * heads][2]
     // of attention over pages alone
-    uint32_t waves;                  // of attention_rows
     uint32_t exponents, row_exponents;   // of 8-bit pages; 0: 16-bit elements
     uint64_t slot_bytes;
     const uint64_t *tree;            // [total_q][tree_words] or null
@@ -148,6 +147,8 @@ constexpr uint32_t kFewRows = 16;
 // 32 rows to a wave, two waves to a SIMD; at a head_dim of more than 128 the registers hold one.
 constexpr int row_waves(uint32_t head_dim) { return head_dim > 128 ? 4 : 8; }
 constexpr uint32_t kTileKeys = 64;
+// Rows of a sequence up to which attention over pages has its waves split the keys.
+constexpr uint32_t some_rows(uint32_t head_dim) { return head_dim > 128 ? 32 : 64; }
 
 constexpr uint32_t kConvertTokens = 64;    // to a workgroup
 

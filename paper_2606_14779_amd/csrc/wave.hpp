@@ -207,13 +207,15 @@ __device__ __forceinline__ uint32_t sum_upto(uint32_t x)
 
 // The rank-th longest row tile of a batch of up to 64 sequences: tiles of tile_rows rows (of a KV head) by the keys
 // that a causal mask leaves them, in units of `keys`; of equal ones the earlier sequence's first.  Workgroups begin
-// in this order, so that none with much to do begins last.  Ranks past the last tile give tile == none.
+// in this order, so that none with much to do begins last.  Where the keys are cut into parts, `index` counts the tiles
+// of one part after the other: indexes past the last part's last tile, tile == none, come after all that have work.
 struct Tile {
-    uint32_t seq, tile;
+    uint32_t seq, tile, split;
     Seq s;
 };
 constexpr uint32_t kNoTile = 0xFFFFFFFFu;
-__device__ __forceinline__ Tile tile_by_length(const CacheView &c, uint32_t rank, uint32_t tile_rows, uint32_t keys)
+__device__ __forceinline__ Tile tile_by_length(const CacheView &c, uint32_t index, uint32_t splits, uint32_t tile_rows,
+                                               uint32_t keys)
 {
     const uint32_t lane = threadIdx.x & 63;
     Seq s = load_seq(c, min(lane, c.n_seq - 1));
@@ -226,7 +228,8 @@ __device__ __forceinline__ Tile tile_by_length(const CacheView &c, uint32_t rank
         return token >= s.n_q ? 0u : tiles - (uint32_t)((uint64_t)token * c.group / tile_rows);
     };
     auto all = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane(sum_upto(x), 63); };
-    if (rank >= all(tiles)) return {0, kNoTile, s};
+    const uint32_t there = all(tiles), split = there ? index / there : splits, rank = index - split * there;
+    if (split >= splits) return {0, kNoTile, 0, s};
     uint32_t lo = 0, hi = c.max_kv / keys + 2;       // all(at_least(lo)) > rank >= all(at_least(hi))
     while (hi - lo > 1) {
         const uint32_t mid = (lo + hi) / 2;
@@ -241,7 +244,7 @@ __device__ __forceinline__ Tile tile_by_length(const CacheView &c, uint32_t rank
     const int who = __ffsll((unsigned long long)found) - 1;
     auto from = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane(x, who); };
     s = {(int32_t)from(s.q_begin), (int32_t)from(s.n_q), (int32_t)from(s.kv)};
-    return {(uint32_t)who, from(tiles) - from(longer + these) + left - (from(upto) - from(these)), s};
+    return {(uint32_t)who, from(tiles) - from(longer + these) + left - (from(upto) - from(these)), split, s};
 }
 
 }  // namespace kvp
