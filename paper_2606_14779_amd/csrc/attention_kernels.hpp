@@ -159,7 +159,6 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
 {
     constexpr int TK = kTileKeys, NW = row_waves(DP), TR = NW * 32;
     constexpr bool E8 = KIND == kEight;
-    constexpr int AHEAD = DP > 128 || KIND == kCausal16 ? 1 : 2;   // tiles that have been asked for and are not in LDS
     constexpr int XW = E8 ? (DP + 127) / 128 : 1;    // words of exponents to a row of 8-bit pages
     constexpr int CH = DP / 8;                       // 16-byte pieces of a row
     constexpr int PASS = NW * 64 / CH;               // rows that the workgroup loads at once
@@ -251,8 +250,8 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
     const bool piece_live = (uint32_t)load_piece * 8 < c.head_dim;
     const Offset piece_at = piece_live ? load_piece * (E8 ? 8 : 16) : 0;
     const int32_t *table = c.table + (uint64_t)seq * c.table_stride;
-    std::conditional_t<E8, w2, w4> rk[AHEAD][N], rv[AHEAD][N];   // 8 elements each
-    uint32_t xk[AHEAD][XW], xv[AHEAD][XW];                         // exponents of this lane's key in 8-bit pages
+    std::conditional_t<E8, w2, w4> rk[N], rv[N];     // 8 elements each
+    uint32_t xk[XW], xv[XW];                         // exponents of this lane's key in 8-bit pages
 
     auto slot_at = [&](int32_t t) __attribute__((always_inline)) {   // table entry of this lane's key of tile t
         return load4g(table + block_of(c, min(keys.begin + t * TK + lane, keys.end - 1)));
@@ -344,22 +343,22 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
 #pragma unroll
         for (int i = 0; i < N; ++i) *(w4 *)(lds + (v_store + buffer) + i * PASS * DP * 2) = x[i];
     };
-    auto store_k = [&](uint32_t buffer, int set) __attribute__((always_inline)) {
+    auto store_k = [&](uint32_t buffer) __attribute__((always_inline)) {
         if constexpr (E8) {
             w4 x[N];
-            wide(rk[set], xk[set], x);
+            wide(rk, xk, x);
             put_k(buffer, x);
         } else {
-            put_k(buffer, rk[set]);
+            put_k(buffer, rk);
         }
     };
-    auto store_v = [&](int32_t t, uint32_t buffer, uint64_t seen, int set) __attribute__((always_inline)) {
+    auto store_v = [&](int32_t t, uint32_t buffer, uint64_t seen) __attribute__((always_inline)) {
         if constexpr (E8) {
             w4 x[N];
-            wide(rv[set], xv[set], x);
+            wide(rv, xv, x);
             put_v(t, buffer, seen, x);
         } else {
-            put_v(t, buffer, seen, rv[set]);
+            put_v(t, buffer, seen, rv);
         }
     };
 
@@ -434,8 +433,8 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
     };
 
     if (tiles_n) {
-        // which keys of tiles t to t + AHEAD + 1 are there; the first half of the waves does not use the last
-        uint64_t seen0, seen1, seen2 = 0, seen3 = 0;
+        // which keys of tiles t to t + 2 are there; the first half of the waves does not use the last
+        uint64_t seen0, seen1, seen2 = 0;
         const int32_t slot0 = slot_at(0), slot1 = slot_at(1);
         uint32_t r0 = row_at(0, slot0), r1 = row_at(1, slot1);
         int32_t slot = slot_at(2);
@@ -443,63 +442,34 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
         seen1 = __ballot(r1 != kNoRow);
         Offset at_v = offset_of(r0, slot0), at_k = offset_of(r1, slot1);
         Offset exponents_v = exponents_of(r0, slot0), exponents_k = exponents_of(r1, slot1);
-        load(a.k, at_v, rk[0]);
-        if (AHEAD == 1 || second) load(a.v, at_v, rv[0]);
-        load_exponents(a.k, exponents_v, xk[0]);
-        if (AHEAD == 1 || second) load_exponents(a.v, exponents_v, xv[0]);
-        store_k(0, 0);
+        load(a.k, at_v, rk);
+        load(a.v, at_v, rv);
+        load_exponents(a.k, exponents_v, xk);
+        load_exponents(a.v, exponents_v, xv);
+        store_k(0);
 #pragma unroll
         for (int i = 0; i < N; ++i) *(w4 *)(lds + (v_store + 3 * BUF) + i * PASS * DP * 2) = w4{0, 0, 0, 0};   // "V(-1)"
-        if (AHEAD == 1 || second) {
-            load(a.k, at_k, rk[0]);
-            load_exponents(a.k, exponents_k, xk[0]);
-        }
+        load(a.k, at_k, rk);
+        load_exponents(a.k, exponents_k, xk);
         int32_t next = 2;                            // tile of the next K to load; slot is its table entry
-        // starts the loads of the next pair into a set of registers
-        auto ask = [&](int set) __attribute__((always_inline)) {
-            ++next;
-            if constexpr (AHEAD == 2) slot = slot_at(next);   // first: so that using it does not wait for the pair
-            load(a.v, at_v, rv[set]);                // past the last tile: some row
-            load(a.k, at_k, rk[set]);
-            load_exponents(a.v, exponents_v, xv[set]);
-            load_exponents(a.k, exponents_k, xk[set]);
-            if constexpr (AHEAD == 1) slot = slot_at(next);
-        };
-        auto move_on = [&](uint32_t r) __attribute__((always_inline)) {
+        // stores the pair that was loaded to the buffers of parity odd and starts the next one's loads
+        auto pass_on = [&](int32_t t, bool odd, uint64_t seen) __attribute__((always_inline)) {   // t: V's tile
+            const uint32_t r = row_at(next, slot);   // before the loads: so that it does not wait for them
             at_v = at_k;
             at_k = offset_of(r, slot);
             exponents_v = exponents_k;
             exponents_k = exponents_of(r, slot);
-        };
-        // stores the pair that was loaded to the buffers of parity odd and starts the loads of another
-        auto pass_on = [&](int32_t t, bool odd, uint64_t seen, int set) __attribute__((always_inline)) {   // t: V's tile
-            const uint32_t r = row_at(next, slot);   // before the loads: so that it does not wait for them
-            move_on(r);
-            store_v(t, odd ? 3 * BUF : 2 * BUF, seen, set);
-            store_k(odd ? 0 : BUF, set);
-            ask(set);
+            store_v(t, odd ? 3 * BUF : 2 * BUF, seen);
+            store_k(odd ? 0 : BUF);
+            load(a.v, at_v, rv);                     // past the last tile: some row
+            load(a.k, at_k, rk);
+            load_exponents(a.v, exponents_v, xv);
+            load_exponents(a.k, exponents_k, xk);
+            ++next;
+            slot = slot_at(next);
             return __ballot(r != kNoRow);
         };
-        if constexpr (AHEAD == 2) {
-            // the sets take turns, the second half's a stage earlier: an iteration uses the same one in both
-            const uint32_t r = row_at(next, slot);
-            if (second) {
-                move_on(r);
-                ask(1);
-                seen2 = __ballot(r != kNoRow);
-                seen3 = pass_on(0, false, seen0, 0);
-            } else {
-                load(a.v, at_v, rv[AHEAD - 1]);
-                load(a.k, at_k, rk[AHEAD - 1]);
-                load_exponents(a.v, exponents_v, xv[AHEAD - 1]);
-                load_exponents(a.k, exponents_k, xk[AHEAD - 1]);
-                move_on(r);
-                ask(0);
-                seen2 = __ballot(r != kNoRow);
-            }
-        } else {
-            if (second) seen2 = pass_on(0, false, seen0, 0);
-        }
+        if (second) seen2 = pass_on(0, false, seen0);
         __syncthreads();
         if (second) __syncthreads();
         auto iteration = [&](int32_t t, auto buffer) __attribute__((always_inline)) {
@@ -507,17 +477,10 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
             products(buf * BUF, (3 - buf) * BUF);
             __syncthreads();
             softmax(t, seen0);
-            const uint64_t after = pass_on(second ? t + 1 : t, second != (buf == 1), second ? seen1 : seen0,
-                                           AHEAD == 2 ? 1 - buf : 0);
+            const uint64_t after = pass_on(second ? t + 1 : t, second != (buf == 1), second ? seen1 : seen0);
             seen0 = seen1;
-            if constexpr (AHEAD == 2) {
-                seen1 = seen2;
-                seen2 = second ? seen3 : after;
-                seen3 = after;
-            } else {
-                seen1 = second ? seen2 : after;
-                seen2 = after;
-            }
+            seen1 = second ? seen2 : after;
+            seen2 = after;
             __syncthreads();
         };
         for (int32_t t = 0;; t += 2) {
@@ -593,6 +556,8 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
 
 constexpr int kFewWaves = 4;
 constexpr int kFewKeys = 32;    // to a wave at a time
+// Of 8-bit pages 64: as many bytes on their way.
+constexpr int few_keys(int head_dim, int kind) { return kFewKeys; }
 
 // Bound by reading the cache: 16 KB in flight to a wave (head_dim 128), each loaded as soon as its registers are free.
 // One token over 128K (64 heads, 8 KV heads, 64): 55 us with its join, 4.8 TB/s, where inputs change from call to call
@@ -606,7 +571,9 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
 {
     constexpr bool E8 = KIND == kEight;
     constexpr int XW = E8 ? (DP + 127) / 128 : 1;    // words of exponents to a row of 8-bit pages
-    constexpr int NW = kFewWaves, TK = kFewKeys;
+    constexpr int NW = kFewWaves, TK = few_keys(DP, KIND);
+    constexpr int KB = TK / 16;                      // products of 16 keys
+    typedef std::conditional_t<TK == 64, uint64_t, uint32_t> Keys;   // a bit to each of a step's
     constexpr int EL = E8 ? 16 : 8;                  // elements of a load
     constexpr int CH = DP / EL;
     constexpr int PASS = 64 / CH;                    // rows that a wave loads at once
@@ -615,7 +582,7 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
     // each wave's values, and at the end its part of the output: [wave][16 rows][DP] in 32 bits
     __shared__ __align__(16) uint16_t lds_v[NW][TK * DP];
     __shared__ float lds_ml[NW][2][16];
-    static_assert(sizeof(lds_v) == NW * 16 * DP * sizeof(float), "the parts reuse the values' space");
+    static_assert(sizeof(lds_v) >= NW * 16 * DP * sizeof(float), "the parts reuse the values' space");
 
     const CacheView &c = a.c;
     const uint32_t kv_head = blockIdx.x % c.kv_heads;
@@ -626,7 +593,7 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
     const int32_t *table = c.table + (uint64_t)seq * c.table_stride;
     int32_t slot0 = -1, slot1 = -1;                  // table entries of this lane's first two keys
     if (!a.window && c.max_kv) {
-        const int64_t key = (int64_t)split * a.split_keys + wave * TK + (lane & 31);
+        const int64_t key = (int64_t)split * a.split_keys + wave * TK + (lane & (TK - 1));
         slot0 = load4g(table + block_of(c, (uint32_t)min(key, (int64_t)c.max_kv - 1)));
         slot1 = load4g(table + block_of(c, (uint32_t)min(key + NW * TK, (int64_t)c.max_kv - 1)));
     }
@@ -674,26 +641,30 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
     const int32_t steps = keys.end > mine ? (keys.end - mine + NW * TK - 1) / (NW * TK) : 0;
 
     bool bounded = true;                             // the values of tiles that not all rows see are finite
-    w4 rk[2][KS * 8 / EL], rv[N];
-    uint32_t exponents[XW];                          // lane i: of key i, and lane i + 32 of value i
-    uint32_t seen_next = 0;
+    w4 rk[KB][KS * 8 / EL], rv[N];
+    uint32_t xk[XW], xv[XW];                         // exponents of this lane's key and value; of 32 keys, xk has both: lane
+                                                     // i key i, lane i + 32 value i
+    Keys seen_next = 0;
     auto slot_at = [&](int32_t t) {
-        const int32_t key = mine + t * (NW * TK) + (lane & 31);
+        const int32_t key = mine + t * (NW * TK) + (lane & (TK - 1));
         return load4g(table + block_of(c, min(key, keys.end - 1)));
     };
     auto load_tile = [&](int32_t t, int32_t slot) {
-        const int32_t key = mine + t * (NW * TK) + (lane & 31);
+        const int32_t key = mine + t * (NW * TK) + (lane & (TK - 1));
         const uint32_t r = row_of(c, key < keys.end ? slot : -1, kv_head, key);
-        const uint32_t ok = (uint32_t)__ballot(r != kNoRow);
+        const Keys ok = (Keys)__ballot(r != kNoRow);
         if constexpr (E8) {
             const uint64_t base = r == kNoRow ? 0 : (uint64_t)(uint32_t)slot * a.slot_bytes;
             const uint64_t row = r == kNoRow ? 0 : r - (uint32_t)slot * (c.kv_heads * c.block);
             const uint64_t at_row = base + row * c.head_dim;
-            const uint8_t *x = (const uint8_t *)(lane < 32 ? a.k : a.v) + base + a.exponents + row * a.row_exponents;
+            const uint64_t x = base + a.exponents + row * a.row_exponents;
 #pragma unroll
-            for (int w = 0; w < XW; ++w) exponents[w] = (uint32_t)load4g((const int32_t *)x + w);
+            for (int w = 0; w < XW; ++w) {
+                xk[w] = (uint32_t)load4g((const int32_t *)((const uint8_t *)(TK == 64 || lane < 32 ? a.k : a.v) + x) + w);
+                if (TK == 64) xv[w] = (uint32_t)load4g((const int32_t *)((const uint8_t *)a.v + x) + w);
+            }
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
+            for (int b = 0; b < KB; ++b) {
                 const uint8_t *p = (const uint8_t *)a.k + lane_value(at_row, b * 16 + col);
 #pragma unroll
                 for (int i = 0; i < KS / 2; ++i) {
@@ -707,7 +678,7 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
             return ok;
         }
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < KB; ++b) {
             uint32_t from = __shfl(r, b * 16 + col);
             from = from == kNoRow ? 0 : from;
             const uint16_t *p = a.k + (uint64_t)from * c.head_dim;
@@ -739,17 +710,18 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
     uint16_t *vs = lds_v[wave];
 
     for (int32_t t = 0; t < steps; ++t) {
-        const uint32_t seen = seen_next;
+        const Keys seen = seen_next;
         const int32_t k0 = mine + t * (NW * TK);
         const bool edge = !(k0 + TK - 1 <= all_first && (int64_t)k0 >= all_full);   // not all rows see these keys
-        v4f z[2];
+        const bool partial = edge || seen != (Keys)~(Keys)0 || c.head_dim != DP;   // there may be values to leave out
+        v4f z[KB];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < KB; ++b) {
             z[b] = v4f{};
             uint32_t word[XW];
             if constexpr (E8) {
 #pragma unroll
-                for (int w = 0; w < XW; ++w) word[w] = lane_value(exponents[w], b * 16 + col);
+                for (int w = 0; w < XW; ++w) word[w] = lane_value(xk[w], b * 16 + col);
             }
 #pragma unroll
             for (int i = 0; i < KS; ++i) {
@@ -761,7 +733,9 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
                 } else {
                     k = rk[b][i];
                 }
-                if (c.head_dim != DP && element_of(i) >= c.head_dim) k = w4{0, 0, 0, 0};
+                if (E8 ? __builtin_expect(c.head_dim != DP, 0) && element_of(i) >= c.head_dim
+                       : c.head_dim != DP && element_of(i) >= c.head_dim)
+                    k = w4{0, 0, 0, 0};
                 z[b] = T::mma16(k, q[i], z[b]);
             }
         }
@@ -769,21 +743,23 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int r = load_row + i * PASS;
-                uint32_t word = lane_value(exponents[0], 32 + r);
+                uint32_t word = TK == 64 ? lane_value(xv[0], r) : lane_value(xk[0], 32 + r);
                 if constexpr (XW > 1) {
-                    const uint32_t other = lane_value(exponents[XW - 1], 32 + r);
+                    const uint32_t other = TK == 64 ? lane_value(xv[XW - 1], r) : lane_value(xk[XW - 1], 32 + r);
                     word = load_piece >= 8 ? other : word;
                 }
                 const float power = power_of(word, load_piece / 2 % 4 * 8);
+                w4 v[2] = {widen<T>(w2{rv[i][0], rv[i][1]}, power), widen<T>(w2{rv[i][2], rv[i][3]}, power)};
+                if (__builtin_expect(partial, 0)) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const bool there = 16u * load_piece + 8 * j < c.head_dim && (seen >> r & 1);
-                    const int vp = (2 * load_piece + j) ^ (DP >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2);
-                    w4 v = widen<T>(w2{rv[i][2 * j], rv[i][2 * j + 1]}, power);
-                    v = there ? v : w4{0, 0, 0, 0};
-                    if (__builtin_expect(edge, 0)) bounded &= T::bound(v);
-                    *(w4 *)&vs[r * DP + vp * 8] = v;
+                    for (int j = 0; j < 2; ++j) {
+                        if (16u * load_piece + 8 * j >= c.head_dim || !(seen >> r & 1)) v[j] = w4{0, 0, 0, 0};
+                        if (edge) bounded &= T::bound(v[j]);
+                    }
                 }
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    *(w4 *)&vs[r * DP + ((2 * load_piece + j) ^ (DP >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2)) * 8] = v[j];
             }
         }
 #pragma unroll
@@ -799,11 +775,11 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
             seen_next = load_tile(t + 1, slot_next);
             slot_next = slot_at(t + 2);
         }
-        if (edge || seen != ~0u) {
-            const uint32_t here = seen >> (4 * quad);
-            const uint32_t drafted = tree ? ((uint32_t)tree_bits(a, s, token, k0 - shift) & seen) >> (4 * quad) : 0;
+        if (edge || seen != (Keys)~(Keys)0) {
+            const Keys here = seen >> (4 * quad);
+            const Keys drafted = tree ? ((Keys)tree_bits(a, s, token, k0 - shift) & seen) >> (4 * quad) : 0;
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < KB; ++b)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int32_t key = k0 + b * 16 + 4 * quad + r;
@@ -816,7 +792,9 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
 #pragma unroll
         for (int r = 1; r < 4; ++r) top = fmaxf(top, z[0][r]);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) top = fmaxf(top, z[1][r]);
+        for (int b = 1; b < KB; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) top = fmaxf(top, z[b][r]);
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, other_half(top)) * a.scale_log2;
         if (__any(top > m + (8.0f + T::kLift))) {    // as in attention_rows
@@ -830,36 +808,41 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
                 for (int r = 0; r < 4; ++r) o[i][r] *= f;
         }
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < KB; ++b)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 z[b][r] = exp2_fast(__builtin_fmaf(z[b][r], a.scale_log2, -m));
                 l += z[b][r];
             }
-        const w4 p = {T::pack(z[0][0], z[0][1]), T::pack(z[0][2], z[0][3]), T::pack(z[1][0], z[1][1]),
-                      T::pack(z[1][2], z[1][3])};
+        w4 p[KB / 2];
+#pragma unroll
+        for (int b = 0; b < KB; b += 2)
+            p[b / 2] = w4{T::pack(z[b][0], z[b][1]), T::pack(z[b][2], z[b][3]), T::pack(z[b + 1][0], z[b + 1][1]),
+                          T::pack(z[b + 1][2], z[b + 1][3])};
         // the wave's own values: LDS keeps a wave's accesses in order
         wave_lds_order();
         const int r = 4 * quad + col / 4;
 #pragma unroll
-        for (int db = 0; db < DP / 16; ++db) {
-            const int piece = db * 2 + (col % 4) / 2;
-            const int at = (piece ^ (DP >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2)) * 8 + (col & 1) * 4;
-            const w2 x = read_down(&vs[r * DP + at]), y = read_down(&vs[(r + 16) * DP + at]);
-            o[db] = T::mma16(w4{x[0], x[1], y[0], y[1]}, p, o[db]);
-        }
+        for (int b = 0; b < KB / 2; ++b)
+#pragma unroll
+            for (int db = 0; db < DP / 16; ++db) {
+                const int piece = db * 2 + (col % 4) / 2;
+                const int at = (piece ^ (DP >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2)) * 8 + (col & 1) * 4;
+                const w2 x = read_down(&vs[(32 * b + r) * DP + at]), y = read_down(&vs[(32 * b + r + 16) * DP + at]);
+                o[db] = T::mma16(w4{x[0], x[1], y[0], y[1]}, p[b], o[db]);
+            }
         wave_lds_order();
     }
 
     if (__builtin_expect(__any(!bounded), 0)) {
         for (int32_t t = 0; t < steps; ++t) {
-            const int32_t k0 = mine + t * (NW * TK), key = k0 + (lane & 31);
+            const int32_t k0 = mine + t * (NW * TK), key = k0 + (lane & (TK - 1));
             if (k0 + TK - 1 <= all_first && (int64_t)k0 >= all_full) continue;
             const uint32_t r = row_of(c, key < keys.end ? slot_at(t) : -1, kv_head, key);
             const bool found = r != kNoRow && unbounded_row<T, KIND>(a, r);
-            const uint32_t drafted = tree ? (uint32_t)tree_bits(a, s, token, k0 - shift) : 0;
-            for (uint32_t left = (uint32_t)__ballot(found); left; left &= left - 1) {
-                const int j = __ffs(left) - 1;
+            const uint64_t drafted = tree ? tree_bits(a, s, token, k0 - shift) : 0;
+            for (uint64_t left = (Keys)__ballot(found); left; left &= left - 1) {
+                const int j = __ffsll((unsigned long long)left) - 1;
                 const uint32_t at = (uint32_t)__builtin_amdgcn_readlane(r, j);
                 const float weight = weight_of<T, KIND>(a, q, at, m, element_of, [](float x) {
                     x += __shfl_xor(x, 16);

@@ -58,6 +58,28 @@ __device__ __forceinline__ int32_t exponent_for(float largest)
     return min(max(e, E4M3<T>::kLeast), E4M3<T>::kMost);
 }
 
+__device__ __forceinline__ w2 to_e4m3(const float (&y)[8])
+{
+    w2 out;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        int v = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * w], y[4 * w + 1], 0, false);
+        v = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * w + 2], y[4 * w + 3], v, true);
+        out[w] = (uint32_t)v;
+    }
+    return out;
+}
+
+// Eight finite floats of magnitudes up to 448 * 2^e.
+__device__ __forceinline__ w2 narrow_plain(const float (&x)[8], int32_t e)
+{
+    const float power = __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = x[i] * power;
+    return to_e4m3(y);
+}
+
 // Eight floats as e4m3 elements of exponent e, rounded to nearest even; those that are not finite become NaN.
 template <class T>
 __device__ __forceinline__ w2 narrow(const float (&x)[8], int32_t e)
@@ -70,28 +92,7 @@ __device__ __forceinline__ w2 narrow(const float (&x)[8], int32_t e)
         const float s = __builtin_amdgcn_fmed3f(x[i] * power, -limit, limit);
         y[i] = __builtin_isfinite(x[i]) ? s : __builtin_nanf("");
     }
-    w2 out;
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-        int v = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * w], y[4 * w + 1], 0, false);
-        v = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * w + 2], y[4 * w + 3], v, true);
-        out[w] = (uint32_t)v;
-    }
-    return out;
-}
-
-// The exponents' word of the 16 lanes (128 elements) that this lane belongs to, where a row has 2^lanes_log2 lanes of 8
-// elements and every four lanes agree on e; 0 in the place of lanes past the row.
-__device__ __forceinline__ uint32_t exponent_word(uint32_t byte, int lane, uint32_t lanes_log2)
-{
-    const int row = 1 << (lanes_log2 < 4 ? lanes_log2 : 4), base = lane & ~(row - 1);
-    uint32_t word = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t b = __shfl(byte, base + 4 * i & 63);
-        word |= (4 * i < row ? b : 0) << (8 * i);
-    }
-    return word;
+    return to_e4m3(y);
 }
 
 }  // namespace kvp

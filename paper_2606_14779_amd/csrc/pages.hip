@@ -9,6 +9,9 @@
 // A head is the work of 2^lanes_log2 neighbouring lanes with 8 elements each, so that sums of squares and largest
 // elements are exchanges within a wave.
 
+#include <algorithm>
+#include <type_traits>
+
 #include "e4m3.hpp"
 
 namespace kvp {
@@ -23,16 +26,46 @@ __device__ __forceinline__ float largest_of(const float (&x)[8])
     return top;
 }
 
-// Over the lanes of a row, or the four lanes of 32 elements.
+// Another lane's value within the vector unit: the neighbour's, that of the other pair of four, of the mirrored four of
+// eight, of the mirrored eight of sixteen.
+constexpr int kNeighbour = 0xB1, kOtherPair = 0x4E, kHalfMirror = 0x141, kMirror = 0x140;
+template <int WHICH>
+__device__ __forceinline__ float lane_of(float x)
+{
+    const int v = __builtin_bit_cast(int, x);
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(v, v, WHICH, 0xF, 0xF, true));
+}
+
+// Over the lanes of a row, or the four lanes of 32 elements.  Once four lanes agree, a mirror is as good as an exchange.
+template <class F>
+__device__ __forceinline__ float over(float x, uint32_t lanes, F f)
+{
+    if (lanes > 1) x = f(x, lane_of<kNeighbour>(x));
+    if (lanes > 2) x = f(x, lane_of<kOtherPair>(x));
+    if (lanes > 4) x = f(x, lane_of<kHalfMirror>(x));
+    if (lanes > 8) x = f(x, lane_of<kMirror>(x));
+    if (lanes > 16) x = f(x, __shfl_xor(x, 16));
+    return x;
+}
 __device__ __forceinline__ float sum_over(float x, uint32_t lanes)
 {
-    for (uint32_t d = 1; d < lanes; d *= 2) x += __shfl_xor(x, d);
-    return x;
+    return over(x, lanes, [](float a, float b) { return a + b; });
 }
 __device__ __forceinline__ float largest_over(float x, uint32_t lanes)
 {
-    for (uint32_t d = 1; d < lanes; d *= 2) x = fmaxf(x, __shfl_xor(x, d));
-    return x;
+    return over(x, lanes, [](float a, float b) { return fmaxf(a, b); });
+}
+
+// The word of a row's first four exponents (or of each 16 lanes' four) in its first lane, where every fourth lane has one.
+__device__ __forceinline__ uint32_t gather_bytes(uint32_t byte, uint32_t lanes_log2)
+{
+    uint32_t word = byte;
+    if (lanes_log2 > 2) word |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)byte, 0x104, 0xF, 0xF, true) << 8;   // 4 lanes on
+    if (lanes_log2 > 3) {
+        word |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)byte, 0x108, 0xF, 0xF, true) << 16;
+        word |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)byte, 0x10C, 0xF, 0xF, true) << 24;
+    }
+    return word;
 }
 
 template <class T>
@@ -53,18 +86,29 @@ __device__ __forceinline__ uint32_t row_in_slot(const CacheView &c, uint32_t kv_
     return kv_head * c.block + token - block_of(c, token) * c.block;
 }
 
-// 8 elements of a row of 8-bit pages, from all lanes of a row together (the exponents' word comes from all of them);
-// to: the slot, null: not written.
+// 8 elements of a row of 8-bit pages, from all lanes of a row together; those with `asked` write, to the slot `to`.
 template <class T>
-__device__ __forceinline__ void put8(const PageView &p, uint32_t head_dim, uint8_t *to, uint32_t row, uint32_t piece,
+__device__ __forceinline__ void put8(const PageView &p, uint32_t head_dim, uint8_t *to, bool asked, uint32_t row, uint32_t piece,
                                      uint32_t lanes_log2, const float (&x)[8])
 {
-    const uint32_t lanes = 1u << lanes_log2;
+    // the largest |x| as an integer, which has the order of the floats: from 0x7F800000 on there is one that is not finite
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, __builtin_bit_cast(uint32_t, x[i]) & 0x7FFFFFFFu);
     const bool live = piece * 8 < head_dim;
-    const int32_t e = exponent_for<T>(largest_over(live ? largest_of(x) : 0.0f, min(lanes, 4u)));
-    const uint32_t word = exponent_word(live ? e + 127 : 0, threadIdx.x & 63, lanes_log2);
-    if (!to || !live) return;
-    *(w2 *)(to + (uint64_t)row * head_dim + piece * 8) = narrow<T>(x, e);
+    if (!live) top = 0;
+    const uint32_t group = min(1u << lanes_log2, 4u);
+    float largest = __builtin_bit_cast(float, top);
+    bool plain = top < 0x7F800000u;
+    if (!plain) largest = largest_of(x);             // of the finite ones
+    largest = largest_over(largest, group);
+    const int32_t e = exponent_for<T>(largest);
+    plain &= e < E4M3<T>::kMost;
+    uint32_t word = live ? (uint32_t)(e + 127) : 0;
+    word = gather_bytes(word, lanes_log2);
+    const w2 out = __builtin_expect(__all(plain), 1) ? narrow_plain(x, e) : narrow<T>(x, e);
+    if (!asked) return;
+    *(w2 *)(to + (uint64_t)row * head_dim + piece * 8) = out;
     if (piece % 16 == 0) *(uint32_t *)(to + p.exponents + (uint64_t)row * p.row_exponents + piece / 16 * 4) = word;
 }
 
@@ -88,7 +132,7 @@ __device__ __forceinline__ float norm_factor(const AppendArgs &a, const float (&
             float s = 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) s = __builtin_fmaf(x[i] * up, x[i] * up, s);
-            for (uint32_t d = 1; d < lanes; d *= 2) s += __shfl_xor(s, d);
+            s = sum_over(s, lanes);
             const float mean = s * a.per_dim + __builtin_ldexpf(a.eps, 2 * k);
             factor = __builtin_ldexpf(__builtin_amdgcn_rsqf(mean), k);
         }
@@ -96,119 +140,188 @@ __device__ __forceinline__ float norm_factor(const AppendArgs &a, const float (&
     return factor;
 }
 
+// A token to a workgroup.  A wave takes whole heads of one kind (queries, keys or values) at a time, so that its lanes go
+// one way, and a lane the same eight elements of every head: what an element and its partner are multiplied by, weight and
+// angle in one, is worked out once for all heads.
 template <class T, bool E8, int PAIRS>
 __global__ __launch_bounds__(256) void append(const AppendArgs a)
 {
+    enum Kind { kQueries, kKeys, kValues };
     __shared__ v2f angles[kMostRotary / 2];          // of this token
     const CacheView &c = a.c;
     const uint32_t token = blockIdx.x, lane = threadIdx.x & 63;
-    const uint32_t lanes = 1u << a.lanes_log2;
-    const uint32_t q_heads = a.q ? c.heads : 0, keys_end = q_heads + c.kv_heads;
-    const uint32_t units = (keys_end + c.kv_heads) << a.lanes_log2;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const uint32_t lanes = 1u << a.lanes_log2, per_wave = 64 >> a.lanes_log2;
+    const uint32_t piece = lane & (lanes - 1), at = piece * 8, mine = lane >> a.lanes_log2;
+    const bool live = at < c.head_dim;
+    const uint32_t jobs_log2 = 6 - a.lanes_log2;
+    const uint32_t q_jobs = a.q ? (c.heads + per_wave - 1) >> jobs_log2 : 0, k_jobs = (c.kv_heads + per_wave - 1) >> jobs_log2;
+    const uint16_t *q = a.q + token * a.q_stride, *k = a.k + token * a.k_stride, *v = a.v + token * a.v_stride;
 
-    // a position that the table does not have: NaN, so that it shows
-    bool known = true;
-    for (uint32_t i = 0; i < a.axes; ++i) {
-        const int32_t p = load4g(a.positions + (uint64_t)i * c.total_q + token);
-        known &= p >= 0 && (uint32_t)p < a.n_positions;
-    }
-    for (uint32_t j = threadIdx.x; j < a.rot / 2; j += blockDim.x) {
-        const int32_t p = known ? load4g(a.positions + (uint64_t)a.axis_of[j] * c.total_q + token) : 0;
-        angles[j] = *(const v2f *)(a.angles + (uint64_t)(uint32_t)p * a.rot + 2 * j);
-    }
-    // the token's sequence: the last one that begins at or before it, 64 at a time
+    auto load = [&](auto kind, uint32_t job) __attribute__((always_inline)) {
+        constexpr int what = decltype(kind)::value;
+        const uint32_t head = job * per_wave + mine;
+        const uint16_t *from = what == kQueries ? q : what == kKeys ? k : v;
+        return live && head < (what == kQueries ? c.heads : c.kv_heads) ? load16g(from + (uint64_t)(head * c.head_dim + at))
+                                                                        : w4{0, 0, 0, 0};
+    };
+    // jobs go round the waves, queries, then keys, then values; the first of each kind are asked for before all else
+    typedef std::integral_constant<int, kQueries> Queries;
+    typedef std::integral_constant<int, kKeys> Keys;
+    typedef std::integral_constant<int, kValues> Values;
+    const uint32_t first_k = (wave - q_jobs) & (waves - 1), first_v = (first_k - k_jobs) & (waves - 1);   // 1, 2 or 4 waves
+    w4 ahead_q{}, ahead_k{}, ahead_v{};
+    if (wave < q_jobs) ahead_q = load(Queries(), wave);
+    if (first_k < k_jobs) ahead_k = load(Keys(), first_k);
+    if (first_v < k_jobs) ahead_v = load(Values(), first_v);
+    // and what they are multiplied by, with their partners' in the other half of the pairs
+    const uint32_t half = a.rot / 2;
+    const bool turns = at < a.rot, upper = at >= half;
+    const uint32_t partner = upper ? at - half : at + half;
+    w4 weight[2]{}, weight_of_partner[2]{};
+    auto load_weights = [&](int kind, const uint16_t *from) __attribute__((always_inline)) {
+        if (!from || !live) return;
+        weight[kind] = load16g(from + at);
+        if (PAIRS == kApart && turns) weight_of_partner[kind] = load16g(from + partner);
+    };
+    if (wave < q_jobs) load_weights(0, a.q_weight);
+    if (first_k < k_jobs) load_weights(1, a.k_weight);
+
+    // Then what has to be known of the token: few loads one after the other, as they are most of a token's time.
+    int32_t position[kMostAxes];
+#pragma unroll
+    for (uint32_t i = 0; i < kMostAxes; ++i) position[i] = load4g(a.positions + (uint64_t)min(i, a.axes - 1) * c.total_q + token);
+    const uint32_t my_axis = a.axes > 1 && threadIdx.x < half ? a.axis_of[threadIdx.x] : 0;
+    // its sequence: the last one that begins at or before it, 64 at a time
+    Seq s;
     uint32_t seq = 0;
-    for (uint32_t n = c.n_seq; n > 1;) {
-        const uint32_t step = (n + 63) / 64, at = seq + lane * step;
-        const uint32_t count = __popcll(__ballot(lane * step < n && load4g(c.cu_q + min(at, c.n_seq)) <= (int32_t)token));
-        const uint32_t last = count ? count - 1 : 0;
-        seq += last * step;
-        n = min(step, n - last * step);
+    if (c.n_seq <= 64) {
+        const Seq its = load_seq(c, min(lane, c.n_seq - 1));
+        const uint64_t begun = __ballot(lane < c.n_seq && its.q_begin <= (int32_t)token);
+        seq = begun ? 63 - __builtin_clzll(begun) : 0;
+        s = {__builtin_amdgcn_readlane(its.q_begin, seq), __builtin_amdgcn_readlane(its.n_q, seq),
+             __builtin_amdgcn_readlane(its.kv, seq)};
+    } else {
+        for (uint32_t n = c.n_seq; n > 1;) {
+            const uint32_t step = (n + 63) / 64, first = seq + lane * step;
+            const uint32_t count = __popcll(__ballot(lane * step < n && load4g(c.cu_q + min(first, c.n_seq)) <= (int32_t)token));
+            const uint32_t last = count ? count - 1 : 0;
+            seq += last * step;
+            n = min(step, n - last * step);
+        }
+        s = load_seq(c, seq);
     }
-    const Seq s = load_seq(c, seq);
     const int32_t i = (int32_t)token - s.q_begin, index = s.kv - s.n_q + i;
     const bool placed = i >= 0 && i < s.n_q && index >= 0;
     const int32_t slot = placed ? load4g(c.table + (uint64_t)seq * c.table_stride + block_of(c, index)) : -1;
+    // a position that the table does not have: NaN, so that it shows
+    bool known = true;
+#pragma unroll
+    for (uint32_t i = 0; i < kMostAxes; ++i) known &= position[i] >= 0 && (uint32_t)position[i] < a.n_positions;
+    for (uint32_t j = threadIdx.x; j < half; j += blockDim.x) {
+        const uint32_t axis = j == threadIdx.x ? my_axis : a.axis_of[j];
+        const int32_t p = axis < 2 ? axis ? position[1] : position[0] : axis == 2 ? position[2] : position[3];
+        angles[j] = *(const v2f *)(a.angles + (uint64_t)(uint32_t)(known ? p : 0) * a.rot + 2 * j);
+    }
     const bool there = (uint32_t)slot < c.num_slots;
+    const uint64_t slot_at = there ? (uint64_t)(uint32_t)slot * a.pages.slot_bytes : 0;
     __syncthreads();
 
-    for (uint32_t first = threadIdx.x & ~63u; first < units; first += blockDim.x) {
-        const uint32_t unit = first + lane, piece = unit & (lanes - 1), at = piece * 8;
-        const uint32_t all = unit >> a.lanes_log2;   // head among queries, keys and values
-        const bool query = all < q_heads, value = all >= keys_end;
-        const uint32_t head = query ? all : value ? all - keys_end : all - q_heads;
-        const bool live = unit < units && at < c.head_dim;
-        const uint16_t *from = (query ? a.q + token * a.q_stride : value ? a.v + token * a.v_stride : a.k + token * a.k_stride) +
-                               (uint64_t)head * c.head_dim;
-        const w4 raw = live ? load16g(from + at) : w4{0, 0, 0, 0};
-        float x[8];
-        unpack8<T>(raw, x);
-        const uint16_t *weight = query ? a.q_weight : a.k_weight;
-        float factor = 1.0f;
-        if (a.norm) {
-            factor = norm_factor<T>(a, x, lanes);
-            if (!value) {
-                float w[8];
-                unpack8<T>(weight && live ? load16g(weight + at) : w4{0, 0, 0, 0}, w);
+    // factors of the lane's elements and of their partners
+    float p[8], r[8];
+    auto factors = [&](int kind, bool weighted) __attribute__((always_inline)) {
+        float w[8], o[8];
+        unpack8<T>(weight[kind], w);
+        unpack8<T>(weight_of_partner[kind], o);
+        if (!weighted) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = x[e] * factor * (weight ? w[e] : 1.0f);
-            }
+            for (int e = 0; e < 8; ++e) w[e] = o[e] = 1.0f;
         }
-        if constexpr (PAIRS == kInside) {
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                if (value || at + e >= a.rot) continue;
-                const v2f f = angles[(at + e) / 2];
-                const float p = x[e], q = x[e + 1];
-                x[e] = __builtin_fmaf(p, f[0], -(q * f[1]));
-                x[e + 1] = __builtin_fmaf(q, f[0], p * f[1]);
-            }
-        } else if constexpr (PAIRS == kApart) {
-            const uint32_t half = a.rot / 16;        // lanes
-            const bool upper = piece >= half;
-            const int other = (int)lane + (upper ? -(int)half : (int)half);
+        for (int e = 0; e < 8; ++e) {
+            p[e] = known ? w[e] : __builtin_nanf("");
+            r[e] = 0.0f;
+            if (PAIRS == kAnyhow || !turns) continue;
+            const v2f f = angles[PAIRS == kInside ? (at + e) / 2 : at + e - (upper ? half : 0)];
+            const float other = PAIRS == kInside ? w[e ^ 1] : o[e];
+            const bool second = PAIRS == kInside ? e & 1 : upper;
+            p[e] *= f[0];
+            r[e] = second ? other * f[1] : -(other * f[1]);
+        }
+    };
+    auto process = [&](auto kind, uint32_t job, w4 raw) __attribute__((always_inline)) {
+        constexpr bool query = decltype(kind)::value == kQueries, value = decltype(kind)::value == kValues;
+        const uint32_t head = job * per_wave + mine;
+        const bool asked = live && head < (query ? c.heads : c.kv_heads);
+        float x[8];
+        if (E8 || !value) unpack8<T>(raw, x);
+        if (!value) {
             float y[8];
+            if constexpr (PAIRS == kInside) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = __shfl(x[e], other & 63);
-            if (!value && at < a.rot) {
+                for (int e = 0; e < 8; ++e) y[e] = x[e ^ 1];
+            } else if constexpr (PAIRS == kApart) {
+                const int other = (int)(lane + (upper ? -half / 8 : half / 8)) & 63;
+                w4 far;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const v2f f = angles[at + e - (upper ? a.rot / 2 : 0)];
-                    x[e] = __builtin_fmaf(x[e], f[0], upper ? y[e] * f[1] : -(y[e] * f[1]));
-                }
+                for (int w = 0; w < 4; ++w) far[w] = __shfl(raw[w], other);
+                unpack8<T>(far, y);
             }
-        } else {
-            if (live && !value) {
-                const uint32_t half = a.rot / 2;
+            const float factor = a.norm ? norm_factor<T>(a, x, lanes) : 1.0f;
+            if constexpr (PAIRS == kAnyhow) {
+                const uint16_t *from = (query ? q : k) + (uint64_t)(head * c.head_dim), *weight = query ? a.q_weight : a.k_weight;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    if (at + e >= a.rot) continue;
-                    const bool upper = at + e >= half;
-                    const uint32_t other = upper ? at + e - half : at + e + half;
-                    float y = T::unpack(from[other], 0);
-                    if (a.norm) y = y * factor * (weight ? T::unpack(weight[other], 0) : 1.0f);
-                    const v2f f = angles[upper ? other : at + e];
+                    x[e] *= p[e];
+                    if (!asked || at + e >= a.rot) continue;
+                    const bool upper = a.interleaved ? e & 1 : at + e >= half;
+                    const uint32_t other = a.interleaved ? (at + e) ^ 1 : upper ? at + e - half : at + e + half;
+                    const float y = T::unpack(from[other], 0) * (weight ? T::unpack(weight[other], 0) : 1.0f);
+                    const v2f f = angles[a.interleaved ? (at + e) / 2 : upper ? other : at + e];
                     x[e] = __builtin_fmaf(x[e], f[0], upper ? y * f[1] : -(y * f[1]));
                 }
+            } else if (turns) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = __builtin_fmaf(x[e], p[e], y[e] * r[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] *= p[e];
+            }
+            if (a.norm) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] *= factor;
             }
         }
-        if (!known && !value) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = __builtin_nanf("");
+        if constexpr (query) {
+            if (asked) *(w4 *)(a.q_out + token * a.q_out_stride + (uint64_t)(head * c.head_dim + at)) = pack8<T>(x);
+            return;
         }
-        if (live && query) *(w4 *)(a.q_out + token * a.q_out_stride + (uint64_t)head * c.head_dim + at) = pack8<T>(x);
-        const bool cached = unit < units && !query;
-        if (cached && !value && piece == 0 && a.pos && placed)
-            a.pos[((uint64_t)seq * c.kv_heads + head) * a.pos_stride + index] = load4g(a.positions + token);
-        const uint32_t row = cached && there ? row_in_slot(c, head, index) : 0;
-        uint8_t *to = (value ? a.pages.v : a.pages.k) + (uint64_t)(there ? slot : 0) * a.pages.slot_bytes;
-        if constexpr (E8) {
-            if (__any(cached)) put8<T>(a.pages, c.head_dim, cached && there ? to : nullptr, row, piece, a.lanes_log2, x);
-        } else {
-            if (live && cached && there)
-                *(w4 *)(to + ((uint64_t)row * c.head_dim + at) * 2) = value ? raw : pack8<T>(x);
+        if (!value && asked && piece == 0 && a.pos && placed)
+            a.pos[((uint64_t)seq * c.kv_heads + head) * a.pos_stride + index] = position[0];
+        if (!there) return;
+        const uint32_t row = row_in_slot(c, head, index);
+        uint8_t *to = (value ? a.pages.v : a.pages.k) + slot_at;
+        if constexpr (E8)
+            put8<T>(a.pages, c.head_dim, to, asked, row, piece, a.lanes_log2, x);
+        else if (asked)
+            *(w4 *)(to + ((uint64_t)row * c.head_dim + at) * 2) = value ? raw : pack8<T>(x);
+    };
+    auto all_of = [&](auto kind, uint32_t first, uint32_t jobs, w4 ahead) __attribute__((always_inline)) {
+        for (uint32_t job = first; job < jobs; job += waves) {
+            const w4 raw = ahead;
+            if (job + waves < jobs) ahead = load(kind, job + waves);
+            process(kind, job, raw);
         }
+    };
+    if (wave < q_jobs) {
+        factors(0, a.q_weight);
+        all_of(Queries(), wave, q_jobs, ahead_q);
     }
+    if (first_k < k_jobs) {
+        factors(1, a.k_weight);
+        all_of(Keys(), first_k, k_jobs, ahead_k);
+    }
+    all_of(Values(), first_v, k_jobs, ahead_v);
 }
 
 // A workgroup has kConvertTokens tokens of a sequence and KV head: all of its loads are asked for before the first store.
@@ -272,7 +385,7 @@ __global__ __launch_bounds__(256) void convert(const ConvertArgs a)
                 } else {
                     float x[8];
                     unpack8<T>(wide[v][r], x);
-                    put8<T>(a.to, c.head_dim, there[r] ? p : nullptr, row[r], piece, a.lanes_log2, x);
+                    put8<T>(a.to, c.head_dim, p, there[r] && live, row[r], piece, a.lanes_log2, x);
                 }
             }
     }
@@ -280,61 +393,67 @@ __global__ __launch_bounds__(256) void convert(const ConvertArgs a)
 
 // A workgroup has a sequence and KV head.  As the path ascends, a row moves down or stays, so rows are taken in order:
 // what a pass stores lies where it or an earlier one has read.
-template <bool E8>
-__global__ __launch_bounds__(256) void commit(const CommitArgs a)
+template <bool E8, int ROWS>
+__global__ __launch_bounds__(ROWS > 1 ? 1024 : 256) void commit(const CommitArgs a)
 {
     const CacheView &c = a.c;
     const uint32_t kv_head = blockIdx.x % c.kv_heads, seq = blockIdx.x / c.kv_heads;
     const Seq s = load_seq(c, seq);
     const int32_t count = min(max(load4g(a.accepted + seq), 0), s.n_q), shift = s.kv - s.n_q;
     if (a.len_out && kv_head == 0 && threadIdx.x == 0) a.len_out[seq] = max(shift, 0) + count;
-    const uint32_t lanes = 1u << a.lanes_log2, step = 256 >> a.lanes_log2, piece = threadIdx.x & (lanes - 1);
+    const uint32_t lanes = 1u << a.lanes_log2, step = blockDim.x >> a.lanes_log2, piece = threadIdx.x & (lanes - 1);
     const bool live = piece * 8 < c.head_dim;
     const int32_t *table = c.table + (uint64_t)seq * c.table_stride;
     int32_t *pos = a.pos ? a.pos + ((uint64_t)seq * c.kv_heads + kv_head) * a.pos_stride : nullptr;
-    for (int32_t i0 = 0; i0 < count; i0 += step) {
-        const int32_t i = i0 + (int32_t)(threadIdx.x >> a.lanes_log2);
-        const int32_t j = i < count ? min(max(load4g(a.path + s.q_begin + i), 0), s.n_q - 1) : i;
-        const int32_t to = shift + i, from = shift + j;
-        bool moves = i < count && j != i && to >= 0 && from >= 0;
-        const int32_t slot_from = moves ? load4g(table + block_of(c, from)) : -1;
-        const int32_t slot_to = moves ? load4g(table + block_of(c, to)) : -1;
-        const bool listed = moves;
-        moves = (uint32_t)slot_from < c.num_slots && (uint32_t)slot_to < c.num_slots;
-        w4 wide[2];
-        w2 thin[2];
-        uint32_t word[2];
-        int32_t position = 0;
-        uint8_t *cache[2] = {a.pages.k, a.pages.v};
-        const uint64_t at = moves ? (uint64_t)(uint32_t)slot_from * a.pages.slot_bytes : 0;
-        const uint32_t row = moves ? row_in_slot(c, kv_head, from) : 0;
+    uint8_t *cache[2] = {a.pages.k, a.pages.v};
+    for (int32_t i0 = 0; i0 < count; i0 += ROWS * step) {
+        w4 wide[ROWS][2];
+        w2 thin[ROWS][2];
+        uint32_t word[ROWS][2];
+        int32_t slot_to[ROWS], position[ROWS];
+        bool moves[ROWS], listed[ROWS];
 #pragma unroll
-        for (int v = 0; v < 2; ++v) {
-            const uint8_t *p = cache[v] + at;
-            const uint64_t element = (uint64_t)row * c.head_dim + (live ? piece * 8 : 0);
-            if constexpr (E8) {
-                thin[v] = load8g((const uint16_t *)(p + element));
-                word[v] = (uint32_t)load4g((const int32_t *)(p + a.pages.exponents + (uint64_t)row * a.pages.row_exponents) +
-                                           (live ? piece / 16 : 0));
-            } else {
-                wide[v] = load16g((const uint16_t *)(p + element * 2));
-            }
-        }
-        if (pos && listed && piece == 0) position = pos[from];
-        __syncthreads();
-        if (pos && listed && piece == 0) pos[to] = position;
-        if (moves && live) {
-            const uint32_t row_to = row_in_slot(c, kv_head, to);
+        for (int u = 0; u < ROWS; ++u) {
+            const int32_t i = i0 + u * step + (int32_t)(threadIdx.x >> a.lanes_log2);
+            const int32_t j = i < count ? min(max(load4g(a.path + s.q_begin + i), 0), s.n_q - 1) : i;
+            const int32_t to = shift + i, from = shift + j;
+            listed[u] = i < count && j != i && to >= 0 && from >= 0;
+            const int32_t slot = listed[u] ? load4g(table + block_of(c, from)) : -1;
+            slot_to[u] = listed[u] ? load4g(table + block_of(c, to)) : -1;
+            moves[u] = (uint32_t)slot < c.num_slots && (uint32_t)slot_to[u] < c.num_slots;
+            const uint64_t at = moves[u] ? (uint64_t)(uint32_t)slot * a.pages.slot_bytes : 0;
+            const uint32_t row = moves[u] ? row_in_slot(c, kv_head, from) : 0;
 #pragma unroll
             for (int v = 0; v < 2; ++v) {
-                uint8_t *p = cache[v] + (uint64_t)(uint32_t)slot_to * a.pages.slot_bytes;
-                const uint64_t element = (uint64_t)row_to * c.head_dim + piece * 8;
+                const uint8_t *p = cache[v] + at;
+                const uint64_t element = (uint64_t)row * c.head_dim + (live ? piece * 8 : 0);
                 if constexpr (E8) {
-                    *(w2 *)(p + element) = thin[v];
-                    if (piece % 16 == 0)
-                        *(uint32_t *)(p + a.pages.exponents + (uint64_t)row_to * a.pages.row_exponents + piece / 16 * 4) = word[v];
+                    thin[u][v] = load8g((const uint16_t *)(p + element));
+                    word[u][v] = (uint32_t)load4g((const int32_t *)(p + a.pages.exponents + (uint64_t)row * a.pages.row_exponents) +
+                                                  (live ? piece / 16 : 0));
                 } else {
-                    *(w4 *)(p + element * 2) = wide[v];
+                    wide[u][v] = load16g((const uint16_t *)(p + element * 2));
+                }
+            }
+            position[u] = pos && listed[u] && piece == 0 ? pos[from] : 0;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) {
+            const int32_t to = shift + i0 + u * (int32_t)step + (int32_t)(threadIdx.x >> a.lanes_log2);
+            if (pos && listed[u] && piece == 0) pos[to] = position[u];
+            if (!moves[u] || !live) continue;
+            const uint32_t row = row_in_slot(c, kv_head, to);
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+                uint8_t *p = cache[v] + (uint64_t)(uint32_t)slot_to[u] * a.pages.slot_bytes;
+                const uint64_t element = (uint64_t)row * c.head_dim + piece * 8;
+                if constexpr (E8) {
+                    *(w2 *)(p + element) = thin[u][v];
+                    if (piece % 16 == 0)
+                        *(uint32_t *)(p + a.pages.exponents + (uint64_t)row * a.pages.row_exponents + piece / 16 * 4) = word[u][v];
+                } else {
+                    *(w4 *)(p + element * 2) = wide[u][v];
                 }
             }
         }
@@ -353,12 +472,13 @@ __global__ __launch_bounds__(256) void commit_lengths(const CommitArgs a, int32_
 template <class T, bool E8>
 hipError_t launch_append_as(const AppendArgs &a, hipStream_t stream)
 {
-    // whole wavefronts, as many as a token's units fill, up to four
-    const uint32_t units = ((a.q ? a.c.heads : 0) + 2 * a.c.kv_heads) << a.lanes_log2;
-    const uint32_t threads = units >= 256 ? 256 : (units + 63) / 64 * 64;
-    if (a.interleaved || a.rot == 0)
+    // as many waves as a token's heads fill, up to four
+    const uint32_t per_wave = 64 >> a.lanes_log2;
+    const uint32_t jobs = ((a.q ? a.c.heads : 0) + per_wave - 1) / per_wave + 2 * ((a.c.kv_heads + per_wave - 1) / per_wave);
+    const uint32_t threads = jobs >= 4 ? 256 : jobs >= 2 ? 128 : 64;
+    if (a.rot == 0 || (a.interleaved && a.rot % 8 == 0))
         append<T, E8, kInside><<<a.c.total_q, threads, 0, stream>>>(a);
-    else if (a.rot % 16 == 0)
+    else if (!a.interleaved && a.rot % 16 == 0)
         append<T, E8, kApart><<<a.c.total_q, threads, 0, stream>>>(a);
     else
         append<T, E8, kAnyhow><<<a.c.total_q, threads, 0, stream>>>(a);
@@ -400,10 +520,11 @@ hipError_t launch_convert(const ConvertArgs &a, uint32_t dtype, hipStream_t stre
 hipError_t launch_commit(const CommitArgs &a, hipStream_t stream)
 {
     const uint32_t grid = a.c.n_seq * a.c.kv_heads;
+    const bool more = a.c.max_q > 256u >> a.lanes_log2;   // than a workgroup moves at once
     if (a.pages.exponents)
-        commit<true><<<grid, 256, 0, stream>>>(a);
+        more ? commit<true, 4><<<grid, 1024, 0, stream>>>(a) : commit<true, 1><<<grid, 256, 0, stream>>>(a);
     else
-        commit<false><<<grid, 256, 0, stream>>>(a);
+        more ? commit<false, 4><<<grid, 1024, 0, stream>>>(a) : commit<false, 1><<<grid, 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 
