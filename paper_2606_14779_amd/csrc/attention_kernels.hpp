@@ -15,6 +15,26 @@ namespace {
 // either mask.
 enum PageKind { kCausal16, kTree16, kEight };
 
+// Row of a cached token: of the cache, or with 8-bit pages of its slot; kNoRow where the slot is none of the cache's.
+template <int KIND>
+__device__ __forceinline__ uint32_t row_in(const CacheView &c, int32_t slot, uint32_t kv_head, uint32_t token)
+{
+    if constexpr (KIND != kEight) return row_of(c, slot, kv_head, token);
+    const uint32_t row = kv_head * c.block + token - block_of(c, token) * c.block;
+    return (uint32_t)slot < c.num_slots ? row : kNoRow;
+}
+// Where a row of 8-bit pages begins, and its exponents; row 0 of the cache in the place of one that is not there.
+template <class Offset>
+__device__ __forceinline__ Offset elements_at(const AttentionArgs &a, int32_t slot, uint32_t row)
+{
+    return row == kNoRow ? 0 : (Offset)slot * (Offset)a.slot_bytes + (Offset)row * a.c.head_dim;
+}
+template <class Offset>
+__device__ __forceinline__ Offset exponents_at(const AttentionArgs &a, int32_t slot, uint32_t row)
+{
+    return (row == kNoRow ? 0 : (Offset)slot * (Offset)a.slot_bytes + (Offset)row * a.row_exponents) + a.exponents;
+}
+
 // Eight elements of a cache's row, from element d on; r counts rows of a head over all slots.
 template <class T, int KIND>
 __device__ __forceinline__ w4 eight_at(const AttentionArgs &a, const uint16_t *cache, uint32_t r, uint32_t d)
@@ -258,24 +278,20 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
     };
     auto row_at = [&](int32_t t, int32_t slot) __attribute__((always_inline)) {
         const int32_t key = keys.begin + t * TK + lane;
-        return row_of(c, key < keys.end ? slot : -1, kv_head, key);
+        return row_in<KIND>(c, key < keys.end ? slot : -1, kv_head, key);
     };
     // where a row begins, and the exponents of one in 8-bit pages; not there: a row that is
     auto offset_of = [&](uint32_t r, int32_t slot) __attribute__((always_inline)) {
-        if constexpr (E8) {
-            const uint32_t row = r == kNoRow ? 0 : r - (uint32_t)slot * (c.kv_heads * c.block);
-            return (r == kNoRow ? 0 : (Offset)slot * (Offset)a.slot_bytes) + (Offset)row * c.head_dim;
-        } else {
+        if constexpr (E8)
+            return elements_at<Offset>(a, slot, r);
+        else
             return (Offset)(r == kNoRow ? 0 : r) * (c.head_dim * 2);
-        }
     };
     auto exponents_of = [&](uint32_t r, int32_t slot) __attribute__((always_inline)) {
-        if constexpr (E8) {
-            const uint32_t row = r == kNoRow ? 0 : r - (uint32_t)slot * (c.kv_heads * c.block);
-            return (r == kNoRow ? 0 : (Offset)slot * (Offset)a.slot_bytes) + a.exponents + (Offset)row * a.row_exponents;
-        } else {
+        if constexpr (E8)
+            return exponents_at<Offset>(a, slot, r);
+        else
             return (Offset)0;
-        }
     };
     auto load = [&](const uint16_t *cache, Offset at, auto (&to)[N]) __attribute__((always_inline)) {
 #pragma unroll
@@ -497,7 +513,8 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
             for (int32_t t = 0; t < tiles_n; ++t) {
                 const int32_t k0 = keys.begin + t * TK;
                 if (k0 + TK - 1 <= all_first && k0 >= all_full) continue;
-                const uint32_t r = row_at(t, slot_at(t));
+                const int32_t key = k0 + lane;
+                const uint32_t r = row_of(c, key < keys.end ? slot_at(t) : -1, kv_head, key);
                 const bool found = r != kNoRow && unbounded_row<T, KIND>(a, r);
                 const uint64_t drafted = tree ? tree_bits(a, s, token, k0 - shift) : 0;
                 for (uint64_t left = __ballot(found); left; left &= left - 1) {
@@ -556,8 +573,6 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
 
 constexpr int kFewWaves = 4;
 constexpr int kFewKeys = 32;    // to a wave at a time
-// Of 8-bit pages 64: as many bytes on their way.
-constexpr int few_keys(int head_dim, int kind) { return kFewKeys; }
 
 // Bound by reading the cache: 16 KB in flight to a wave (head_dim 128), each loaded as soon as its registers are free.
 // One token over 128K (64 heads, 8 KV heads, 64): 55 us with its join, 4.8 TB/s, where inputs change from call to call
@@ -571,9 +586,7 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
 {
     constexpr bool E8 = KIND == kEight;
     constexpr int XW = E8 ? (DP + 127) / 128 : 1;    // words of exponents to a row of 8-bit pages
-    constexpr int NW = kFewWaves, TK = few_keys(DP, KIND);
-    constexpr int KB = TK / 16;                      // products of 16 keys
-    typedef std::conditional_t<TK == 64, uint64_t, uint32_t> Keys;   // a bit to each of a step's
+    constexpr int NW = kFewWaves, TK = kFewKeys;
     constexpr int EL = E8 ? 16 : 8;                  // elements of a load
     constexpr int CH = DP / EL;
     constexpr int PASS = 64 / CH;                    // rows that a wave loads at once
@@ -582,7 +595,7 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
     // each wave's values, and at the end its part of the output: [wave][16 rows][DP] in 32 bits
     __shared__ __align__(16) uint16_t lds_v[NW][TK * DP];
     __shared__ float lds_ml[NW][2][16];
-    static_assert(sizeof(lds_v) >= NW * 16 * DP * sizeof(float), "the parts reuse the values' space");
+    static_assert(sizeof(lds_v) == NW * 16 * DP * sizeof(float), "the parts reuse the values' space");
 
     const CacheView &c = a.c;
     const uint32_t kv_head = blockIdx.x % c.kv_heads;
@@ -593,7 +606,7 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
     const int32_t *table = c.table + (uint64_t)seq * c.table_stride;
     int32_t slot0 = -1, slot1 = -1;                  // table entries of this lane's first two keys
     if (!a.window && c.max_kv) {
-        const int64_t key = (int64_t)split * a.split_keys + wave * TK + (lane & (TK - 1));
+        const int64_t key = (int64_t)split * a.split_keys + wave * TK + (lane & 31);
         slot0 = load4g(table + block_of(c, (uint32_t)min(key, (int64_t)c.max_kv - 1)));
         slot1 = load4g(table + block_of(c, (uint32_t)min(key + NW * TK, (int64_t)c.max_kv - 1)));
     }
@@ -641,30 +654,24 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
     const int32_t steps = keys.end > mine ? (keys.end - mine + NW * TK - 1) / (NW * TK) : 0;
 
     bool bounded = true;                             // the values of tiles that not all rows see are finite
-    w4 rk[KB][KS * 8 / EL], rv[N];
-    uint32_t xk[XW], xv[XW];                         // exponents of this lane's key and value; of 32 keys, xk has both: lane
-                                                     // i key i, lane i + 32 value i
-    Keys seen_next = 0;
+    w4 rk[2][KS * 8 / EL], rv[N];
+    uint32_t exponents[XW];                          // lane i: of key i, and lane i + 32 of value i
+    uint32_t seen_next = 0;
     auto slot_at = [&](int32_t t) {
-        const int32_t key = mine + t * (NW * TK) + (lane & (TK - 1));
+        const int32_t key = mine + t * (NW * TK) + (lane & 31);
         return load4g(table + block_of(c, min(key, keys.end - 1)));
     };
     auto load_tile = [&](int32_t t, int32_t slot) {
-        const int32_t key = mine + t * (NW * TK) + (lane & (TK - 1));
-        const uint32_t r = row_of(c, key < keys.end ? slot : -1, kv_head, key);
-        const Keys ok = (Keys)__ballot(r != kNoRow);
+        const int32_t key = mine + t * (NW * TK) + (lane & 31);
+        const uint32_t r = row_in<KIND>(c, key < keys.end ? slot : -1, kv_head, key);
+        const uint32_t ok = (uint32_t)__ballot(r != kNoRow);
         if constexpr (E8) {
-            const uint64_t base = r == kNoRow ? 0 : (uint64_t)(uint32_t)slot * a.slot_bytes;
-            const uint64_t row = r == kNoRow ? 0 : r - (uint32_t)slot * (c.kv_heads * c.block);
-            const uint64_t at_row = base + row * c.head_dim;
-            const uint64_t x = base + a.exponents + row * a.row_exponents;
+            const uint64_t at_row = elements_at<uint64_t>(a, slot, r);
+            const uint8_t *x = (const uint8_t *)(lane < 32 ? a.k : a.v) + exponents_at<uint64_t>(a, slot, r);
 #pragma unroll
-            for (int w = 0; w < XW; ++w) {
-                xk[w] = (uint32_t)load4g((const int32_t *)((const uint8_t *)(TK == 64 || lane < 32 ? a.k : a.v) + x) + w);
-                if (TK == 64) xv[w] = (uint32_t)load4g((const int32_t *)((const uint8_t *)a.v + x) + w);
-            }
+            for (int w = 0; w < XW; ++w) exponents[w] = (uint32_t)load4g((const int32_t *)x + w);
 #pragma unroll
-            for (int b = 0; b < KB; ++b) {
+            for (int b = 0; b < 2; ++b) {
                 const uint8_t *p = (const uint8_t *)a.k + lane_value(at_row, b * 16 + col);
 #pragma unroll
                 for (int i = 0; i < KS / 2; ++i) {
@@ -678,7 +685,7 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
             return ok;
         }
 #pragma unroll
-        for (int b = 0; b < KB; ++b) {
+        for (int b = 0; b < 2; ++b) {
             uint32_t from = __shfl(r, b * 16 + col);
             from = from == kNoRow ? 0 : from;
             const uint16_t *p = a.k + (uint64_t)from * c.head_dim;
@@ -710,18 +717,18 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
     uint16_t *vs = lds_v[wave];
 
     for (int32_t t = 0; t < steps; ++t) {
-        const Keys seen = seen_next;
+        const uint32_t seen = seen_next;
         const int32_t k0 = mine + t * (NW * TK);
         const bool edge = !(k0 + TK - 1 <= all_first && (int64_t)k0 >= all_full);   // not all rows see these keys
-        const bool partial = edge || seen != (Keys)~(Keys)0 || c.head_dim != DP;   // there may be values to leave out
-        v4f z[KB];
+        const bool partial = edge || seen != ~0u || c.head_dim != DP;   // there may be values to leave out
+        v4f z[2];
 #pragma unroll
-        for (int b = 0; b < KB; ++b) {
+        for (int b = 0; b < 2; ++b) {
             z[b] = v4f{};
             uint32_t word[XW];
             if constexpr (E8) {
 #pragma unroll
-                for (int w = 0; w < XW; ++w) word[w] = lane_value(xk[w], b * 16 + col);
+                for (int w = 0; w < XW; ++w) word[w] = lane_value(exponents[w], b * 16 + col);
             }
 #pragma unroll
             for (int i = 0; i < KS; ++i) {
@@ -743,9 +750,9 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int r = load_row + i * PASS;
-                uint32_t word = TK == 64 ? lane_value(xv[0], r) : lane_value(xk[0], 32 + r);
+                uint32_t word = lane_value(exponents[0], 32 + r);
                 if constexpr (XW > 1) {
-                    const uint32_t other = TK == 64 ? lane_value(xv[XW - 1], r) : lane_value(xk[XW - 1], 32 + r);
+                    const uint32_t other = lane_value(exponents[XW - 1], 32 + r);
                     word = load_piece >= 8 ? other : word;
                 }
                 const float power = power_of(word, load_piece / 2 % 4 * 8);
@@ -775,11 +782,11 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
             seen_next = load_tile(t + 1, slot_next);
             slot_next = slot_at(t + 2);
         }
-        if (edge || seen != (Keys)~(Keys)0) {
-            const Keys here = seen >> (4 * quad);
-            const Keys drafted = tree ? ((Keys)tree_bits(a, s, token, k0 - shift) & seen) >> (4 * quad) : 0;
+        if (edge || seen != ~0u) {
+            const uint32_t here = seen >> (4 * quad);
+            const uint32_t drafted = tree ? ((uint32_t)tree_bits(a, s, token, k0 - shift) & seen) >> (4 * quad) : 0;
 #pragma unroll
-            for (int b = 0; b < KB; ++b)
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int32_t key = k0 + b * 16 + 4 * quad + r;
@@ -792,9 +799,7 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
 #pragma unroll
         for (int r = 1; r < 4; ++r) top = fmaxf(top, z[0][r]);
 #pragma unroll
-        for (int b = 1; b < KB; ++b)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) top = fmaxf(top, z[b][r]);
+        for (int r = 0; r < 4; ++r) top = fmaxf(top, z[1][r]);
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, other_half(top)) * a.scale_log2;
         if (__any(top > m + (8.0f + T::kLift))) {    // as in attention_rows
@@ -808,41 +813,36 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
                 for (int r = 0; r < 4; ++r) o[i][r] *= f;
         }
 #pragma unroll
-        for (int b = 0; b < KB; ++b)
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 z[b][r] = exp2_fast(__builtin_fmaf(z[b][r], a.scale_log2, -m));
                 l += z[b][r];
             }
-        w4 p[KB / 2];
-#pragma unroll
-        for (int b = 0; b < KB; b += 2)
-            p[b / 2] = w4{T::pack(z[b][0], z[b][1]), T::pack(z[b][2], z[b][3]), T::pack(z[b + 1][0], z[b + 1][1]),
-                          T::pack(z[b + 1][2], z[b + 1][3])};
+        const w4 p = {T::pack(z[0][0], z[0][1]), T::pack(z[0][2], z[0][3]), T::pack(z[1][0], z[1][1]),
+                      T::pack(z[1][2], z[1][3])};
         // the wave's own values: LDS keeps a wave's accesses in order
         wave_lds_order();
         const int r = 4 * quad + col / 4;
 #pragma unroll
-        for (int b = 0; b < KB / 2; ++b)
-#pragma unroll
-            for (int db = 0; db < DP / 16; ++db) {
-                const int piece = db * 2 + (col % 4) / 2;
-                const int at = (piece ^ (DP >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2)) * 8 + (col & 1) * 4;
-                const w2 x = read_down(&vs[(32 * b + r) * DP + at]), y = read_down(&vs[(32 * b + r + 16) * DP + at]);
-                o[db] = T::mma16(w4{x[0], x[1], y[0], y[1]}, p[b], o[db]);
-            }
+        for (int db = 0; db < DP / 16; ++db) {
+            const int piece = db * 2 + (col % 4) / 2;
+            const int at = (piece ^ (DP >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2)) * 8 + (col & 1) * 4;
+            const w2 x = read_down(&vs[r * DP + at]), y = read_down(&vs[(r + 16) * DP + at]);
+            o[db] = T::mma16(w4{x[0], x[1], y[0], y[1]}, p, o[db]);
+        }
         wave_lds_order();
     }
 
     if (__builtin_expect(__any(!bounded), 0)) {
         for (int32_t t = 0; t < steps; ++t) {
-            const int32_t k0 = mine + t * (NW * TK), key = k0 + (lane & (TK - 1));
+            const int32_t k0 = mine + t * (NW * TK), key = k0 + (lane & 31);
             if (k0 + TK - 1 <= all_first && (int64_t)k0 >= all_full) continue;
             const uint32_t r = row_of(c, key < keys.end ? slot_at(t) : -1, kv_head, key);
             const bool found = r != kNoRow && unbounded_row<T, KIND>(a, r);
-            const uint64_t drafted = tree ? tree_bits(a, s, token, k0 - shift) : 0;
-            for (uint64_t left = (Keys)__ballot(found); left; left &= left - 1) {
-                const int j = __ffsll((unsigned long long)left) - 1;
+            const uint32_t drafted = tree ? (uint32_t)tree_bits(a, s, token, k0 - shift) : 0;
+            for (uint32_t left = (uint32_t)__ballot(found); left; left &= left - 1) {
+                const int j = __ffs(left) - 1;
                 const uint32_t at = (uint32_t)__builtin_amdgcn_readlane(r, j);
                 const float weight = weight_of<T, KIND>(a, q, at, m, element_of, [](float x) {
                     x += __shfl_xor(x, 16);
@@ -1034,14 +1034,12 @@ __global__ __launch_bounds__(kFewWaves * RG * 64, DP > 128 ? 1 : 2) void attenti
     };
     auto load_tile = [&](int32_t t, int32_t slot) __attribute__((always_inline)) {
         const int32_t key = mine + t * (NW * TK) + col;
-        const uint32_t r = row_of(c, key < keys.end ? slot : -1, kv_head, key);
+        const uint32_t r = row_in<KIND>(c, key < keys.end ? slot : -1, kv_head, key);
         seen_next = (uint32_t)__ballot(r != kNoRow);
         uint64_t at_row;                             // bytes
         if constexpr (E8) {
-            const uint64_t base = r == kNoRow ? 0 : (uint64_t)(uint32_t)slot * a.slot_bytes;
-            const uint64_t row = r == kNoRow ? 0 : r - (uint32_t)slot * (c.kv_heads * c.block);
-            at_row = base + row * c.head_dim;
-            const uint8_t *x = (const uint8_t *)(lane < 32 ? a.k : a.v) + base + a.exponents + row * a.row_exponents;
+            at_row = elements_at<uint64_t>(a, slot, r);
+            const uint8_t *x = (const uint8_t *)(lane < 32 ? a.k : a.v) + exponents_at<uint64_t>(a, slot, r);
 #pragma unroll
             for (int w = 0; w < XW; ++w) exponents[w] = (uint32_t)load4g((const int32_t *)x + w);
         } else {
