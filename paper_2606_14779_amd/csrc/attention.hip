@@ -27,7 +27,7 @@ namespace {
 // Adds the parts of the rows.  A row is the work of `slices` times LANES neighbouring threads: a thread has 4
 // elements of head_dim and every slices-th part, U of them in flight; the slices are added through LDS, always in
 // the same order.
-template <class T, int LANES, int U>
+template <class T, int LANES, int U, bool SPARSE>
 __global__ __launch_bounds__(256) void attention_join(const AttentionArgs a, const uint32_t slices)
 {
     constexpr int GROUPS = 256 / LANES;
@@ -49,7 +49,15 @@ __global__ __launch_bounds__(256) void attention_join(const AttentionArgs a, con
         for (int u = 0; u < U; ++u) {
             const uint64_t part = (uint64_t)min(i0 + u * slices, a.splits - 1) * rows + row;
             ml[u] = *(const v2f *)(a.part_ml + 2 * part);
-            o[u] = *(const v4f *)(a.part_o + part * c.head_dim + (live ? at : 0));
+            if (!SPARSE) o[u] = *(const v4f *)(a.part_o + part * c.head_dim + (live ? at : 0));
+        }
+        if (SPARSE) {                                // many parts of short sequences are empty
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint64_t part = (uint64_t)min(i0 + u * slices, a.splits - 1) * rows + row;
+                o[u] = v4f{};
+                if (ml[u][1] != 0.0f) o[u] = *(const v4f *)(a.part_o + part * c.head_dim + (live ? at : 0));
+            }
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -455,10 +463,13 @@ struct Join {
         uint32_t slices = 1;
         while (slices < groups && slices * 4 < a.splits) slices *= 2;
         const uint32_t per = groups / slices, rows = a.c.total_q * a.c.heads;
-        if (a.splits <= 2)
-            attention_join<T, DP / 4, 2><<<(rows + per - 1) / per, 256, 0, stream>>>(a, slices);
+        const uint32_t grid = (rows + per - 1) / per;
+        if (a.uneven)
+            attention_join<T, DP / 4, 4, true><<<grid, 256, 0, stream>>>(a, slices);
+        else if (a.splits <= 2)
+            attention_join<T, DP / 4, 2, false><<<grid, 256, 0, stream>>>(a, slices);
         else
-            attention_join<T, DP / 4, 4><<<(rows + per - 1) / per, 256, 0, stream>>>(a, slices);
+            attention_join<T, DP / 4, 4, false><<<grid, 256, 0, stream>>>(a, slices);
         return hipGetLastError();
     }
 };

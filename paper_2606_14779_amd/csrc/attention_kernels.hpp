@@ -94,18 +94,42 @@ __device__ __forceinline__ RowEnd finish_row(float m, float l, const float *sink
 struct Split {
     int32_t begin, end;   // keys
 };
-// Keys of one workgroup: what its rows can see, cut into the launch's parts.
+// Keys of one workgroup: what its rows can see, cut into the launch's parts of split_keys.
 __device__ __forceinline__ Split keys_of(const AttentionArgs &a, const Seq &s, int32_t first_token, int32_t last_token,
-                                         uint32_t split)
+                                         uint32_t split, uint32_t split_keys)
 {
     const int32_t shift = s.kv - s.n_q;
     int32_t lo = 0;
     if (a.window) lo = (int32_t)max((int64_t)0, (int64_t)(shift + first_token) + 1 - (int64_t)a.window);
     lo &= ~(int32_t)(kTileKeys - 1);
     const int32_t hi = min(shift + last_token + 1, s.kv);
-    const int64_t begin = (int64_t)lo + (int64_t)split * a.split_keys;
-    const int64_t end = split + 1 == a.splits ? (int64_t)hi : min((int64_t)hi, begin + (int64_t)a.split_keys);
+    const int64_t begin = (int64_t)lo + (int64_t)split * split_keys;
+    const int64_t end = split + 1 == a.splits ? (int64_t)hi : min((int64_t)hi, begin + (int64_t)split_keys);
     return {(int32_t)min(begin, (int64_t)max(hi, 0)), (int32_t)max(end, (int64_t)0)};
+}
+
+// Keys of a part where the lengths of a batch decide, which the host does not know: lane i has sequence i's span of keys and
+// its row tiles (0: none), and every workgroup finds the same.  The parts of a call are at most a.splits.
+__device__ __forceinline__ uint32_t lowest_of(uint32_t x)
+{
+    for (int d = 1; d < 64; d *= 2) x = min(x, (uint32_t)__shfl_xor(x, d));
+    return (uint32_t)__builtin_amdgcn_readfirstlane(x);
+}
+__device__ __forceinline__ uint32_t longest_of(uint32_t x) { return ~lowest_of(~x); }
+// Workgroups of row tiles, one to a CU: of 1 to 64 parts to the longest sequence that number for which the rounds of the chip,
+// each as long as a part's tiles of keys and about five more to begin and end, take least.
+__device__ __forceinline__ uint32_t keys_of_rounds(const AttentionArgs &a, uint32_t span, uint32_t tiles)
+{
+    const uint32_t lane = threadIdx.x & 63, longest = longest_of(tiles ? span : 0);
+    const uint32_t n = min(lane + 1, a.splits), keys = max((longest + n - 1) / n + 63 & ~63u, 64u);
+    const float per_key = 1.0f / (float)keys;
+    uint32_t count = 0;
+    for (uint32_t s = 0; s < a.c.n_seq; ++s)
+        count += (uint32_t)__builtin_amdgcn_readlane(tiles, s) *
+                 (uint32_t)ceilf((float)(uint32_t)__builtin_amdgcn_readlane(span, s) * per_key);
+    const uint32_t rounds = (count * a.c.kv_heads + 255) / 256;
+    const uint32_t best = lowest_of(min(rounds * (keys / 64 + 5), (1u << 26) - 1) << 6 | lane) & 63;
+    return (uint32_t)__builtin_amdgcn_readlane(keys, best);
 }
 
 // A row must not meet the infinities and NaN of values that it does not see, but a weight of 0 times them is NaN, and in a
@@ -191,11 +215,12 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
     const uint32_t rest = blockIdx.x / c.kv_heads;
     // the tiles of a part of the keys run side by side, so that its keys come from L2 for all but one of them;
     // under a causal mask later tiles have more keys
-    uint32_t split, seq, row0;
+    uint32_t split, seq, row0, split_keys = a.split_keys;
     Seq s;
     if (c.n_seq > 1 && c.n_seq <= 64) {
         const Tile t = tile_by_length(c, rest, a.splits, TR, TK);
         if (t.tile == kNoTile) return;
+        if (a.uneven) split_keys = keys_of_rounds(a, t.mine.kv, t.tiles);
         split = t.split;
         seq = t.seq;
         s = t.s;
@@ -232,7 +257,12 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
     const int32_t floor_key = a.window ? (int32_t)max(place - (int64_t)a.window, (int64_t)0) : 0;
 
     const Split keys = keys_of(a, s, tree ? -1 : (int32_t)token_of(c, row0),
-                               tree ? s.n_q - 1 : (int32_t)token_of(c, row0 + rows_here - 1), split);
+                               tree ? s.n_q - 1 : (int32_t)token_of(c, row0 + rows_here - 1), split, split_keys);
+    if (a.uneven && keys.begin >= keys.end) {      // of no weight: its output is not looked at
+        const uint64_t part = (uint64_t)split * c.total_q * c.heads + (uint64_t)(s.q_begin + token) * c.heads + head;
+        if (half == 0 && wave_row + col < rows_here) *(v2f *)(a.part_ml + 2 * part) = v2f{kLowest, 0.0f};
+        return;
+    }
     const int32_t tiles_n = keys.end > keys.begin ? (keys.end - keys.begin + TK - 1) / TK : 0;
     // all of the wave's rows see the keys of [wave_full, wave_first]
     const int32_t wave_first = tree ? shift - 1 : shift + (int32_t)token_of(c, row0 + min(wave_row, rows_here - 1));
@@ -624,7 +654,7 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
     const int32_t limit = tree ? shift - 1 : min(shift + token, s.kv - 1);
     const int64_t place = tree && a.window ? (int64_t)shift + tree_depth(a, s, token) : (int64_t)limit + 1;
     const int32_t floor_key = a.window ? (int32_t)max(place - (int64_t)a.window, (int64_t)0) : 0;
-    const Split keys = keys_of(a, s, tree ? -1 : 0, s.n_q - 1, split);
+    const Split keys = keys_of(a, s, tree ? -1 : 0, s.n_q - 1, split, a.split_keys);
     const int32_t all_first = tree ? shift - 1 : shift;   // last key that every row sees
     const int64_t all_full = a.window ? (int64_t)s.kv - (int64_t)a.window : 0;   // first key that every row sees
 
@@ -919,12 +949,9 @@ __device__ __forceinline__ Part part_of(const AttentionArgs &a, uint32_t rest, b
     const uint32_t lane = threadIdx.x & 63;
     Seq s = load_seq(a.c, min(lane, a.c.n_seq - 1));
     if (lane >= a.c.n_seq) s.n_q = 0;
-    uint32_t parts = 0;                              // of this lane's sequence that hold keys
-    if (s.n_q) {
-        const Split first = keys_of(a, s, tree ? -1 : 0, s.n_q - 1, 0);
-        const uint32_t span = (uint32_t)max(s.kv - first.begin, 0);
-        parts = min((span + a.split_keys - 1) / a.split_keys, a.splits);
-    }
+    uint32_t span = 0;
+    if (s.n_q) span = (uint32_t)max(s.kv - keys_of(a, s, tree ? -1 : 0, s.n_q - 1, 0, a.split_keys).begin, 0);
+    const uint32_t parts = min((span + a.split_keys - 1) / a.split_keys, a.splits);   // of this lane's sequence that hold keys
     const uint32_t upto = sum_upto(parts), all = (uint32_t)__builtin_amdgcn_readlane(upto, 63);
     const uint32_t empty = s.n_q ? a.splits - parts : 0, empty_upto = sum_upto(empty);
     const bool held = rest < all;
@@ -978,7 +1005,7 @@ __global__ __launch_bounds__(kFewWaves * RG * 64, DP > 128 ? 1 : 2) void attenti
     const int32_t *table = c.table + (uint64_t)seq * c.table_stride;
     const uint32_t rows = (uint32_t)s.n_q * c.group;   // at most 32 RG
     if (!rows) return;
-    const Split keys = keys_of(a, s, tree ? -1 : 0, s.n_q - 1, split);
+    const Split keys = keys_of(a, s, tree ? -1 : 0, s.n_q - 1, split, a.split_keys);
     if (a.splits > 1 && keys.begin >= keys.end) {      // of no weight: its output is not looked at
         for (uint32_t r = tid; r < rows; r += kFewWaves * RG * 64) {
             const uint32_t t = token_of(c, r), h = kv_head * c.group + r - t * c.group;

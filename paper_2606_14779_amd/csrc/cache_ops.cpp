@@ -103,6 +103,7 @@ struct CutRule {
 struct Cut {
     uint32_t few;     // most rows of a sequence, or 0: tiles of rows
     uint32_t tiles, splits, split_keys;
+    bool uneven;      // sequences of different lengths, which the kernels go by
     uint64_t bytes;   // of workspace
 };
 
@@ -148,6 +149,8 @@ Cut cut_of(const CacheView &c, uint32_t window, const CutRule &rule)
             const uint64_t f = units * n * 1000 / ((units * n + 255) / 256 * 256);
             if (f > filled) best = n, filled = f;
         }
+        // a batch of different lengths may want more
+        if (c.n_seq > 1) best = std::min(2 * best, std::max<uint64_t>(1, most));
         keys = (span + best - 1) / best;
     }
     // no more parts than without a window: the workspace is asked for without one
@@ -156,6 +159,7 @@ Cut cut_of(const CacheView &c, uint32_t window, const CutRule &rule)
     keys = std::max(unit, (keys + unit - 1) / unit * unit);
     p.splits = (uint32_t)std::max<uint64_t>(1, (span + keys - 1) / keys);
     p.split_keys = (uint32_t)keys;
+    p.uneven = p.splits > 1 && c.n_seq > 1 && c.n_seq <= 64 && (few ? c.max_q * c.group > kFewRows : !window);
     if (p.splits > 1) p.bytes = (uint64_t)p.splits * c.total_q * c.heads * (c.head_dim + 2) * 4;
     return p;
 }
@@ -255,6 +259,7 @@ void fill_attention(AttentionArgs &a, const void *q, uint64_t q_stride, const vo
     a.tiles = p.tiles;
     a.splits = p.splits;
     a.split_keys = p.split_keys;
+    a.uneven = p.uneven;
     const uint64_t parts = (uint64_t)p.splits * a.c.total_q * a.c.heads;
     a.part_o = static_cast<float *>(workspace);
     a.part_ml = a.part_o ? a.part_o + parts * a.c.head_dim : nullptr;

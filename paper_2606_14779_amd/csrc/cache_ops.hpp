@@ -41,6 +41,8 @@ struct AttentionArgs {
     uint32_t window;                 // 0: none
     uint32_t few_rows;               // most rows of a sequence where the waves split the keys; 0: attention_rows
     uint32_t tiles, splits, split_keys;
+    uint32_t uneven;                 // sequences of different lengths, whose parts are not all there; for attention_rows
+                                     // splits is a bound and split_keys is found by the lengths
     float *part_o;                   // [splits][total_q * heads][head_dim]
     float *part_ml;                  // [splits][total_q * heads][2]
     // of attention over pages alone

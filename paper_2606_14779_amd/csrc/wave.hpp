@@ -212,6 +212,8 @@ __device__ __forceinline__ uint32_t sum_upto(uint32_t x)
 struct Tile {
     uint32_t seq, tile, split;
     Seq s;
+    Seq mine;         // lane i: sequence i
+    uint32_t tiles;   // and how many it has
 };
 constexpr uint32_t kNoTile = 0xFFFFFFFFu;
 __device__ __forceinline__ Tile tile_by_length(const CacheView &c, uint32_t index, uint32_t splits, uint32_t tile_rows,
@@ -229,7 +231,8 @@ __device__ __forceinline__ Tile tile_by_length(const CacheView &c, uint32_t inde
     };
     auto all = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane(sum_upto(x), 63); };
     const uint32_t there = all(tiles), split = there ? index / there : splits, rank = index - split * there;
-    if (split >= splits) return {0, kNoTile, 0, s};
+    if (split >= splits) return {0, kNoTile, 0, s, s, 0};
+    const Seq mine = s;
     uint32_t lo = 0, hi = c.max_kv / keys + 2;       // all(at_least(lo)) > rank >= all(at_least(hi))
     while (hi - lo > 1) {
         const uint32_t mid = (lo + hi) / 2;
@@ -244,7 +247,7 @@ __device__ __forceinline__ Tile tile_by_length(const CacheView &c, uint32_t inde
     const int who = __ffsll((unsigned long long)found) - 1;
     auto from = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane(x, who); };
     s = {(int32_t)from(s.q_begin), (int32_t)from(s.n_q), (int32_t)from(s.kv)};
-    return {(uint32_t)who, from(tiles) - from(longer + these) + left - (from(upto) - from(these)), split, s};
+    return {(uint32_t)who, from(tiles) - from(longer + these) + left - (from(upto) - from(these)), split, s, mine, tiles};
 }
 
 }  // namespace kvp
