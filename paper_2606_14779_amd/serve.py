@@ -46,8 +46,8 @@ class ServeRun:
         self.slots = slots
         self.most = np.array(contexts, np.int64) + room   # cached tokens that a sequence has room for
         self.table = torch.from_numpy(table).to(self.device)
-        self.cache = torch.zeros((shape.layers, 2, slots, shape.kv_heads, bs, shape.head_dim), dtype=self.dtype,
-                                 device=self.device)
+        self.cache_shape = K.CacheShape(dtype, q_heads, shape.kv_heads, shape.head_dim, bs, slots)
+        self.cache, spec = self._new_cache()
         self.k_ptrs = [layer[0].data_ptr() for layer in self.cache]
         self.v_ptrs = [layer[1].data_ptr() for layer in self.cache]
         self.lens = np.array(contexts, np.int32)        # cached tokens
@@ -57,14 +57,19 @@ class ServeRun:
         self.pos = torch.arange(self.max_kv, dtype=torch.int32, device=self.device).expand(per_head).contiguous()
         self.rot, self.rope = shape.head_dim, dict(rope or {})
         self._positions_up_to(self.max_kv + room)
-        self.cache_shape = K.CacheShape(dtype, q_heads, shape.kv_heads, shape.head_dim, bs, slots)
-        spec = K.KVSpec(shape.layers, shape.kv_heads, shape.head_dim, bs, 2)
         held = sum(blocks) * 2 + 2 * n + 2              # twice over, so that a request can be replaced
         self.pool = K.KVPool([K.Region("host", held * spec.block_bytes), K.Region("staging", held * spec.block_bytes)],
                              [1, 1], spec, device)
         self.requests, self._next_request = [None] * n, 1
         self.held = np.zeros(n, bool)                   # whether a sequence's request has its cached tokens as they are
         self._work = None
+
+    def _new_cache(self):
+        """The engine's cache, [layers][K and V][slots]..., and its shape for the pool."""
+        shape = self.shape
+        cache = self.torch.zeros((shape.layers, 2, self.slots, shape.kv_heads, shape.block_size, shape.head_dim),
+                                 dtype=self.dtype, device=self.device)
+        return cache, K.KVSpec(shape.layers, shape.kv_heads, shape.head_dim, shape.block_size, 2)
 
     def _stream(self) -> int:
         return self.torch.cuda.current_stream(self.device).cuda_stream

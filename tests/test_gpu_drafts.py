@@ -1,0 +1,136 @@
+"""Runs over the pool with drafted tokens: pages of either kind fetched, extended by trees, committed and offloaded."""
+import types
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import pages_ref as P   # noqa: E402
+from paper_2606_14779_amd.drafts import DraftRun, tree_mask   # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+SHAPE = types.SimpleNamespace(layers=2, kv_heads=2, head_dim=64, block_size=16)
+CONTEXTS, HEADS = [300, 77], 8
+
+
+@pytest.fixture(autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def _filled(kind, seed=1, **kw):
+    """A run whose contexts hold random tokens, and the same ones whatever the slots are."""
+    run = DraftRun(SHAPE, HEADS, CONTEXTS, room=64, pages=kind, rope=dict(base=10000.0), **kw)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    for layer in run.cache:
+        for buffer in layer:
+            b = _buffer(run, buffer)
+            for s, n in enumerate(CONTEXTS):
+                b.put(*_places(run, s, 0, n), torch.randn(n, 2, 64, generator=g, device="cuda").to(torch.bfloat16))
+    return run, g
+
+
+def _buffer(run, buffer):
+    b = object.__new__(P.Buffer)
+    b.kind, b.dims, b.dtype = run.kind, (run.slots, 2, 16, 64), "bf16"
+    b.raw = buffer.view(torch.uint8).reshape(run.slots, -1)
+    return b
+
+
+def _places(run, s, first, end):
+    slot = np.repeat(run.tables[s], 16)[first:end].astype(np.int64)
+    return torch.from_numpy(slot).cuda(), torch.arange(first, end, device="cuda") % 16
+
+
+def _rows(run, layer, kv, s, n):
+    return _buffer(run, run.cache[layer, kv]).rows(*_places(run, s, 0, n))
+
+
+def _qkv(g, total):
+    return [torch.randn(total, HEADS + 4, 64, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2)]
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "16"])
+def test_a_round_trip_keeps_every_byte(kind):
+    run, _ = _filled(kind)
+    before = [_rows(run, 1, kv, s, n) for kv in (0, 1) for s, n in enumerate(CONTEXTS)]
+    run.offload()
+    run.cache.view(torch.uint8).fill_(0x7F)
+    run.fetch()
+    after = [_rows(run, 1, kv, s, n) for kv in (0, 1) for s, n in enumerate(CONTEXTS)]
+    assert all(torch.equal(a, b) for a, b in zip(before, after))
+    run.close()
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "16"])
+@pytest.mark.parametrize("normed", [False, True])
+def test_accepted_drafts_are_the_tokens_themselves(kind, normed):
+    """Drafts attended in a tree and committed leave what the accepted tokens alone would have left, and gave the outputs
+    that they would have had.
+
+    Outputs are averages of values v of weight 1 in all.  Each is off by a rounding of every weight and one of its own,
+    2^-8 max|v| each at most, and by less than 2^-12 max|v| for logits and exponentials in 32 bits (below 2^4 here:
+    2^-20 of their magnitudes, and 2^-22): two of them by twice that."""
+    w = torch.randn(2, 64, device="cuda").to(torch.bfloat16)
+    norm = (w, w.flip(1).contiguous(), 1e-6) if normed else None
+    drafted, g = _filled(kind, norm=norm)
+    plain, _ = _filled(kind, norm=norm)
+    rng = np.random.default_rng(3)
+    for new in ([20, 5], [3, 12]):
+        parents = [[-1] + [int(rng.integers(max(0, i - 3), i)) for i in range(1, n)] for n in new]
+        paths = []
+        for p in parents:
+            path, at = [], int(rng.integers(0, len(p)))
+            while at >= 0:
+                path.append(at)
+                at = p[at]
+            paths.append(path[::-1])
+        qkv = _qkv(g, sum(new))
+        rows = torch.tensor([a + i for a, p in zip((0, new[0]), paths) for i in p], device="cuda")
+        drafted.begin(new, np.concatenate([tree_mask(p) for p in parents]))
+        outs = [drafted.layer(i, x) for i, x in enumerate(qkv)]
+        drafted.commit(paths)
+        plain.begin([len(p) for p in paths])
+        want = [plain.layer(i, x[rows].contiguous()) for i, x in enumerate(qkv)]
+        assert (drafted.lens == plain.lens).all() and (drafted.seen == plain.seen).all()
+        assert drafted.kv_len.tolist() == plain.lens.tolist()
+        for i in range(2):
+            most = max(_rows(plain, i, 1, s, n).abs().max().item() for s, n in enumerate(plain.lens))
+            assert (outs[i][rows].double() - want[i].double()).abs().max().item() <= 2 * (2 ** -7 + 2 ** -12) * most
+            for s, n in enumerate(plain.lens):
+                for kv in (0, 1):
+                    assert torch.equal(_rows(drafted, i, kv, s, int(n)), _rows(plain, i, kv, s, int(n)))
+                assert torch.equal(drafted.pos[i, s, :, :n], plain.pos[i, s, :, :n])
+    drafted.offload()
+    drafted.fetch()
+    drafted.close()
+    plain.close()
+
+
+def test_what_a_run_refuses():
+    run, g = _filled("e4m3")
+    mask = np.concatenate([tree_mask([-1, 0, 0]), tree_mask([-1])])
+    for bad in (dict(new=[3, 1], tree=mask[:3]), dict(new=[3, 1], tree=mask.ravel()), dict(new=[65, 0], tree=np.ones((65, 1))),
+                dict(new=[3, 1], tree=np.zeros((4, 1)))):
+        with pytest.raises(ValueError):
+            run.begin(**bad)
+    with pytest.raises(ValueError):
+        run.commit([[0], [0]])
+    run, g = _filled("e4m3")
+    run.begin([3, 1], mask)
+    for f in (run.offload, run.fetch, lambda: run.begin([1, 1]), lambda: run.commit([[0]]), lambda: run.commit([[1, 0], []]),
+              lambda: run.commit([[0, 3], []]), lambda: run.commit([[-1], []]), lambda: run.evict(10, 5),
+              lambda: run.layer(0, _qkv(g, 4)[0], mass_from=1)):
+        with pytest.raises(ValueError):
+            f()
+    run.commit([[], []])
+    assert run.lens.tolist() == CONTEXTS
+    for parents in ([0], [-1, 1], [-2]):
+        with pytest.raises(ValueError):
+            tree_mask(parents)
+    with pytest.raises(ValueError):
+        _filled("e4m3", norm=(torch.ones(2, 32, device="cuda").bfloat16(),) * 2 + (1e-6,))
+    run.close()
