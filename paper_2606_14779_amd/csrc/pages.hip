@@ -115,29 +115,32 @@ __device__ __forceinline__ void put8(const PageView &p, uint32_t head_dim, uint8
 // How the pairs lie: both in the 8 elements of a lane, in two lanes, or anyhow.
 enum Pairs { kInside, kApart, kAnyhow };
 
-// The norm's factor of a head whose lanes hold x.  Squares that leave the range of 32 bits are taken of x * 2^k instead.
+// The norm's factor of a head whose lanes hold x.  Where the squares leave the range of 32 bits (as bf16's may) and eps does
+// not make up for it, x and its partners y are scaled by a power of two first: what `up` says.
 template <class T>
-__device__ __forceinline__ float norm_factor(const AppendArgs &a, const float (&x)[8], uint32_t lanes)
+__device__ __forceinline__ float norm_factor(const AppendArgs &a, float (&x)[8], float (&y)[8], uint32_t lanes, float &up)
 {
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(x[i], x[i], sum);
     sum = sum_over(sum, lanes);
-    float factor = __builtin_amdgcn_rsqf(__builtin_fmaf(sum, a.per_dim, a.eps));
-    if (__builtin_expect(__any(!(sum < 1e36f && sum > 1e-30f)), 0)) {
+    up = 1.0f;
+    const bool fits = sum < 1e36f && (sum > 1e-30f || a.eps > 1e-20f);
+    float mean = __builtin_fmaf(sum, a.per_dim, a.eps);
+    if (__builtin_expect(__any(!fits), 0)) {
         const float top = largest_over(largest_of(x), lanes);
-        if (top > 0.0f && !(sum < 1e36f && sum > 1e-30f)) {
-            const int k = top > 1.0f ? -64 : 64;     // bf16 ends at 2^128, and f16 does not come here but with eps below it
-            const float up = __builtin_ldexpf(1.0f, k);
-            float s = 0.0f;
+        if (!fits && top > 0.0f) up = top > 1.0f ? 0x1p-96f : 0x1p96f;   // squares from 2^-74 to 2^92
+        float s = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s = __builtin_fmaf(x[i] * up, x[i] * up, s);
-            s = sum_over(s, lanes);
-            const float mean = s * a.per_dim + __builtin_ldexpf(a.eps, 2 * k);
-            factor = __builtin_ldexpf(__builtin_amdgcn_rsqf(mean), k);
+        for (int i = 0; i < 8; ++i) {
+            x[i] *= up;
+            y[i] *= up;
+            s = __builtin_fmaf(x[i], x[i], s);
         }
+        s = sum_over(s, lanes);
+        if (up != 1.0f) mean = __builtin_fmaf(s, a.per_dim, a.eps * up * up);
     }
-    return factor;
+    return __builtin_amdgcn_rsqf(mean);
 }
 
 // A token to a workgroup.  A wave takes whole heads of one kind (queries, keys or values) at a time, so that its lanes go
@@ -256,7 +259,7 @@ __global__ __launch_bounds__(256) void append(const AppendArgs a)
         float x[8];
         if (E8 || !value) unpack8<T>(raw, x);
         if (!value) {
-            float y[8];
+            float y[8] = {}, up = 1.0f;
             if constexpr (PAIRS == kInside) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[e] = x[e ^ 1];
@@ -267,7 +270,7 @@ __global__ __launch_bounds__(256) void append(const AppendArgs a)
                 for (int w = 0; w < 4; ++w) far[w] = __shfl(raw[w], other);
                 unpack8<T>(far, y);
             }
-            const float factor = a.norm ? norm_factor<T>(a, x, lanes) : 1.0f;
+            const float factor = a.norm ? norm_factor<T>(a, x, y, lanes, up) : 1.0f;
             if constexpr (PAIRS == kAnyhow) {
                 const uint16_t *from = (query ? q : k) + (uint64_t)(head * c.head_dim), *weight = query ? a.q_weight : a.k_weight;
 #pragma unroll
@@ -276,7 +279,7 @@ __global__ __launch_bounds__(256) void append(const AppendArgs a)
                     if (!asked || at + e >= a.rot) continue;
                     const bool upper = a.interleaved ? e & 1 : at + e >= half;
                     const uint32_t other = a.interleaved ? (at + e) ^ 1 : upper ? at + e - half : at + e + half;
-                    const float y = T::unpack(from[other], 0) * (weight ? T::unpack(weight[other], 0) : 1.0f);
+                    const float y = T::unpack(from[other], 0) * up * (weight ? T::unpack(weight[other], 0) : 1.0f);
                     const v2f f = angles[a.interleaved ? (at + e) / 2 : upper ? other : at + e];
                     x[e] = __builtin_fmaf(x[e], f[0], upper ? y * f[1] : -(y * f[1]));
                 }
