@@ -383,8 +383,8 @@ __global__ __launch_bounds__(256) void convert(const ConvertArgs a)
                 uint8_t *p = to_cache[v] + (there[r] ? to[r] : 0);
                 if constexpr (BACK) {
                     if (there[r] && live)
-                        *(w4 *)(p + ((uint64_t)row[r] * c.head_dim + piece * 8) * 2) =
-                            widen<T>(thin[v][r], power_of(word[v][r], piece / 4 % 4 * 8));
+                        __builtin_nontemporal_store(widen<T>(thin[v][r], power_of(word[v][r], piece / 4 % 4 * 8)),
+                                                    (w4 *)(p + ((uint64_t)row[r] * c.head_dim + piece * 8) * 2));
                 } else {
                     float x[8];
                     unpack8<T>(wide[v][r], x);

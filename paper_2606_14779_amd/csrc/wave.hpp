@@ -100,6 +100,8 @@ struct F16 {
 };
 
 __device__ __forceinline__ w4 load16g(const uint16_t *p) { return *(gw4 *)p; }
+// The same past the caches, for what is read once: a line has to be one load's, or it is fetched again.
+__device__ __forceinline__ w4 stream16g(const uint16_t *p) { return __builtin_nontemporal_load((gw4 *)p); }
 __device__ __forceinline__ w2 load8g(const uint16_t *p) { return *(__attribute__((address_space(1))) const w2 *)p; }
 __device__ __forceinline__ int32_t load4g(const int32_t *p) { return *(gi32 *)p; }
 
