@@ -756,7 +756,8 @@ int kv_evict_workspace(const kvp_cache_shape *shape, const kvp_batch *batch, uin
  *       what they hold; bytes past the last such b are written as 0,
  * rounded up to a multiple of 16 bytes (kv_page_bytes).  Where nothing has to
  * be rounded up, a pool moves such slots as those of a kvp_kv_spec with
- * elem_bytes 1 and head_dim + 4 * ceil(head_dim / 128) in place of head_dim.
+ * elem_bytes 1 and head_dim + 4 * ceil(head_dim / 128) in place of head_dim;
+ * slots of 32 KB and more do so at the pool's full rate.
  *
  * A row x of 32 elements (fewer at the end of a head) is written with the
  * least exponent e that has max |x| <= 448 * 2^e, within -117 to 120 for

@@ -7,7 +7,7 @@
 // exp2(S log2e - m log2e), so the exponential is one instruction).
 //
 // The rows of a KV head are its (new token, query head of the group) pairs, token-major: every key and
-// value that is fetched serves the whole group.  Both kernels compute S transposed, S^T = K Q^T: a lane
+// value that is fetched serves the whole group.  The kernels compute S transposed, S^T = K Q^T: a lane
 // then owns one row (column of the MFMA result), so maximum and sum are per-lane values, and the lane's
 // results, rounded to 16 bits, already are the B operand of O^T = V^T P^T, with no exchange between lanes:
 // the order of the keys inside a product is free, and V's transposed LDS reads follow the order that the
@@ -16,7 +16,8 @@
 // attention_rows: 32 rows to a wave, 256 to a workgroup, kTileKeys keys at a time through LDS.
 // attention_few: up to 16 rows (single tokens and very short chunks), where reading the cache is all that
 // counts: the waves of a workgroup split the keys, and a join in LDS ends the workgroup.
-// Where there are few row tiles both split the keys over workgroups as well; attention_join adds the parts.
+// attention_some: the same for 17 to 64 rows, of drafts or over 8-bit pages.
+// Where there are few row tiles all split the keys over workgroups as well; attention_join adds the parts.
 
 #include "attention_kernels.hpp"
 
@@ -26,7 +27,7 @@ namespace {
 
 // Adds the parts of the rows.  A row is the work of `slices` times LANES neighbouring threads: a thread has 4
 // elements of head_dim and every slices-th part, U of them in flight; the slices are added through LDS, always in
-// the same order.
+// the same order.  SPARSE: parts without weight have no output to be asked for, which a look at their sums tells first.
 template <class T, int LANES, int U, bool SPARSE>
 __global__ __launch_bounds__(256) void attention_join(const AttentionArgs a, const uint32_t slices)
 {

@@ -1,4 +1,5 @@
-// Attention over 8-bit pages, causal or with a mask among the new tokens, for gfx950 (MI355X): instances of attention_kernels.hpp.
+// Attention over 8-bit pages, causal or with a mask among the new tokens, for gfx950 (MI355X): instances of
+// attention_kernels.hpp.
 
 #include "attention_kernels.hpp"
 

@@ -1,5 +1,11 @@
-// Kernels of attention over the paged cache, for gfx950: what attention.hip launches on 16-bit pages and
-// attention_pages.hip on pages of either kind with a mask among the new tokens.
+// Kernels of attention over the paged cache, for gfx950 (MI355X): attention.hip, whose first lines have the formulas,
+// launches them on 16-bit pages, attention_tree.hip with a mask among the new tokens, attention_e4m3.hip on 8-bit pages.
+//
+// With a mask a new token sees all keys before the new ones (as far as its window goes) and the new ones whose bit is set in
+// its row, words of 64 bits: tiles of keys before the new tokens are as under a causal mask without an edge, and the
+// others' bits are shifted to where the tile begins.
+// Of 8-bit pages the elements become 16-bit floats on their way to the products: exact, one instruction for two of them with
+// their power of two (e4m3.hpp), so that all that follows is the same.
 #ifndef KVP_ATTENTION_KERNELS_HPP
 #define KVP_ATTENTION_KERNELS_HPP
 
@@ -117,7 +123,8 @@ __device__ __forceinline__ uint32_t lowest_of(uint32_t x)
 }
 __device__ __forceinline__ uint32_t longest_of(uint32_t x) { return ~lowest_of(~x); }
 // Workgroups of row tiles, one to a CU: of 1 to 64 parts to the longest sequence that number for which the rounds of the chip,
-// each as long as a part's tiles of keys and about five more to begin and end, take least.
+// each as long as a part's tiles of keys (2.1 us each at head_dim 128) and about five more to begin and end, take least.
+// Trees of 32 x 16 over up to 8K (32, 8, 128): 125 us by sizes alone, 90 so; of 64 x 4 over 32K (32, 4, 128) 217 and 174.
 __device__ __forceinline__ uint32_t keys_of_rounds(const AttentionArgs &a, uint32_t span, uint32_t tiles)
 {
     const uint32_t lane = threadIdx.x & 63, longest = longest_of(tiles ? span : 0);
@@ -198,6 +205,10 @@ __device__ __forceinline__ bool unbounded_row(const AttentionArgs &a, uint32_t r
 // 512 new tokens over 128K (32 heads, 8 KV heads, 128): 1074 us, 1022 TFLOP/s, where a bf16 matrix product of 16384^3
 // reaches 1370.  Matrix cores busy for 51 % of the cycles, no LDS bank conflicts, 87 % of the L2 reads hit; the clock
 // falls to about 2.0 GHz of 2.4 under it.  Without turns (four waves, two such workgroups to a CU) 1218 us.
+// The same over 8-bit pages: 1080 us on a card where 16-bit ones take 1050 to 1090: a sixth more vector instructions, for
+// widening what a lane has loaded, and half the bytes.  64 drafts over 128K (32, 4, 128) in 8 bits: 163 us with the join,
+// 840 TFLOP/s, 67 tiles to each of 248 workgroups.  Two tiles ahead instead of one: 2 % more for 8-bit pages, 1 % less for
+// 16-bit ones.
 template <class T, int DP, class Offset, int KIND = kCausal16>
 __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attention_rows(const AttentionArgs a)
 {
@@ -611,6 +622,9 @@ constexpr int kFewKeys = 32;    // to a wave at a time
 // Short contexts are bound by what has to be known before the first key can be asked for, so the block table's
 // entries are asked for together with the sequence's length wherever they do not depend on it.
 // Two waves to a SIMD: three would have 168 registers, and what does not fit them costs more (276 us for those 32 tokens).
+// Of 8-bit pages a lane's load is 16 elements and half the registers do, so there are three.  One token over 128K (32, 8, 128):
+// 52.8 us with its join, 5.2 TB/s; 32 over ragged 16K 113 us, 4.4 TB/s (116 if the values, each line one load's, stay in the
+// caches; 119 if keys go past them as well, whose lines are two loads').  64 keys at a time and two waves: 61 and 129.
 template <class T, int DP, int KIND = kCausal16>
 __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2) void attention_few(const AttentionArgs a)
 {
@@ -940,7 +954,8 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
 // ---- up to 32 or 64 rows, the waves split the keys
 
 // The rest-th part of the keys of a batch of up to 64 sequences: those that hold keys first, sequence by sequence, then the
-// empty ones.  Workgroups begin in this order on one place of the chip after the other, whether they have work or not.
+// empty ones.  Workgroups begin in this order on one place of the chip after the other, whether they have work or not: with the
+// empty ones between the others some CUs have two that work and some none (trees of 8 x 16 over up to 8K: 61 us, 50 in order).
 struct Part {
     uint32_t seq, split;
     Seq s;
@@ -969,6 +984,10 @@ __device__ __forceinline__ Part part_of(const AttentionArgs &a, uint32_t rest, b
 // Drafts of a few tokens, whose group's heads make 17 to 64 rows: attention_few with products of 32 rows.  A wave has 32
 // rows and 32 keys at a time, which its lanes take from memory as the products want them; values pass through the wave's
 // own part of LDS, to be read by columns.  With two groups of rows (RG) neighbouring waves load the same keys.
+// Bound by reading the cache up to 32 rows: 8 drafts over 128K (32 heads, 8 KV heads, 128) 97 us, 5.5 TB/s with the join, in 8
+// bits 60, 4.6; trees of 8 x 16 over up to 8K 45 to 49 us, where workgroups of 64 rows in attention_rows took 175.  With 64 rows
+// by the vector unit and each wave's own turn: 16 drafts over 128K in 8 bits 93 us; all 64 rows in one wave, without another
+// wave on the SIMD to fill the gaps, took 153.
 template <class T, int DP, int KIND, int RG>
 __global__ __launch_bounds__(kFewWaves * RG * 64, DP > 128 ? 1 : 2) void attention_some(const AttentionArgs a)
 {
@@ -999,7 +1018,8 @@ __global__ __launch_bounds__(kFewWaves * RG * 64, DP > 128 ? 1 : 2) void attenti
         split = __builtin_amdgcn_readfirstlane(p.split);
         seq = __builtin_amdgcn_readfirstlane(p.seq);
         if (seq == kNoTile) return;
-        s = {__builtin_amdgcn_readfirstlane(p.s.q_begin), __builtin_amdgcn_readfirstlane(p.s.n_q), __builtin_amdgcn_readfirstlane(p.s.kv)};
+        s = {__builtin_amdgcn_readfirstlane(p.s.q_begin), __builtin_amdgcn_readfirstlane(p.s.n_q),
+             __builtin_amdgcn_readfirstlane(p.s.kv)};
     } else {
         s = load_seq(c, seq);
     }
@@ -1010,7 +1030,8 @@ __global__ __launch_bounds__(kFewWaves * RG * 64, DP > 128 ? 1 : 2) void attenti
     if (a.splits > 1 && keys.begin >= keys.end) {      // of no weight: its output is not looked at
         for (uint32_t r = tid; r < rows; r += kFewWaves * RG * 64) {
             const uint32_t t = token_of(c, r), h = kv_head * c.group + r - t * c.group;
-            *(v2f *)(a.part_ml + 2 * ((uint64_t)split * c.total_q * c.heads + ((uint64_t)s.q_begin + t) * c.heads + h)) = v2f{kLowest, 0.0f};
+            const uint64_t part = (uint64_t)split * c.total_q * c.heads + ((uint64_t)s.q_begin + t) * c.heads + h;
+            *(v2f *)(a.part_ml + 2 * part) = v2f{kLowest, 0.0f};
         }
         return;
     }

@@ -108,7 +108,8 @@ struct Cut {
 };
 
 // How an attention call is cut.  A KV head's rows (new tokens x group) go to attention_few if no sequence has more
-// than a 16-row product holds, else to tiles of 256 (128 at a head_dim of more than 128).  Where the tiles do not
+// than a 16-row product holds, to attention_some up to 64 (32) by the rule of calls that it is for, else to tiles of
+// 256 (128 at a head_dim of more than 128).  Where the tiles do not
 // fill the chip, the keys are split, as far as a part holds enough keys to be worth its output's way through memory.
 Cut cut_of(const CacheView &c, uint32_t window, const CutRule &rule)
 {
@@ -130,10 +131,10 @@ Cut cut_of(const CacheView &c, uint32_t window, const CutRule &rule)
                                            : std::max<uint64_t>(c.n_seq, rows / tile_rows + c.n_seq / 2)) * c.kv_heads;
     uint64_t keys = span;                            // of a part
     if (few) {
-        // about 1024 parts (by the rule), which read the cache at its full rate, and not above 1024 keys where lengths may differ, so
-        // that none is left alone at the end.  32 sequences of up to 16K: 191 us at 1024 keys, 210 at 512, 223 at 4096;
-        // one of 128K: 47 us at 1024, 49 at 512, 67 at 128.  256 keys stay whole: 8.5 us, where two parts and their join
-        // take 10.8.
+        // about 1024 parts of 16-bit pages, which read the cache at its full rate (512 by the rule of other calls), and not
+        // above 1024 keys where lengths may differ, so that none is left alone at the end.  32 sequences of up to 16K: 191 us
+        // at 1024 keys, 210 at 512, 223 at 4096; one of 128K: 47 us at 1024, 49 at 512, 67 at 128.  256 keys stay whole: 8.5
+        // us, where two parts and their join take 10.8.
         if (span > 256) {
             keys = std::max<uint64_t>(128, units * span / rule.parts);
             if (c.n_seq > 1) keys = std::min<uint64_t>(keys, 1024);
@@ -149,8 +150,8 @@ Cut cut_of(const CacheView &c, uint32_t window, const CutRule &rule)
             const uint64_t f = units * n * 1000 / ((units * n + 255) / 256 * 256);
             if (f > filled) best = n, filled = f;
         }
-        // a batch of different lengths may want more
-        if (c.n_seq > 1) best = std::min(2 * best, std::max<uint64_t>(1, most));
+        // a batch of different lengths may want more, which its workgroups find out
+        if (c.n_seq > 1 && c.n_seq <= 64 && !window) best = std::min(2 * best, std::max<uint64_t>(1, most));
         keys = (span + best - 1) / best;
     }
     // no more parts than without a window: the workspace is asked for without one

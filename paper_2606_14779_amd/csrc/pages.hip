@@ -7,7 +7,12 @@
 //   table has for the pair and the token's position on the pair's axis
 // in 32 bits, and is rounded once: to 16 bits, or to e4m3 with the least power of two that holds 32 elements.
 // A head is the work of 2^lanes_log2 neighbouring lanes with 8 elements each, so that sums of squares and largest
-// elements are exchanges within a wave.
+// elements are exchanges within a wave.  Queries, keys and values are read once and written once.
+//
+// Bound by memory and by what a token has to wait for: packed prompts of 12.7K tokens (64 heads, 8 KV heads, 64; norms, three
+// axes, pairs interleaved, 16-bit pages) 55.5 us, 263 MB at 4.7 TB/s, vector unit busy for 57 % of the cycles.  With every
+// head's weights and angles worked out anew 73; with the token's positions, sequence and slot asked for one after the other
+// 65.  A decoding step of 32 tokens takes 6.5 us on the GPU.
 
 #include <algorithm>
 #include <type_traits>
@@ -158,7 +163,8 @@ __global__ __launch_bounds__(256) void append(const AppendArgs a)
     const uint32_t piece = lane & (lanes - 1), at = piece * 8, mine = lane >> a.lanes_log2;
     const bool live = at < c.head_dim;
     const uint32_t jobs_log2 = 6 - a.lanes_log2;
-    const uint32_t q_jobs = a.q ? (c.heads + per_wave - 1) >> jobs_log2 : 0, k_jobs = (c.kv_heads + per_wave - 1) >> jobs_log2;
+    const uint32_t q_jobs = a.q ? (c.heads + per_wave - 1) >> jobs_log2 : 0;
+    const uint32_t k_jobs = (c.kv_heads + per_wave - 1) >> jobs_log2;
     const uint16_t *q = a.q + token * a.q_stride, *k = a.k + token * a.k_stride, *v = a.v + token * a.v_stride;
 
     auto load = [&](auto kind, uint32_t job) __attribute__((always_inline)) {
@@ -328,6 +334,9 @@ __global__ __launch_bounds__(256) void append(const AppendArgs a)
 }
 
 // A workgroup has kConvertTokens tokens of a sequence and KV head: all of its loads are asked for before the first store.
+// Bound by memory: 72.6K cached tokens (8 KV heads, 128) from 8 bits to 16 in 60.7 us, 308 MB at 5.1 TB/s, the rate of a copy
+// of this size by torch; 66.7 where the stores stay in the caches, 64.4 where the loads go past them too.  5001 tokens (5 KV
+// heads, 80) from 16 bits to 8 take 7.8 us, four dependent loads and the exchanges of an exponent.
 template <class T, bool BACK, int ROWS>
 __global__ __launch_bounds__(256) void convert(const ConvertArgs a)
 {
@@ -396,6 +405,8 @@ __global__ __launch_bounds__(256) void convert(const ConvertArgs a)
 
 // A workgroup has a sequence and KV head.  As the path ascends, a row moves down or stays, so rows are taken in order:
 // what a pass stores lies where it or an earlier one has read.
+// Bound by dependent loads: the path, the block table, the rows.  1024 lanes with four rows each in flight: 256 drafts x 48 (4
+// KV heads, 128, 8 bits) 6.7 us, 11.0 with 256 lanes and one row; 8 x 32 3.2 us.
 template <bool E8, int ROWS>
 __global__ __launch_bounds__(ROWS > 1 ? 1024 : 256) void commit(const CommitArgs a)
 {
@@ -511,8 +522,9 @@ hipError_t launch_convert_as(const ConvertArgs &a, hipStream_t stream)
 
 hipError_t launch_append(const AppendArgs &a, uint32_t dtype, hipStream_t stream)
 {
-    if (dtype == KVP_BF16) return a.pages.exponents ? launch_append_as<BF16, true>(a, stream) : launch_append_as<BF16, false>(a, stream);
-    return a.pages.exponents ? launch_append_as<F16, true>(a, stream) : launch_append_as<F16, false>(a, stream);
+    const bool e8 = a.pages.exponents;
+    if (dtype == KVP_BF16) return e8 ? launch_append_as<BF16, true>(a, stream) : launch_append_as<BF16, false>(a, stream);
+    return e8 ? launch_append_as<F16, true>(a, stream) : launch_append_as<F16, false>(a, stream);
 }
 
 hipError_t launch_convert(const ConvertArgs &a, uint32_t dtype, hipStream_t stream)
