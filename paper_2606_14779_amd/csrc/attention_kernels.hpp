@@ -350,17 +350,14 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
             for (int w = 0; w < XW; ++w) to[w] = (uint32_t)load4g((const int32_t *)((const char *)cache + at) + w);
         }
     };
-    // what was loaded of 8-bit pages, as 16-bit floats
-    auto wide = [&](const w2 (&from)[N], const uint32_t (&exponents)[XW], w4 (&to)[N]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            uint32_t word = lane_value(exponents[0], load_row + i * PASS);
-            if constexpr (XW > 1) {
-                const uint32_t other = lane_value(exponents[1], load_row + i * PASS);
-                word = load_piece >= 16 ? other : word;
-            }
-            to[i] = widen<T>(from[i], power_of(word, load_piece / 4 % 4 * 8));
+    // row i of what was loaded of 8-bit pages, as 16-bit floats
+    auto wide = [&](w2 from, const uint32_t (&exponents)[XW], int i) __attribute__((always_inline)) {
+        uint32_t word = lane_value(exponents[0], load_row + i * PASS);
+        if constexpr (XW > 1) {
+            const uint32_t other = lane_value(exponents[1], load_row + i * PASS);
+            word = load_piece >= 16 ? other : word;
         }
+        return widen<T>(from, power_of(word, load_piece / 4 % 4 * 8));
     };
     // Rows of 64 elements lie two to 64 banks of LDS, longer ones fill them: the pieces of a row change places with
     // its number, so that 16 rows read at one place of K, and four at four places of V, meet different banks.  PASS
@@ -378,44 +375,51 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
         for (int i = 0; i < DP / 32; ++i)
             v_read[i] = r * DP * 2 + ((4 * i + 2 * (lane >> 4 & 1) + (ti % 4) / 2) ^ v_place(r)) * 16 + (ti & 1) * 8;
     }
-    auto put_k = [&](uint32_t buffer, w4 (&x)[N]) __attribute__((always_inline)) {
-        if (__builtin_expect(c.head_dim != DP, 0) && !piece_live) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) x[i] = w4{0, 0, 0, 0};
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i) *(w4 *)(lds + (k_store + buffer) + i * PASS * DP * 2) = x[i];
-    };
-    auto put_v = [&](int32_t t, uint32_t buffer, uint64_t seen, w4 (&x)[N]) __attribute__((always_inline)) {
-        if (__builtin_expect(c.head_dim != DP || seen != ~0ull, 0)) {
-#pragma unroll
-            for (int i = 0; i < N; ++i)              // what is not there must be finite: its weight is 0
-                if (!piece_live || !(seen >> (load_row + i * PASS) & 1)) x[i] = w4{0, 0, 0, 0};
-        }
-        const int32_t k0 = keys.begin + t * TK;
-        if (__builtin_expect(k0 + TK - 1 > all_first || k0 < all_full, 0)) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) bounded &= T::bound(x[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i) *(w4 *)(lds + (v_store + buffer) + i * PASS * DP * 2) = x[i];
-    };
     auto store_k = [&](uint32_t buffer) __attribute__((always_inline)) {
         if constexpr (E8) {
-            w4 x[N];
-            wide(rk, xk, x);
-            put_k(buffer, x);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                w4 x = wide(rk[i], xk, i);
+                if (__builtin_expect(c.head_dim != DP, 0) && !piece_live) x = w4{0, 0, 0, 0};
+                *(w4 *)(lds + (k_store + buffer) + i * PASS * DP * 2) = x;
+                if (DP > 128) __builtin_amdgcn_sched_barrier(0);   // widened all at once they do not fit the registers
+            }
+            return;
         } else {
-            put_k(buffer, rk);
+            if (__builtin_expect(c.head_dim != DP, 0) && !piece_live) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) rk[i] = w4{0, 0, 0, 0};
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) *(w4 *)(lds + (k_store + buffer) + i * PASS * DP * 2) = rk[i];
         }
     };
     auto store_v = [&](int32_t t, uint32_t buffer, uint64_t seen) __attribute__((always_inline)) {
+        const int32_t k0 = keys.begin + t * TK;
         if constexpr (E8) {
-            w4 x[N];
-            wide(rv, xv, x);
-            put_v(t, buffer, seen, x);
+            const bool edge = k0 + TK - 1 > all_first || k0 < all_full;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                w4 x = wide(rv[i], xv, i);
+                if (__builtin_expect(c.head_dim != DP || seen != ~0ull, 0))   // what is not there must be finite: its weight is 0
+                    if (!piece_live || !(seen >> (load_row + i * PASS) & 1)) x = w4{0, 0, 0, 0};
+                if (__builtin_expect(edge, 0)) bounded &= T::bound(x);
+                *(w4 *)(lds + (v_store + buffer) + i * PASS * DP * 2) = x;
+                if (DP > 128) __builtin_amdgcn_sched_barrier(0);
+            }
+            return;
         } else {
-            put_v(t, buffer, seen, rv);
+            if (__builtin_expect(c.head_dim != DP || seen != ~0ull, 0)) {
+#pragma unroll
+                for (int i = 0; i < N; ++i)          // what is not there must be finite: its weight is 0
+                    if (!piece_live || !(seen >> (load_row + i * PASS) & 1)) rv[i] = w4{0, 0, 0, 0};
+            }
+            if (__builtin_expect(k0 + TK - 1 > all_first || k0 < all_full, 0)) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) bounded &= T::bound(rv[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) *(w4 *)(lds + (v_store + buffer) + i * PASS * DP * 2) = rv[i];
         }
     };
 
