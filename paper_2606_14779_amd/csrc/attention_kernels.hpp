@@ -350,14 +350,27 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
             for (int w = 0; w < XW; ++w) to[w] = (uint32_t)load4g((const int32_t *)((const char *)cache + at) + w);
         }
     };
-    // row i of what was loaded of 8-bit pages, as 16-bit floats
-    auto wide = [&](w2 from, const uint32_t (&exponents)[XW], int i) __attribute__((always_inline)) {
-        uint32_t word = lane_value(exponents[0], load_row + i * PASS);
-        if constexpr (XW > 1) {
-            const uint32_t other = lane_value(exponents[1], load_row + i * PASS);
-            word = load_piece >= 16 ? other : word;
+    // hands out the rows of what was loaded of 8-bit pages as 16-bit floats: all are widened first, or one after the other
+    // where that does not fit the registers
+    auto each_wide = [&](const auto &from, const uint32_t (&exponents)[XW], auto out) __attribute__((always_inline)) {
+        w4 x[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            uint32_t word = lane_value(exponents[0], load_row + i * PASS);
+            if constexpr (XW > 1) {
+                const uint32_t other = lane_value(exponents[1], load_row + i * PASS);
+                word = load_piece >= 16 ? other : word;
+            }
+            x[i] = widen<T>(from[i], power_of(word, load_piece / 4 % 4 * 8));
+            if constexpr (DP > 128) {
+                out(i, x[i]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
-        return widen<T>(from, power_of(word, load_piece / 4 % 4 * 8));
+        if constexpr (DP <= 128) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) out(i, x[i]);
+        }
     };
     // Rows of 64 elements lie two to 64 banks of LDS, longer ones fill them: the pieces of a row change places with
     // its number, so that 16 rows read at one place of K, and four at four places of V, meet different banks.  PASS
@@ -377,14 +390,10 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
     }
     auto store_k = [&](uint32_t buffer) __attribute__((always_inline)) {
         if constexpr (E8) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                w4 x = wide(rk[i], xk, i);
+            each_wide(rk, xk, [&](int i, w4 x) __attribute__((always_inline)) {
                 if (__builtin_expect(c.head_dim != DP, 0) && !piece_live) x = w4{0, 0, 0, 0};
                 *(w4 *)(lds + (k_store + buffer) + i * PASS * DP * 2) = x;
-                if (DP > 128) __builtin_amdgcn_sched_barrier(0);   // widened all at once they do not fit the registers
-            }
-            return;
+            });
         } else {
             if (__builtin_expect(c.head_dim != DP, 0) && !piece_live) {
 #pragma unroll
@@ -398,16 +407,12 @@ __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attenti
         const int32_t k0 = keys.begin + t * TK;
         if constexpr (E8) {
             const bool edge = k0 + TK - 1 > all_first || k0 < all_full;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                w4 x = wide(rv[i], xv, i);
+            each_wide(rv, xv, [&](int i, w4 x) __attribute__((always_inline)) {
                 if (__builtin_expect(c.head_dim != DP || seen != ~0ull, 0))   // what is not there must be finite: its weight is 0
                     if (!piece_live || !(seen >> (load_row + i * PASS) & 1)) x = w4{0, 0, 0, 0};
                 if (__builtin_expect(edge, 0)) bounded &= T::bound(x);
                 *(w4 *)(lds + (v_store + buffer) + i * PASS * DP * 2) = x;
-                if (DP > 128) __builtin_amdgcn_sched_barrier(0);
-            }
-            return;
+            });
         } else {
             if (__builtin_expect(c.head_dim != DP || seen != ~0ull, 0)) {
 #pragma unroll
