@@ -765,6 +765,10 @@ int kv_evict_workspace(const kvp_cache_shape *shape, const kvp_batch *batch, uin
  * even; at the largest e they stop at 240.  So every element that a call here
  * writes is exact and finite in the shape's dtype, in which it is read.
  * Infinities and NaN become NaN and do not count for max |x|.
+ *
+ * In the calls here total_q may be more than cu_q[n_seq], as for a graph that is
+ * replayed on batches of up to so many tokens: rows of q_out, out and lse
+ * behind the last sequence are left as they are.
  */
 #define KVP_PAGES_16BIT 0u    /* elements of the shape's dtype: [num_slots][num_kv_heads][block_size][head_dim] */
 #define KVP_PAGES_E4M3  1u    /* 8 bits, as above */

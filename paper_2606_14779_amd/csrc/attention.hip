@@ -40,6 +40,7 @@ __global__ __launch_bounds__(256) void attention_join(const AttentionArgs a, con
     const uint32_t slice = group % slices, at = lane * 4;
     const uint32_t row = min(blockIdx.x * (GROUPS / slices) + group / slices, rows - 1);
     const bool live = at < c.head_dim;
+    const int32_t end = load4g(c.cu_q + c.n_seq);
     // a part of a group's own threads at a time: its maximum and sum first, to rescale by
     float m = kLowest, l = 0.0f;
     v4f sum{};
@@ -86,7 +87,7 @@ __global__ __launch_bounds__(256) void attention_join(const AttentionArgs a, con
     }
     const uint32_t head = row % c.heads, token = row / c.heads;
     const RowEnd e = finish_row(m, l, a.sinks, head);
-    if (blockIdx.x * (GROUPS / slices) + group / slices >= rows) return;
+    if (blockIdx.x * (GROUPS / slices) + group / slices >= rows || (int32_t)token >= end) return;
     if (live)
         *(w2 *)(a.out + (uint64_t)token * a.out_stride + (uint64_t)head * c.head_dim + at) =
             w2{T::pack(sum[0] * e.scale_o, sum[1] * e.scale_o), T::pack(sum[2] * e.scale_o, sum[3] * e.scale_o)};

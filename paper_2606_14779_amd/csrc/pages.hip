@@ -221,7 +221,8 @@ __global__ __launch_bounds__(256) void append(const AppendArgs a)
         s = load_seq(c, seq);
     }
     const int32_t i = (int32_t)token - s.q_begin, index = s.kv - s.n_q + i;
-    const bool placed = i >= 0 && i < s.n_q && index >= 0;
+    if (i < 0 || i >= s.n_q) return;                 // behind the last sequence
+    const bool placed = index >= 0;
     const int32_t slot = placed ? load4g(c.table + (uint64_t)seq * c.table_stride + block_of(c, index)) : -1;
     // a position that the table does not have: NaN, so that it shows
     bool known = true;
@@ -265,18 +266,26 @@ __global__ __launch_bounds__(256) void append(const AppendArgs a)
         float x[8];
         if (E8 || !value) unpack8<T>(raw, x);
         if (!value) {
-            float y[8] = {}, up = 1.0f;
-            if constexpr (PAIRS == kInside) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = x[e ^ 1];
-            } else if constexpr (PAIRS == kApart) {
+            float y[8] = {}, up = 1.0f, factor = 1.0f;
+            if constexpr (PAIRS == kApart) {
                 const int other = (int)(lane + (upper ? -half / 8 : half / 8)) & 63;
                 w4 far;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) far[w] = __shfl(raw[w], other);
                 unpack8<T>(far, y);
             }
-            const float factor = a.norm ? norm_factor<T>(a, x, y, lanes, up) : 1.0f;
+            if (a.norm) {                            // before the weight, as their product stays within 32 bits then
+                factor = norm_factor<T>(a, x, y, lanes, up);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[e] *= factor;
+                    if constexpr (PAIRS == kApart) y[e] *= factor;
+                }
+            }
+            if constexpr (PAIRS == kInside) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = x[e ^ 1];
+            }
             if constexpr (PAIRS == kAnyhow) {
                 const uint16_t *from = (query ? q : k) + (uint64_t)(head * c.head_dim), *weight = query ? a.q_weight : a.k_weight;
 #pragma unroll
@@ -285,7 +294,7 @@ __global__ __launch_bounds__(256) void append(const AppendArgs a)
                     if (!asked || at + e >= a.rot) continue;
                     const bool upper = a.interleaved ? e & 1 : at + e >= half;
                     const uint32_t other = a.interleaved ? (at + e) ^ 1 : upper ? at + e - half : at + e + half;
-                    const float y = T::unpack(from[other], 0) * up * (weight ? T::unpack(weight[other], 0) : 1.0f);
+                    const float y = T::unpack(from[other], 0) * up * factor * (weight ? T::unpack(weight[other], 0) : 1.0f);
                     const v2f f = angles[a.interleaved ? (at + e) / 2 : upper ? other : at + e];
                     x[e] = __builtin_fmaf(x[e], f[0], upper ? y * f[1] : -(y * f[1]));
                 }
@@ -295,10 +304,6 @@ __global__ __launch_bounds__(256) void append(const AppendArgs a)
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] *= p[e];
-            }
-            if (a.norm) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] *= factor;
             }
         }
         if constexpr (query) {

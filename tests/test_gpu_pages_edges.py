@@ -130,6 +130,38 @@ def test_lengths_that_are_too_long_are_cut():
     assert left.tolist() == [100, 64]
 
 
+@pytest.mark.parametrize("kind", ["e4m3", "16"])
+@pytest.mark.parametrize("lens", [[(2, 5000), (1, 900)], [(12, 6000), (0, 40), (3, 10)], [(200, 9000), (7, 7)], [(3, 20)]])
+def test_rows_behind_the_last_sequence(kind, lens):
+    """A batch padded to more tokens than its sequences have: the others as without, the rows behind as they were."""
+    c = P.Case(lens, kind, heads=8, kv_heads=2, head_dim=64, seed=len(lens))
+    q = c.normal(c.total + 5, 8, 64)
+    bits, _ = c.tree(1)
+    tail = torch.full((5, bits.shape[1]), -1, dtype=torch.int64, device="cuda")
+    plain, real = c.batch, c.total
+    padded = K.Batch(len(lens), real + 5, c.max_q, c.max_kv, c.cu.data_ptr(), c.kv_len.data_ptr(), c.table_dev.data_ptr(),
+                     c.stride)
+    qkv, positions = c.normal(real + 5, 12, 64), torch.zeros(real + 5, dtype=torch.int32, device="cuda")
+    for tree in (None, bits):
+        c.batch, c.total = plain, real
+        want = P.attention(c, q[:real], 0.125, mask=c.tree(1)[1] if tree is not None else None)
+        c.batch, c.total = padded, real + 5
+        out, lse = T._attend(c, q, 0.125, torch.cat([tree, tail]) if tree is not None else None)
+        T._check((out[:real], lse[:, :real]), want)
+        assert (out[real:] == 7).all() and (lse[:, real:] == 7).all()
+    before = [b.raw.clone() for b in c.buffers]
+    q_out = T._append(c, qkv, T._table(1, 64), 64, positions)
+    assert (q_out[real:] == 3).all() and not (q_out[:real] == 3).all((1, 2)).any()
+    # nothing but the new tokens' rows was written
+    for b, old in zip(c.buffers, before):
+        got = b.raw.clone()
+        b.raw.copy_(old)
+        c.batch, c.total = plain, real
+        T._append(c, qkv[:real], T._table(1, 64), 64, positions[:real])
+        assert torch.equal(got, b.raw)
+        b.raw.copy_(got)
+
+
 # ---- append
 
 @pytest.mark.parametrize("kind", ["e4m3", "16"])
@@ -172,6 +204,21 @@ def test_norms_of_the_smallest_and_largest_heads(rot, interleaved, eps):
     keys = c.buffers[0].rows(*c.places(0, 12))
     want, err = P.turned(qkv[:, 1:2], None, eps, table, positions, [0] * 64, rot, interleaved, True)
     assert T._near(keys, want, err + 2.0 ** -126, "bf16")
+
+
+@pytest.mark.parametrize("rot,interleaved", [(0, False), (128, True), (64, False), (12, False)])
+def test_norms_with_the_smallest_and_largest_weights(rot, interleaved):
+    """Heads of any size times weights from 2^-120 to 2^120: only the product with the normed head has to fit."""
+    c = P.Case([(9, 9)], "16", heads=1, kv_heads=1, head_dim=128, seed=2)
+    x = c.normal(9, 128, to=torch.float64)
+    x = x / x.abs().amax(1, keepdim=True) * P.pow2(torch.tensor([120, 58, 50, 20, 0, -20, -40, -48, -120], device="cuda"))[:, None]
+    qkv = x.to(torch.bfloat16)[:, None].expand(9, 3, 128).contiguous()
+    positions, table = torch.arange(9, dtype=torch.int32, device="cuda")[None], T._table(9, rot)
+    w = (1.5 * P.pow2(torch.arange(128, device="cuda") // 32 * 80 - 120)).to(torch.bfloat16)     # pairs of unlike weights
+    q_out = T._append(c, qkv, table, rot, positions, norm=K.HeadNorm(w.data_ptr(), w.data_ptr(), 0.0), interleaved=interleaved)
+    want, err = P.turned(qkv[:, :1], w, 0.0, table, positions, [0] * 64, rot, interleaved, True)
+    assert T._near(q_out, want, err + 2.0 ** -126, "bf16")
+    assert T._near(c.buffers[0].rows(*c.places(0, 9)), want, err + 2.0 ** -126, "bf16")
 
 
 def test_rows_of_128_elements_with_what_is_no_number():
