@@ -205,9 +205,9 @@ __device__ __forceinline__ bool unbounded_row(const AttentionArgs &a, uint32_t r
 // 512 new tokens over 128K (32 heads, 8 KV heads, 128): 1074 us, 1022 TFLOP/s, where a bf16 matrix product of 16384^3
 // reaches 1370.  Matrix cores busy for 51 % of the cycles, no LDS bank conflicts, 87 % of the L2 reads hit; the clock
 // falls to about 2.0 GHz of 2.4 under it.  Without turns (four waves, two such workgroups to a CU) 1218 us.
-// The same over 8-bit pages: 1080 us on a card where 16-bit ones take 1050 to 1090: a sixth more vector instructions, for
-// widening what a lane has loaded, and half the bytes.  64 drafts over 128K (32, 4, 128) in 8 bits: 163 us with the join,
-// 840 TFLOP/s, 67 tiles to each of 248 workgroups.  Two tiles ahead instead of one: 2 % more for 8-bit pages, 1 % less for
+// The same over 8-bit pages: 1055 to 1097 us by card where 16-bit ones take 1050 to 1090: an eighth more vector
+// instructions, for widening what a lane has loaded, and half the bytes.  64 drafts over 128K (32, 4, 128) in 8 bits: 163 to
+// 172 us with the join, 800 to 840 TFLOP/s, 67 tiles to each of 248 workgroups.  Two tiles ahead instead of one: 2 % more for 8-bit pages, 1 % less for
 // 16-bit ones.
 template <class T, int DP, class Offset, int KIND = kCausal16>
 __global__ __launch_bounds__(row_waves(DP) * 64, row_waves(DP) / 4) void attention_rows(const AttentionArgs a)

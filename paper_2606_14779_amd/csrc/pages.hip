@@ -10,7 +10,7 @@
 // elements are exchanges within a wave.  Queries, keys and values are read once and written once.
 //
 // Bound by memory and by what a token has to wait for: packed prompts of 12.7K tokens (64 heads, 8 KV heads, 64; norms, three
-// axes, pairs interleaved, 16-bit pages) 55.5 us, 263 MB at 4.7 TB/s, vector unit busy for 57 % of the cycles.  With every
+// axes, pairs interleaved, 16-bit pages) 55.5 to 59.5 us by card, 263 MB at 4.7 TB/s, vector unit busy for 57 % of the cycles.  With every
 // head's weights and angles worked out anew 73; with the token's positions, sequence and slot asked for one after the other
 // 65.  A decoding step of 32 tokens takes 6.5 us on the GPU.
 

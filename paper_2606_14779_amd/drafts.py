@@ -154,7 +154,8 @@ def main() -> None:
     one = torch.ones((shape.layers, shape.head_dim), dtype=torch.bfloat16, device="cuda")
 
     for kind, block in (("16", 16), ("e4m3", 64)):      # slots of 16 and 33 KB
-        run = DraftRun(dataclasses.replace(shape, block_size=block), heads, contexts, room=512, pages=kind, norm=(one, one, 1e-6), rope=dict(base=1000000.0))
+        run = DraftRun(dataclasses.replace(shape, block_size=block), heads, contexts, room=512, pages=kind,
+                       norm=(one, one, 1e-6), rope=dict(base=1000000.0))
 
         def timed(what, f):
             torch.cuda.synchronize()
