@@ -837,7 +837,10 @@ int kv_convert_pages(const kvp_cache_shape *shape, const kvp_batch *batch, const
  *                are not looked at.  It sees all tokens cached before the new ones.  8-byte aligned.
  *   tree_words   at least ceil(max_q / 64), at most 2^20; 0 without a tree.
  *   window       with a tree, a token that sees d new tokens stands d - 1 places behind the first: it sees the tokens
- *                cached before the new ones at j > kv_len - n_q + d - 1 - window, and new ones by its mask alone.
+ *                cached before the new ones at j > kv_len - n_q + d - 1 - window, and new ones by its mask alone.  So
+ *                for a window that reaches over the drafts too the caller leaves out of a token's mask the ancestors
+ *                `window` or more places above it: `window` of them are left, itself included, which hide what is
+ *                cached before the new tokens.
  * A token that sees nothing gets 0 and an lse of -inf (or that of its sink).
  */
 int kv_attention_pages(const kvp_cache_shape *shape, const kvp_batch *batch, const kvp_pages *pages, const uint64_t *tree,

@@ -3,8 +3,8 @@
 A ``DraftRun`` is a ``ServeRun`` whose engine cache is 8-bit pages (or 16-bit ones): the pool moves half the bytes.  A
 step's new tokens go layer by layer through ``kv_norm_rope_append`` (queries and keys normed where the model does so,
 turned, and written to the pages) and ``kv_attention_pages``.  New tokens may be drafts that form a tree: each sees the
-context and its own ancestors, and after the caller has checked them, ``commit`` keeps a path of each tree
-(``kv_tree_commit``) and the others are gone.  ``python -m paper_2606_14779_amd.drafts`` runs that and prints what each
+context and its own ancestors, as far as a window lets it, and after the caller has checked them, ``commit`` keeps a path
+of each tree (``kv_tree_commit``) and the others are gone.  ``python -m paper_2606_14779_amd.drafts`` runs that and prints what each
 part took.
 """
 from __future__ import annotations
@@ -27,6 +27,19 @@ def tree_mask(parents) -> np.ndarray:
             sees[i] = sees[p]
         sees[i, i] = True
     return np.packbits(sees, axis=1, bitorder="little").view(np.int64)
+
+
+def _within(bits, depth, window: int):
+    """What the drafts of one sequence see under a window: of a mask [drafts][bits], whose draft i stands depth[i] places
+    behind the first, the ones less than `window` places before a draft.  ``kv_attention_pages`` finds a draft's place in
+    the window by how many drafts it sees: all before it that are near enough to hide what is cached must be there."""
+    n = len(depth)
+    near = bits.copy()
+    near[:, :n] &= (depth[:, None] - depth[None, :] < window).astype(bits.dtype)
+    count = near[:, :n].sum(1, dtype=np.int64)
+    if (count < np.minimum(depth + 1, window)).any():
+        raise ValueError("a draft that does not see the %d drafts before it that a window leaves" % (window - 1))
+    return near
 
 
 class DraftRun(ServeRun):
@@ -80,7 +93,8 @@ class DraftRun(ServeRun):
 
     def begin(self, new, tree=None) -> None:
         """A step of new[i] tokens of sequence i; tree: None, or the rows of ``tree_mask`` of all sequences, one after the
-        other, all of the same number of words."""
+        other, all of the same number of words.  A draft's place behind the cached tokens is the number of drafts before it
+        that its row has; under a window it sees none of those that are `window` or more places before it."""
         self._settled()
         new, seen = np.asarray(new, np.int64), self.seen
         if tree is not None:
@@ -91,6 +105,9 @@ class DraftRun(ServeRun):
             depth = [bits[a:a + n, :n].sum(1, dtype=np.int64) - 1 for a, n in zip(np.cumsum(new) - new, new)]
             if any((d < 0).any() for d in depth):
                 raise ValueError("a draft that sees no draft, not even itself")
+            if self.window:
+                near = [_within(bits[a:a + n], d, self.window) for a, n, d in zip(np.cumsum(new) - new, new, depth)]
+                tree = np.packbits(np.concatenate(near), axis=1, bitorder="little").view(np.int64)
         super().begin(new)
         self.tree = None
         if tree is not None:

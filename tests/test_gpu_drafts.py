@@ -134,3 +134,32 @@ def test_what_a_run_refuses():
     with pytest.raises(ValueError):
         _filled("e4m3", norm=(torch.ones(2, 32, device="cuda").bfloat16(),) * 2 + (1e-6,))
     run.close()
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "16"])
+@pytest.mark.parametrize("window", [1, 4, 70])
+def test_drafts_under_a_window(kind, window):
+    """Every draft has the output that it and its ancestors would have as plain tokens under the window, tolerance as
+    above."""
+    trees = [[-1, 0, 1, 2, 3, 4, 5, 6, 7, 8, 2, 10, 11, 12, 13], list(range(-1, 9))]
+    new = [len(p) for p in trees]
+    drafted, g = _filled(kind, window=window)
+    qkv = _qkv(g, sum(new))[0]
+    drafted.begin(new, np.concatenate([tree_mask(p) for p in trees]))
+    out = drafted.layer(0, qkv)
+    for ends in ([9, 9], [14, 4]):
+        rows = []
+        for p, at, first in zip(trees, ends, (0, new[0])):
+            path = []
+            while at >= 0:
+                path.append(first + at)
+                at = p[at]
+            rows.append(path[::-1])
+        plain, _ = _filled(kind, window=window)
+        plain.begin([len(r) for r in rows])
+        rows = torch.tensor(sum(rows, []), device="cuda")
+        want = plain.layer(0, qkv[rows].contiguous())
+        most = max(_rows(plain, 0, 1, s, n).abs().max().item() for s, n in enumerate(plain.lens))
+        assert (out[rows].double() - want.double()).abs().max().item() <= 2 * (2 ** -7 + 2 ** -12) * most
+        plain.close()
+    drafted.close()
