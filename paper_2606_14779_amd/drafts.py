@@ -102,7 +102,8 @@ class DraftRun(ServeRun):
             if tree.ndim != 2 or tree.shape[0] != new.sum() or tree.shape[1] * 64 < new.max(initial=0):
                 raise ValueError("tree is not [new tokens][words]")
             bits = np.unpackbits(tree.view(np.uint8), axis=1, bitorder="little")
-            depth = [bits[a:a + n, :n].sum(1, dtype=np.int64) - 1 for a, n in zip(np.cumsum(new) - new, new)]
+            sees = [bits[a:a + n, :n].astype(bool) for a, n in zip(np.cumsum(new) - new, new)]
+            depth = [x.sum(1, dtype=np.int64) - 1 for x in sees]
             if any((d < 0).any() for d in depth):
                 raise ValueError("a draft that sees no draft, not even itself")
             if self.window:
@@ -113,6 +114,7 @@ class DraftRun(ServeRun):
         if tree is not None:
             self.positions = self._dev(np.concatenate([s + d for s, d in zip(seen, depth)]))
             self.tree, self.drafted, self.seen = self._dev(tree, np.int64), new, seen
+            self._sees = sees                           # which drafts of its sequence each one follows
 
     def layer(self, index: int, qkv, mass_from: int = 0):
         """Attention output of a layer; qkv as in ``ServeRun.layer``."""
@@ -136,15 +138,19 @@ class DraftRun(ServeRun):
         return out
 
     def commit(self, paths) -> None:
-        """paths[i]: the accepted drafts of sequence i, ascending as a path down its tree is."""
+        """paths[i]: the accepted drafts of sequence i, ascending as a path down its tree is: each of them sees those before
+        it, and none that is not accepted."""
         if self.drafted is None:
             raise ValueError("no drafted tokens")
         paths = [np.asarray(p, np.int64).reshape(-1) for p in paths]
         if len(paths) != self.n:
             raise ValueError("one path per sequence")
-        for p, n in zip(paths, self.drafted):
+        for p, n, sees in zip(paths, self.drafted, self._sees):
             if len(p) and (p[0] < 0 or p[-1] >= n or (np.diff(p) <= 0).any()):
                 raise ValueError("a path is not ascending among its sequence's %d drafts" % n)
+            # one left out, or one of another branch, would leave positions with holes and outputs of other contexts
+            if np.delete(sees[p], p, axis=1).any() or not sees[np.ix_(p, p)][np.tril_indices(len(p))].all():
+                raise ValueError("drafts %s are no path of their sequence's tree from its first on" % p.tolist())
         path = np.zeros(max(self.total, 1), np.int32)
         for a, p in zip(np.cumsum(self.drafted) - self.drafted, paths):
             path[a:a + len(p)] = p

@@ -96,3 +96,52 @@ def test_masks_that_a_window_cannot_place(make):
     both[5, 5] = True
     run.begin([6, 0], np.packbits(both, axis=1, bitorder="little").view(np.int64))
     assert (_bits(run.tree, 6) == both[:, :6]).all() and run.positions.tolist() == [34] * 5 + [35]
+
+
+# ---- what is committed is a path
+
+def test_only_paths_are_committed(make):
+    """One left out would leave a hole in the positions, one of another branch a token that followed others."""
+    #            0
+    #        1       2
+    #      3   4     5
+    #          6
+    parents = [-1, 0, 0, 1, 1, 2, 4]
+    for window in (0, 2):
+        for bad in ([1], [0, 3], [0, 1, 2], [0, 1, 3, 4], [0, 1, 6], [0, 4, 6], [6], [0, 1, 5], [0, 2, 6]):
+            run, called = make(window)
+            run.begin([7, 1], np.concatenate([tree_mask(parents), tree_mask([-1])]))
+            with pytest.raises(ValueError, match="path"):
+                run.commit([bad, [0]])
+            assert not called and run.drafted.tolist() == [7, 1] and run.lens.tolist() == [37, 8]
+        for good in ([], [0], [0, 1], [0, 2, 5], [0, 1, 4, 6]):
+            run, called = make(window)
+            run.begin([7, 1], np.concatenate([tree_mask(parents), tree_mask([-1])]))
+            run.commit([good, []])
+            assert [c[0] for c in called] == ["tree_commit"] and run.lens.tolist() == [30 + len(good), 7]
+
+
+def test_two_trees_of_one_sequence(make):
+    """Drafts without a parent: each begins a path of its own."""
+    for bad in ([0, 1], [1, 2], [0, 3], [0, 1, 2, 3]):
+        run, _ = make()
+        run.begin([4, 0], tree_mask([-1, -1, 0, 1]))
+        with pytest.raises(ValueError, match="path"):
+            run.commit([bad, []])
+    for good in ([0, 2], [1, 3], [1]):
+        run, _ = make()
+        run.begin([4, 0], tree_mask([-1, -1, 0, 1]))
+        run.commit([good, []])
+        assert run.seen.tolist() == [30 + len(good), 7]
+
+
+def test_drafts_that_see_each_other_are_committed_together(make):
+    both = np.zeros((6, 64), bool)
+    both[:, :5] = True
+    both[5, 5] = True
+    rows = np.packbits(both, axis=1, bitorder="little").view(np.int64)
+    for paths, ok in (([0, 1], False), ([0, 1, 2, 3, 4], True), ([5], False), ([0, 1, 2, 3, 4, 5], True)):
+        run, _ = make()
+        run.begin([6, 0], rows)
+        with contextlib.nullcontext() if ok else pytest.raises(ValueError, match="path"):
+            run.commit([paths, []])
