@@ -54,6 +54,7 @@ class DraftRun(ServeRun):
     def __init__(self, shape, q_heads: int, contexts, room: int, dtype: str = "bf16", pages: str = "e4m3", norm=None, **kw):
         self.kind = pages
         self.drafted = None                             # new tokens of every sequence that wait for commit
+        self.batch = None                               # of the step that layers are run for
         super().__init__(shape, q_heads, contexts, room, dtype, **kw)
         self.pages = [K.Pages(pages, k, v) for k, v in zip(self.k_ptrs, self.v_ptrs)]
         self.norm = None
@@ -120,6 +121,8 @@ class DraftRun(ServeRun):
         """Attention output of a layer; qkv as in ``ServeRun.layer``."""
         if mass_from:
             raise ValueError("attention mass is not collected here")
+        if self.batch is None:
+            raise ValueError("no step has begun")
         return super().layer(index, qkv)
 
     def _layer(self, index: int, qkv, mass_from: int):
@@ -163,6 +166,7 @@ class DraftRun(ServeRun):
         self.lens = (self.lens - self.drafted + count).astype(np.int32)
         self.seen = self.seen + count
         self.kv_len, self.drafted = left, None
+        self.batch = None                               # whose lengths were those before
 
 
 def main() -> None:

@@ -145,3 +145,24 @@ def test_drafts_that_see_each_other_are_committed_together(make):
         run.begin([6, 0], rows)
         with contextlib.nullcontext() if ok else pytest.raises(ValueError, match="path"):
             run.commit([paths, []])
+
+
+# ---- steps
+
+def _qkv(run):
+    return torch.zeros(run.total, 12, 64, dtype=torch.bfloat16)
+
+
+def test_no_layers_between_commit_and_the_next_step(make):
+    """The batch of the step before has lengths that are no longer those of the cache, in memory that may be others'."""
+    run, called = make()
+    run.begin([2, 1], np.concatenate([tree_mask([-1, 0]), tree_mask([-1])]))
+    run.layer(0, _qkv(run))
+    run.commit([[0], [0]])
+    del called[:]
+    with pytest.raises(ValueError, match="step"):
+        run.layer(0, _qkv(run))
+    assert not called
+    run.begin([1, 1])
+    run.layer(0, _qkv(run))
+    assert [c[0] for c in called] == ["norm_rope_append", "attention_pages"]
