@@ -132,11 +132,12 @@ class DraftRun(ServeRun):
                            self.positions.data_ptr(), at + h * d * 2, row, at + (h + hk) * d * 2, row,
                            norm=self.norm[index] if self.norm else None, q=at, q_stride=row, q_out=self.q.data_ptr(),
                            q_out_stride=h * d, pos=self.pos[index].data_ptr(), pos_stride=self.max_kv, stream=stream)
+        tree = self.tree if self.total else None        # a step without tokens has no rows to point to
         out = self.torch.empty_like(self.q)
         need = K.attention_pages_workspace(self.cache_shape, self.batch)
         K.attention_pages(self.cache_shape, self.batch, self.pages[index], self.q.data_ptr(), h * d, d ** -0.5,
-                          out.data_ptr(), h * d, tree=self.tree.data_ptr() if self.tree is not None else 0,
-                          tree_words=self.tree.shape[1] if self.tree is not None else 0, window=self.window,
+                          out.data_ptr(), h * d, tree=tree.data_ptr() if tree is not None else 0,
+                          tree_words=tree.shape[1] if tree is not None else 0, window=self.window,
                           lse=self.lse.data_ptr(), workspace=self._workspace(need), workspace_bytes=need, stream=stream)
         return out
 

@@ -166,3 +166,14 @@ def test_no_layers_between_commit_and_the_next_step(make):
     run.begin([1, 1])
     run.layer(0, _qkv(run))
     assert [c[0] for c in called] == ["norm_rope_append", "attention_pages"]
+
+
+def test_a_drafted_step_without_tokens(make):
+    """A mask of no rows has no address: no mask, as words of none are refused."""
+    for window in (0, 4):
+        run, called = make(window)
+        run.begin([0, 0], np.zeros((0, 1), np.int64))
+        run.layer(0, _qkv(run))
+        assert (called[-1][2]["tree"], called[-1][2]["tree_words"]) == (0, 0)
+        run.commit([[], []])
+        assert run.lens.tolist() == SEEN

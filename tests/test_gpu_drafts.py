@@ -163,3 +163,19 @@ def test_drafts_under_a_window(kind, window):
         assert (out[rows].double() - want.double()).abs().max().item() <= 2 * (2 ** -7 + 2 ** -12) * most
         plain.close()
     drafted.close()
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "16"])
+def test_steps_without_tokens(kind):
+    """A drafted step in which no sequence has a draft, and one in which only one has: the other stays as it is."""
+    run, g = _filled(kind)
+    run.begin([0, 0], tree_mask([]))
+    assert run.layer(0, _qkv(g, 0)[0]).shape == (0, HEADS, 64)
+    run.commit([[], []])
+    before = _rows(run, 0, 0, 0, CONTEXTS[0])
+    run.begin([0, 3], tree_mask([-1, 0, 0]))
+    assert torch.isfinite(run.layer(0, _qkv(g, 3)[0])).all()
+    run.commit([[], [0, 2]])
+    assert run.lens.tolist() == [CONTEXTS[0], CONTEXTS[1] + 2] == run.kv_len.tolist()
+    assert torch.equal(before, _rows(run, 0, 0, 0, CONTEXTS[0]))
+    run.close()
