@@ -144,14 +144,31 @@ Cut cut_of(const CacheView &c, uint32_t window, const CutRule &rule)
         // The fewest parts that keep 19 of 20 CUs busy, of 512 keys or more: parts are written and read again, and a
         // workgroup takes some us to begin.  512 new tokens over 128K: 1064 us at 4 parts (256 workgroups), 1096 at 16,
         // 1293 at 64.
-        const uint64_t most = std::min(1024 / units, span / 512);
-        uint64_t best = 1, filled = 0;               // of 1000
-        for (uint64_t n = 1; n <= most && filled < 950; ++n) {
-            const uint64_t f = units * n * 1000 / ((units * n + 255) / 256 * 256);
-            if (f > filled) best = n, filled = f;
+        auto fewest = [&](uint64_t units, uint64_t most) {
+            uint64_t best = 1, filled = 0;           // of 1000
+            for (uint64_t n = 1; n <= most && filled < 950; ++n) {
+                const uint64_t f = units * n * 1000 / ((units * n + 255) / 256 * 256);
+                if (f > filled) best = n, filled = f;
+            }
+            return best;
+        };
+        auto most_of = [&](uint64_t units) { return std::min(1024 / units, span / 512); };
+        uint64_t best = fewest(units, most_of(units));
+        if (c.n_seq > 1 && c.n_seq <= 64 && !window) {
+            // Tiles that fill the chip stay whole: a join and more workgroups cost more than they give, whether lengths
+            // differ or not.  32 x 8 new tokens over 1K (32 heads, 8 KV heads, 128) 43 us, 53 in up to two parts; over up to
+            // 4K 117 and 125; 16 x 96 over 1K 48 and 64, over up to 16K 441 and 453.
+            if (best > 1)                            // a batch of different lengths may want more, which its workgroups find
+                best = std::min(2 * best, most_of(units));
+            else if (c.total_q < 2 * (uint64_t)c.max_q && span >= 16384) {
+                // A chunk among single tokens has more tiles than counted, of which a few would be left for a round of
+                // their own.  31 single tokens and 512 new ones over 16K: 885 us whole, 761 in parts; where the single ones
+                // are over 2K to 16K 504 and 520, and over 1K 75 and 84.
+                const uint64_t chunk = ((uint64_t)c.max_q * c.group + tile_rows - 1) / tile_rows;
+                const uint64_t all = (chunk + c.n_seq - 1) * c.kv_heads;
+                if (all < 512) best = fewest(all, most_of(all));
+            }
         }
-        // a batch of different lengths may want more, which its workgroups find out
-        if (c.n_seq > 1 && c.n_seq <= 64 && !window) best = std::min(2 * best, std::max<uint64_t>(1, most));
         keys = (span + best - 1) / best;
     }
     // no more parts than without a window: the workspace is asked for without one

@@ -159,3 +159,21 @@ def test_workspaces():
         part = total * 8 * (64 + 2) * 4
         assert n % part == 0 and n // part <= 1024 and (n // part) * 128 <= max(kv, 128) + 127
     assert K.evict_workspace(_shape(), _batch()) >= 2 * 2 * 640 // 2 * 8
+
+
+@pytest.mark.parametrize("n,new,heads,kv_heads,d", [(32, 8, 32, 8, 128), (63, 8, 32, 8, 128), (64, 8, 32, 4, 128),
+                                                    (2, 992, 32, 8, 128), (16, 96, 32, 8, 128), (32, 8, 32, 8, 256)])
+def test_tiles_that_fill_the_chip_stay_whole(n, new, heads, kv_heads, d):
+    """256 or 504 workgroups, whose rows are written as they are: no parts, so no workspace."""
+    shape = _shape(heads=heads, kv_heads=kv_heads, head_dim=d, slots=1 << 20)
+    for kv in (1024, 2048, 4096, 16384, 131072):
+        b = _batch(n_seq=n, total=n * new, max_q=new, max_kv=kv, stride=8192)
+        assert K.attention_workspace(shape, b) == 0
+
+
+def test_a_chunk_among_single_tokens_is_cut():
+    """31 single tokens and a chunk of 512: 39 tiles of rows to a KV head, where the rows of 32 even sequences make 32."""
+    shape = _shape(heads=32, kv_heads=8, head_dim=128, slots=1 << 20)
+    part = 543 * 32 * 130 * 4
+    for kv, parts in ((1024, 0), (8192, 0), (16384, 3), (131072, 3)):
+        assert K.attention_workspace(shape, _batch(n_seq=32, total=543, max_q=512, max_kv=kv, stride=8192)) == parts * part
