@@ -111,7 +111,7 @@ struct Cut {
 // than a 16-row product holds, to attention_some up to 64 (32) by the rule of calls that it is for, else to tiles of
 // 256 (128 at a head_dim of more than 128).  Where the tiles do not
 // fill the chip, the keys are split, as far as a part holds enough keys to be worth its output's way through memory.
-Cut cut_of(const CacheView &c, uint32_t window, const CutRule &rule)
+Cut cut_of(const CacheView &c, uint32_t window, const CutRule &rule, bool tree = false)
 {
     Cut p{};
     const uint64_t rows = (uint64_t)c.total_q * c.group;
@@ -122,7 +122,8 @@ Cut cut_of(const CacheView &c, uint32_t window, const CutRule &rule)
     p.tiles = few            ? c.n_seq
               : c.n_seq == 1 ? (uint32_t)((rows + tile_rows - 1) / tile_rows)
                              : (uint32_t)(rows / tile_rows + c.n_seq);
-    const uint64_t tile_tokens = few ? c.max_q : std::min<uint64_t>(c.max_q, tile_rows / c.group + 2);
+    // new tokens whose keys a workgroup goes over: those of its rows, or with a mask among them all
+    const uint64_t tile_tokens = few || tree ? c.max_q : std::min<uint64_t>(c.max_q, tile_rows / c.group + 2);
     uint64_t span = c.max_kv;
     if (window) span = std::min<uint64_t>(span, (uint64_t)window + tile_tokens + kTileKeys);
     // workgroups that have work: a sequence's last tile is half full, if it has another one
@@ -186,7 +187,10 @@ Cut attention_cut(const CacheView &c, uint32_t window) { return cut_of(c, window
 
 // Half as many parts: they move half the bytes of 8-bit pages, or join the outputs of more rows.  One token over 128K in 8
 // bits (32 heads, 8 KV heads, 128) 58.0 us, 62.0 at 1024 parts; trees of 8 and of 16 tokens over 128K 63 and 92, 72 and 106.
-Cut pages_cut(const CacheView &c, uint32_t window) { return cut_of(c, window, {some_rows(c.head_dim), 512}); }
+Cut pages_cut(const CacheView &c, uint32_t window, bool tree = false)
+{
+    return cut_of(c, window, {some_rows(c.head_dim), 512}, tree);
+}
 
 uint32_t row_exponents(uint32_t head_dim) { return (head_dim + 127) / 128 * 4; }
 
@@ -328,7 +332,7 @@ void op_attention_pages(const kvp_cache_shape *s, const kvp_batch *b, const kvp_
     if (a.c.total_q == 0) return;
     const bool eight = pages->kind == KVP_PAGES_E4M3;
     // 16-bit pages under a causal mask are kv_attention's
-    const Cut cut = eight || tree ? pages_cut(a.c, window) : attention_cut(a.c, window);
+    const Cut cut = eight || tree ? pages_cut(a.c, window, tree) : attention_cut(a.c, window);
     fill_attention(a, q, q_stride, p.k, p.v, scale, window, sinks, out, out_stride, lse, cut, workspace, workspace_bytes,
                    "workspace is smaller than kv_attention_pages_workspace says");
     a.exponents = p.exponents;

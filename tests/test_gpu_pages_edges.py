@@ -270,3 +270,13 @@ def test_convert_many_sequences():
             slot, off = c.places(s, kv)
             for source, out in zip(c.buffers, to):
                 assert torch.equal(out.rows(slot, off), source.rows(slot, off))
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "16"])
+@pytest.mark.parametrize("window", [1, 128, 1000])
+def test_a_large_windowed_tree(kind, window):
+    """Row tiles that all go over the window and every draft, in parts."""
+    c = P.Case([(1500, 4000)], kind, heads=4, kv_heads=1, head_dim=128, seed=window)
+    q = c.normal(c.total, 4, 128, std=2.0)
+    bits, mask = c.tree(window)
+    T._check(T._attend(c, q, 128 ** -0.5, bits, window), P.attention(c, q, 128 ** -0.5, window, mask=mask))

@@ -180,3 +180,15 @@ def test_workspaces():
         part = total * 8 * (64 + 2) * 4
         assert n >= K.attention_workspace(_shape(), b)
         assert n % part == 0 and n // part <= 1024 and (n // part) * 128 <= max(kv, 128) + 127
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "16"])
+def test_a_large_windowed_tree_is_cut_by_all_its_drafts(kind):
+    """Every row tile goes over the window and all of 2048 drafts, whatever its own rows are: 64 workgroups of 2200 keys
+    are cut, and that needs a workspace."""
+    shape, batch = _shape(heads=8, kv_heads=1, head_dim=128, slots=1 << 16), _batch(n_seq=1, total=2048, max_q=2048,
+                                                                                      max_kv=8192, stride=512)
+    tree = dict(shape=shape, batch=batch, pages=_pages(kind), q_stride=1024, out_stride=1024, tree=P, tree_words=32, window=128)
+    assert "workspace" in _refused(_attend, **tree, workspace=0)
+    need = K.attention_pages_workspace(shape, batch)
+    assert "workspace" in _refused(_attend, **tree, workspace_bytes=need // 8)
