@@ -729,13 +729,13 @@ __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2
 #pragma unroll
                 for (int i = 0; i < KS / 2; ++i) {
                     const uint32_t at = 64 * i + 16 * quad;
-                    const uint16_t *from = (const uint16_t *)(p + (at < c.head_dim ? at : 0));   // past the end: q is 0 there
-                    rk[b][i] = KS > 2 ? load16g(from) : stream16g(from);
+                    const uint8_t *from = p + (at < c.head_dim ? at : 0);   // past the end: q is 0 there
+                    rk[b][i] = KS > 2 ? load16g_by8(from) : stream16g_by8(from);
                 }
             }
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                rv[i] = stream16g((const uint16_t *)((const uint8_t *)a.v + lane_value(at_row, load_row + i * PASS) + piece_at));
+                rv[i] = stream16g_by8((const uint8_t *)a.v + lane_value(at_row, load_row + i * PASS) + piece_at);
             return ok;
         }
 #pragma unroll
@@ -1107,12 +1107,17 @@ __global__ __launch_bounds__(kFewWaves * RG * 64, DP > 128 ? 1 : 2) void attenti
 #pragma unroll
         for (int i = 0; i < KS * 8 / EL; ++i) {
             const uint32_t at = E8 ? 32u * i + 16 * half : 16u * i + 8 * half;
-            rk[i] = load16g((const uint16_t *)(p + (at < c.head_dim ? at : 0) * (E8 ? 1 : 2)));   // past the end: q is 0 there
+            const uint8_t *from = p + (at < c.head_dim ? at : 0) * (E8 ? 1 : 2);   // past the end: q is 0 there
+            rk[i] = E8 ? load16g_by8(from) : load16g((const uint16_t *)from);
         }
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            rv[i] = (RG > 1 ? load16g : stream16g)(   // two waves' keys: the second's come from a cache
-                (const uint16_t *)((const uint8_t *)a.v + lane_value(at_row, load_row + i * PASS) + piece_at * (E8 ? 1 : 2)));
+        for (int i = 0; i < N; ++i) {                // two waves' keys: the second's come from a cache
+            const uint8_t *from = (const uint8_t *)a.v + lane_value(at_row, load_row + i * PASS) + piece_at * (E8 ? 1 : 2);
+            if constexpr (E8)
+                rv[i] = RG > 1 ? load16g_by8(from) : stream16g_by8(from);
+            else
+                rv[i] = RG > 1 ? load16g((const uint16_t *)from) : stream16g((const uint16_t *)from);
+        }
     };
     char *vs = lds + place * (TK * DP * 2);
     auto v_place = [&](int r) __attribute__((always_inline)) { return DP >= 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2; };

@@ -102,6 +102,14 @@ struct F16 {
 __device__ __forceinline__ w4 load16g(const uint16_t *p) { return *(gw4 *)p; }
 // The same past the caches, for what is read once: a line has to be one load's, or it is fetched again.
 __device__ __forceinline__ w4 stream16g(const uint16_t *p) { return __builtin_nontemporal_load((gw4 *)p); }
+// Both from an address that is a multiple of 8 alone: 16 elements of a row of 8-bit pages, whose rows begin at multiples of
+// head_dim bytes.  One load as well, as the hardware asks for multiples of 4.  Where head_dim is no multiple of 16 a row's
+// last load reads 8 bytes past it: another row or exponents, and past a slot's last row there are 4 bytes of exponents at
+// least and what rounds the slot up to 16, so that these 8 bytes are the slot's.
+typedef uint32_t w4_by8 __attribute__((ext_vector_type(4), aligned(8)));
+typedef __attribute__((address_space(1))) const w4_by8 gw4_by8;
+__device__ __forceinline__ w4 load16g_by8(const uint8_t *p) { return *(gw4_by8 *)p; }
+__device__ __forceinline__ w4 stream16g_by8(const uint8_t *p) { return __builtin_nontemporal_load((gw4_by8 *)p); }
 __device__ __forceinline__ w2 load8g(const uint16_t *p) { return *(__attribute__((address_space(1))) const w2 *)p; }
 __device__ __forceinline__ int32_t load4g(const int32_t *p) { return *(gi32 *)p; }
 

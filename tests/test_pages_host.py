@@ -192,3 +192,11 @@ def test_a_large_windowed_tree_is_cut_by_all_its_drafts(kind):
     assert "workspace" in _refused(_attend, **tree, workspace=0)
     need = K.attention_pages_workspace(shape, batch)
     assert "workspace" in _refused(_attend, **tree, workspace_bytes=need // 8)
+
+
+def test_loads_of_16_elements_stay_in_a_slot():
+    """Rows of 8-bit pages are read 16 elements at a time, the last ones of a head of 8 n elements with 8 bytes past it."""
+    for d in range(8, 264, 8):
+        for rows in range(1, 40):
+            shape = _shape(heads=1, kv_heads=1, head_dim=d, block=rows)
+            assert (rows - 1) * d + (d + 15) // 16 * 16 <= K.page_bytes(shape, "e4m3")
