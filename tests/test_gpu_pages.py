@@ -522,6 +522,39 @@ def test_convert(back, shape, dtype):
                        want[0].rows(*(torch.tensor([x], device="cuda") for x in (int(table[1, 0]), 0))))
 
 
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("before", [False, True])
+@pytest.mark.parametrize("shape", [(2, 64, 16), (3, 80, 8), (1, 136, 130)], ids=str)
+def test_convert_without_a_first_token(back, before, shape):
+    """All cached tokens of all sequences and nothing else, into buffers as they were, or after a call that left out the
+    first ones."""
+    hk, d, block = shape
+    lens = [(0, 90), (0, 1), (0, 300), (0, 0), (0, 64)]
+    a, b = ("e4m3", "16") if back else ("16", "e4m3")
+    c = P.Case(lens, a, heads=hk, kv_heads=hk, head_dim=d, block=block, seed=d)
+    slots = c.slots + 5
+    table = np.full((len(lens), c.stride), -1, np.int32)
+    order = torch.randperm(slots, generator=torch.Generator().manual_seed(2)).tolist()
+    for s, (_, kv) in enumerate(lens):
+        n = -(-kv // block)
+        table[s, :n] = [order.pop() for _ in range(n)]
+    to, want = ([P.Buffer(b, slots, hk, block, d, "bf16") for _ in range(2)] for _ in range(2))
+    pages = K.Pages(b, *(x.raw.data_ptr() for x in to))
+    table_dev, first = _dev(table.tolist()), _dev([7, 1, 299, 0, 200])
+    if before:
+        K.convert_pages(c.shape, c.batch, c.pages, pages, table_dev.data_ptr(), table.shape[1], slots, first=first.data_ptr(),
+                        stream=_stream())
+    K.convert_pages(c.shape, c.batch, c.pages, pages, table_dev.data_ptr(), table.shape[1], slots, stream=_stream())
+    for s, (_, kv) in enumerate(lens):
+        if kv:
+            slot, off = c.places(s, kv)
+            dest = torch.from_numpy(np.repeat(table[s], block)[:kv].astype(np.int64)).cuda()
+            for source, out in zip(c.buffers, want):
+                out.put(dest, off, source.rows(slot, off))
+    for got, w in zip(to, want):
+        assert torch.equal(got.raw, w.raw)
+
+
 def test_there_and_back_again():
     """8 bits to 16 and back to 8 gives the same bits: what was written is what is read."""
     for dtype in ("bf16", "f16"):
