@@ -124,7 +124,9 @@ __device__ __forceinline__ uint32_t lowest_of(uint32_t x)
 __device__ __forceinline__ uint32_t longest_of(uint32_t x) { return ~lowest_of(~x); }
 // Workgroups of row tiles, one to a CU: of 1 to 64 parts to the longest sequence that number for which the rounds of the chip,
 // each as long as a part's tiles of keys (2.1 us each at head_dim 128) and about five more to begin and end, take least.
-// Trees of 32 x 16 over up to 8K (32, 8, 128): 125 us by sizes alone, 90 so; of 64 x 4 over 32K (32, 4, 128) 217 and 174.
+// Trees of 16 x 32 over up to 8K (32, 8, 128): 123 us by sizes alone, 94 so; of 64 x 4 over 32K (32, 4, 128) 220 and 175.
+// Where max_kv is far above the lengths, as in a graph for all of them (2 x 8 tokens over 4K, max_kv 128K), 116 and 28; where
+// it is not and all parts run at once, 1 to 2 us more.
 __device__ __forceinline__ uint32_t keys_of_rounds(const AttentionArgs &a, uint32_t span, uint32_t tiles)
 {
     const uint32_t lane = threadIdx.x & 63, longest = longest_of(tiles ? span : 0);
@@ -632,7 +634,7 @@ constexpr int kFewKeys = 32;    // to a wave at a time
 // entries are asked for together with the sequence's length wherever they do not depend on it.
 // Two waves to a SIMD: three would have 168 registers, and what does not fit them costs more (276 us for those 32 tokens).
 // Of 8-bit pages a lane's load is 16 elements and half the registers do, so there are three.  One token over 128K (32, 8, 128):
-// 52.8 us with its join, 5.2 TB/s; 32 over ragged 16K 113 us, 4.4 TB/s (116 if the values, each line one load's, stay in the
+// 51.7 to 52.8 us by card with its join, 5.2 TB/s; 32 over ragged 16K 113 us, 4.4 TB/s (116 if the values, each line one load's, stay in the
 // caches; 119 if keys go past them as well, whose lines are two loads').  64 keys at a time and two waves: 61 and 129.
 template <class T, int DP, int KIND = kCausal16>
 __global__ __launch_bounds__(kFewWaves * 64, KIND == kEight && DP <= 128 ? 3 : 2) void attention_few(const AttentionArgs a)
@@ -993,10 +995,10 @@ __device__ __forceinline__ Part part_of(const AttentionArgs &a, uint32_t rest, b
 // Drafts of a few tokens, whose group's heads make 17 to 64 rows: attention_few with products of 32 rows.  A wave has 32
 // rows and 32 keys at a time, which its lanes take from memory as the products want them; values pass through the wave's
 // own part of LDS, to be read by columns.  With two groups of rows (RG) neighbouring waves load the same keys.
-// Bound by reading the cache up to 32 rows: 8 drafts over 128K (32 heads, 8 KV heads, 128) 97 us, 5.5 TB/s with the join, in 8
-// bits 60, 4.6; trees of 8 x 16 over up to 8K 45 to 49 us, where workgroups of 64 rows in attention_rows took 175.  With 64 rows
-// by the vector unit and each wave's own turn: 16 drafts over 128K in 8 bits 93 us; all 64 rows in one wave, without another
-// wave on the SIMD to fill the gaps, took 153.
+// Bound by reading the cache up to 32 rows: 8 drafts over 128K (32 heads, 8 KV heads, 128) 93 to 97 us by card, 5.5 to 5.8 TB/s
+// with the join, in 8 bits 57 to 60, 4.6 to 4.9; trees of 8 x 16 over up to 8K 45 to 49 us, where workgroups of 64 rows in
+// attention_rows took 175.  With 64 rows by the vector unit and each wave's own turn: 16 drafts over 128K in 8 bits 88 to 94 us;
+// all 64 rows in one wave, without another wave on the SIMD to fill the gaps, took 153.
 template <class T, int DP, int KIND, int RG>
 __global__ __launch_bounds__(kFewWaves * RG * 64, DP > 128 ? 1 : 2) void attention_some(const AttentionArgs a)
 {

@@ -186,7 +186,8 @@ Cut cut_of(const CacheView &c, uint32_t window, const CutRule &rule, bool tree =
 Cut attention_cut(const CacheView &c, uint32_t window) { return cut_of(c, window, {kFewRows, 1024}); }
 
 // Half as many parts: they move half the bytes of 8-bit pages, or join the outputs of more rows.  One token over 128K in 8
-// bits (32 heads, 8 KV heads, 128) 58.0 us, 62.0 at 1024 parts; trees of 8 and of 16 tokens over 128K 63 and 92, 72 and 106.
+// bits (32 heads, 8 KV heads, 128) 51.7 us, 56.3 at 1024 parts; trees of 8 and of 16 tokens over 128K 57 and 88, 65 and 107;
+// the same over 16-bit pages 93 and 130, 100 and 149.
 Cut pages_cut(const CacheView &c, uint32_t window, bool tree = false)
 {
     return cut_of(c, window, {some_rows(c.head_dim), 512}, tree);

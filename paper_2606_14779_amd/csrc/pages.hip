@@ -12,7 +12,9 @@
 // Bound by memory and by what a token has to wait for: packed prompts of 12.7K tokens (64 heads, 8 KV heads, 64; norms, three
 // axes, pairs interleaved, 16-bit pages) 55.5 to 59.5 us by card, 263 MB at 4.7 TB/s, vector unit busy for 57 % of the cycles.  With every
 // head's weights and angles worked out anew 73; with the token's positions, sequence and slot asked for one after the other
-// 65.  A decoding step of 32 tokens takes 6.5 us on the GPU.
+// 65.  A decoding step of 32 tokens takes 6.5 us on the GPU.  Tokens of few heads (8 heads, 1 KV head, 128) take 27 us for
+// 66 MB, as a workgroup's chain of loads is paid for 4 KB; pairs that lie anyhow (24 heads, 8 KV heads, 80, half of them
+// turned) 110 for 159 MB, by their partners' loads of two bytes.
 
 #include <algorithm>
 #include <type_traits>
@@ -339,9 +341,10 @@ __global__ __launch_bounds__(256) void append(const AppendArgs a)
 }
 
 // A workgroup has kConvertTokens tokens of a sequence and KV head: all of its loads are asked for before the first store.
-// Bound by memory: 72.6K cached tokens (8 KV heads, 128) from 8 bits to 16 in 60.7 us, 308 MB at 5.1 TB/s, the rate of a copy
-// of this size by torch; 66.7 where the stores stay in the caches, 64.4 where the loads go past them too.  5001 tokens (5 KV
-// heads, 80) from 16 bits to 8 take 7.8 us, four dependent loads and the exchanges of an exponent.
+// Bound by memory: 49.7K cached tokens (8 KV heads, 128) from 8 bits to 16 in 60.7 us, 308 MB at 5.1 TB/s, the rate of a copy
+// of this size by torch; 66.7 where the stores stay in the caches, 64.4 where the loads go past them too.  128K from 16 bits to
+// 8 in 165 us, 814 MB at 4.9 TB/s, and back in 162.  5001 tokens (5 KV heads, 80) from 16 bits to 8 take 7.8 us, four dependent
+// loads and the exchanges of an exponent.
 template <class T, bool BACK, int ROWS>
 __global__ __launch_bounds__(256) void convert(const ConvertArgs a)
 {
